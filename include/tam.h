@@ -16,7 +16,10 @@
  *                     mask[n][v] = [token v is valid at node n] (device);
  *   tam_apply_mask -- logits[b, v] = -inf where mask[node_ids[b]][v] == 0, in place;
  *   tam_advance    -- out[b] = the node reached from node_ids[b] by the bytes of
- *                     token_ids[b], or TAM_DEAD.
+ *                     token_ids[b], or TAM_DEAD;
+ * and, for the decode step around them, other edits of the logits in the same
+ * pass (tam_adjust_logits), the pages of a K/V cache (tam_pages_*) and attention
+ * of new tokens over it (tam_attend).
  *
  * Conventions fixed by this interface (the paper leaves them open):
  *   - End of a value: every string is followed by a terminator byte T
@@ -85,7 +88,7 @@ typedef enum {
     TAM_E_STATE = -6       /* operation not available for this handle (see flags) */
 } tam_status;
 
-enum { TAM_DTYPE_FP32 = 0, TAM_DTYPE_BF16 = 1 };
+enum { TAM_DTYPE_FP32 = 0, TAM_DTYPE_BF16 = 1, TAM_DTYPE_FP16 = 2 /* the K/V cache's entry points only */ };
 
 enum {
     /* Build the host tables only: no HIP call, no device memory.  tam_info_get
@@ -468,6 +471,187 @@ void tam_destroy(tam_handle *h);
  */
 tam_status tam_format_rows_noalloc(const uint8_t *classes, int64_t L, int terminator, const tam_vocab *vocab,
                                    uint64_t *out, int64_t out_stride_words, int64_t *pairs_out, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Around the mask: what else a decode step does.  None of these entry points
+ * allocates or synchronises; each only launches kernels on `stream` (and may be
+ * captured into a graph).  Scratch is the caller's (`work`, 16-byte aligned,
+ * sizes below); calls that may overlap need scratch of their own.
+ */
+
+/* Edits of a row's logits other than the mask.  Every pointer is device memory;
+ * a null one leaves its part out. */
+typedef struct {
+    const int32_t *tokens;     /* [B][tokens_stride] the tokens of each row's text so far */
+    int64_t tokens_stride;     /* elements between rows, >= history */
+    int64_t history;           /* columns of `tokens`, 0 .. TAM_MAX_HISTORY */
+    const int32_t *length;     /* [B] tokens of the row (null: history); clamped to 0 .. history */
+    const int32_t *prompt;     /* [B] how many of them are the prompt's (null: none); clamped to 0 .. length */
+    const float *repetition;   /* [B] penalty of every token of the text, > 0 (null: 1) */
+    const float *frequency;    /* [B] subtracted once per occurrence after the prompt (null: 0) */
+    const float *presence;     /* [B] subtracted once from tokens that occur after the prompt (null: 0) */
+    const int32_t *bias_ids;   /* [B][bias_stride] tokens that get a bias */
+    const float *bias;         /* [B][bias_stride] and the bias of each */
+    int64_t bias_stride;       /* elements between rows of both, >= biases */
+    int64_t biases;            /* columns of both, 0 .. TAM_MAX_BIASES */
+} tam_edits;
+
+enum { TAM_MAX_HISTORY = (1 << 19) - 1, TAM_MAX_BIASES = (1 << 12) - 1 };
+
+/*
+ * tam_adjust_logits -- penalties for repeated tokens, biases and the grammar's
+ * mask on logits, in place, each logit read and written at most once.  With x
+ * the logit of row b and token v, n the occurrences of v in tokens[b] after the
+ * prompt, and "seen" if v occurs anywhere in the row's text:
+ *     x = x > 0 ? x / repetition[b] : x * repetition[b]     if seen
+ *     x = x - frequency[b] * n;  x = x - presence[b]        if n > 0
+ *     x = x + bias                                          if bias_ids[b] names v (the last entry that does)
+ *     x = -inf                                              if v is not valid in row b
+ * in fp32, rounded once.  A valid token that is neither seen nor named keeps its
+ * bits; columns v >= V are not touched; ids outside [0, V) name no token.
+ *
+ * The mask is one of:
+ *   h          a handle: v is valid as for tam_apply_mask at node ids[b] (V must
+ *              be the handle's);
+ *   rows       canonical mask rows (device uint64[num_rows][rows_stride], rows_stride
+ *              >= ceil(V/64), 8-byte aligned; bits >= V are not looked at): row b
+ *              has the mask row ids[b], or nothing valid when ids[b] is outside [0, num_rows);
+ *   neither    (both null; ids is not read) every token is valid.
+ * A full table (and `rows`) is masked and edited in one pass; the other
+ * representations of a handle are edited first and then masked.
+ *
+ *   ids         device int32[B] with a mask.
+ *   edits       NULL = none.
+ *   logits, dtype, row_stride   as for tam_apply_mask.
+ * Errors: TAM_E_INVAL, TAM_E_STATE, TAM_E_DEVICE.  TAM_FLAG_LAZY_ROWS handles
+ * order their calls as for tam_apply_mask.
+ */
+tam_status tam_adjust_logits(const tam_handle *h, const uint64_t *rows, int64_t num_rows, int64_t rows_stride,
+                             const int32_t *ids, const tam_edits *edits, int64_t B, int64_t V, void *logits,
+                             int dtype, int64_t row_stride, void *stream);
+
+/*
+ * A paged K/V cache: the caller's memory, described for each call.  A sequence
+ * (slot) of length[s] tokens holds its token t in page table[s][t / page_tokens],
+ * at place t % page_tokens.  The pool has `planes` planes (a K and a V plane per
+ * layer), and a page number stands for that page of every plane.  refs[p] counts
+ * the table entries that name page p (a caller may add holders of its own); a
+ * page at 0 is free.  Table entries past a slot's pages are not read.
+ */
+typedef struct {
+    void *data;            /* device; may be null with planes == 0 */
+    int64_t planes;
+    int64_t plane_stride;  /* bytes between planes */
+    int64_t page_stride;   /* bytes between the pages of a plane */
+    int64_t page_bytes;    /* bytes of a page of one plane */
+    int64_t num_pages;     /* 1 .. 2^31 - 2 */
+    int64_t page_tokens;   /* a power of two, 1 .. 65536 */
+    int32_t *table;        /* device [slots][table_stride] */
+    int64_t slots;
+    int64_t max_pages;     /* pages that a slot can hold: columns of the table */
+    int64_t table_stride;  /* elements between rows, >= max_pages */
+    int32_t *length;       /* device [slots] */
+    int32_t *refs;         /* device [num_pages] */
+} tam_pages;
+
+/* tam_pages_work -- bytes of scratch that a tam_pages_* call over n rows takes
+ * (-1 on a bad argument). */
+int64_t tam_pages_work(const tam_pages *c, int64_t n);
+
+/*
+ * tam_pages_fork -- slot slots[i] becomes a copy of the first lengths[i] tokens of
+ * the sequence that slot parents[i] held before the call, for all i at once, by
+ * naming its pages: beams take over their parents (parents may be among the
+ * slots, in any order), sequences are cut back (parents[i] = slots[i]) and freed
+ * (parents[i] outside [0, slots): length 0).  The counts follow; pages that
+ * nothing names any more are free.  Entries of a written row past its pages
+ * become -1.
+ *   slots, parents  device int32[n]; the slots are distinct; one outside
+ *                   [0, c->slots) is left out.
+ *   lengths         device int32[n], or NULL for the parents' whole length.
+ *   work            tam_pages_work(c, n) bytes.
+ * No page is copied: a last page that stays shared is copied by tam_pages_extend.
+ */
+tam_status tam_pages_fork(const tam_pages *c, const int32_t *slots, const int32_t *parents, const int32_t *lengths,
+                          int64_t n, void *work, void *stream);
+
+/*
+ * tam_pages_extend -- room for counts[i] more tokens in slot slots[i] (<= 0: none),
+ * for every row or for none.  A row whose last page is partly filled writes on
+ * in that page; if others hold the page too it takes a page of its own and the
+ * contents are copied, in every plane.  (If every holder of the page is
+ * among the rows, the last of them in the order of the list keeps it.)  Pages
+ * are taken from the free ones in ascending order, row after row.
+ *   info  device int32[4]: 1 if done, else 0 and nothing has changed; pages
+ *         needed; pages that were free; rows that max_pages is too small for.
+ *   slots, counts  device int32[n]; the slots are distinct.
+ *   work  tam_pages_work(c, n) bytes.
+ */
+tam_status tam_pages_extend(const tam_pages *c, const int32_t *slots, const int32_t *counts, int64_t n, int32_t *info,
+                            void *work, void *stream);
+
+/*
+ * tam_pages_compact -- the pages in use move to the numbers 0 .. used - 1: each
+ * one numbered `used` or more, in ascending order, into the next free page
+ * below, in every plane, with its count and the table entries of every slot.
+ * Entries past a slot's pages become -1.
+ *   info   device int32[2]: pages in use, pages moved.
+ *   moved  device int32[num_pages]: the new number of each page, -1 of a free one.
+ *   work   tam_pages_work(c, 0) bytes.
+ */
+tam_status tam_pages_compact(const tam_pages *c, int32_t *info, int32_t *moved, void *work, void *stream);
+
+/* The new tokens of a call, and where K and V of one layer lie.  Row i's tokens
+ * are offsets[i] .. offsets[i+1] - 1 of the call's `tokens` (offsets: device
+ * int32[rows + 1], non-decreasing, null: one token per row); they are the last
+ * ones of slot slots[i] (null: slot i), whose length counts them already, so
+ * token j of n has the position length - n + j.  Element (page p, head h, place t,
+ * dimension d) of K is at k[p * page_stride + h * head_stride + t * token_stride + d],
+ * in elements of `dtype`; V alike.  The strides are multiples of 8 and the
+ * pointers 16-byte aligned. */
+typedef struct {
+    void *k, *v;
+    int64_t page_stride, head_stride, token_stride;
+    int64_t num_pages, page_tokens;       /* as in tam_pages */
+    int64_t kv_heads, head_dim;           /* head_dim: a multiple of 8, 8 .. 128 */
+    int dtype;                            /* TAM_DTYPE_BF16 or TAM_DTYPE_FP16 */
+    const int32_t *table;                 /* as in tam_pages; an entry outside the pool names no tokens */
+    int64_t slots, max_pages, table_stride;
+    const int32_t *length;
+    int64_t rows, tokens;
+    const int32_t *offsets, *slot_ids;
+    int64_t longest;                      /* the longest row's tokens, or an upper bound (0: tokens): a hint for the
+                                             launch, the result does not depend on it */
+} tam_chunk;
+
+/*
+ * tam_pages_store -- the new tokens' K and V into their pages.  Element (token t,
+ * head h, dimension d) of the new K is at k_new[t * k_token + h * k_head + d] (a
+ * multiple of 8 each, 16-byte aligned), V alike.  Tokens whose position is
+ * negative, past the slot's pages or in a page outside the pool are left out.
+ */
+tam_status tam_pages_store(const tam_chunk *c, const void *k_new, int64_t k_token, int64_t k_head, const void *v_new,
+                           int64_t v_token, int64_t v_head, void *stream);
+
+/*
+ * tam_attend -- attention of the new tokens over their sequences: with keys 0 ..
+ * position of its slot, query (token t, head h) reads head h / (heads / kv_heads):
+ *     out[t][h] = sum_j exp(scale q k_j - lse) v_j,   lse[t][h] = log sum_j exp(scale q k_j)
+ * with the sums and the softmax in fp32 and out rounded once to `dtype`; the
+ * weights are rounded to `dtype` before they meet V.  A query without keys
+ * (position < 0) gets out = 0 and lse = -inf.
+ *   q     device, element (t, h, d) at q[t * q_token + h * q_head + d]; strides
+ *         multiples of 8, 16-byte aligned.
+ *   out   device, like q with out_token and out_head; tokens of no row are not written.
+ *   lse   device float[tokens][heads], or NULL.
+ *   work  tam_attend_work(c, heads) bytes.
+ * Errors: TAM_E_INVAL, TAM_E_DEVICE.
+ */
+tam_status tam_attend(const tam_chunk *c, const void *q, int64_t q_token, int64_t q_head, int64_t heads, float scale,
+                      void *out, int64_t out_token, int64_t out_head, float *lse, void *work, void *stream);
+
+/* tam_attend_work -- bytes of scratch of tam_attend (-1 on a bad argument). */
+int64_t tam_attend_work(const tam_chunk *c, int64_t heads);
 
 /* Message of the last failing call on this thread ("" if none). */
 const char *tam_last_error(void);

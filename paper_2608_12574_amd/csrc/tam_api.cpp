@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "host_build.hpp"
+#include "step.hpp"
 #include "tam_internal.hpp"
 #include "trie_layout.hpp"
 
@@ -147,6 +148,16 @@ tam_status hip_fail(hipError_t e, const char *what) {
         const hipError_t e_ = (expr);                      \
         if (e_ != hipSuccess) return hip_fail(e_, #expr);  \
     } while (0)
+
+}  // namespace
+
+// for the entry points in step_api.cpp
+namespace tam {
+void api_begin() { g_err.clear(); }
+tam_status api_fail(tam_status st, const std::string &msg) { return fail(st, msg); }
+}  // namespace tam
+
+namespace {
 
 double ms_since(std::chrono::steady_clock::time_point t0) {
     return std::chrono::duration<double, std::milli>(std::chrono::steady_clock::now() - t0).count();
@@ -1369,6 +1380,48 @@ tam_status tam_apply_mask(const tam_handle *h, const int32_t *node_ids, int64_t 
     }
     TAM_HIP(tam::launch_apply(h->dt, node_ids, B, logits, dtype, row_stride, s));
     return TAM_OK;
+}
+
+tam_status tam_adjust_logits(const tam_handle *h, const uint64_t *rows, int64_t num_rows, int64_t rows_stride,
+                             const int32_t *ids, const tam_edits *edits, int64_t B, int64_t V, void *logits,
+                             int dtype, int64_t row_stride, void *stream) {
+    g_err.clear();
+    if (B < 0) return fail(TAM_E_INVAL, "B must be >= 0");
+    if (V < 1 || V >= INT32_MAX) return fail(TAM_E_INVAL, "V must be in 1 .. 2^31 - 2");
+    if (h && rows) return fail(TAM_E_INVAL, "a handle and mask rows");
+    if (h && h->V != V) return fail(TAM_E_INVAL, "V is not the handle's vocabulary size");
+    if (dtype != TAM_DTYPE_FP32 && dtype != TAM_DTYPE_BF16) return fail(TAM_E_INVAL, "dtype must be FP32 or BF16");
+    if (row_stride < V) return fail(TAM_E_INVAL, "row_stride must be >= V");
+    const size_t elem = dtype == TAM_DTYPE_BF16 ? 2 : 4;
+    if (B > 0 && (!logits || ((h || rows) && !ids))) return fail(TAM_E_INVAL, "null device pointer");
+    if ((reinterpret_cast<uintptr_t>(logits) % elem) != 0) return fail(TAM_E_INVAL, "logits are not element-aligned");
+    if (rows && (num_rows < 0 || rows_stride < (V + 63) / 64 || (reinterpret_cast<uintptr_t>(rows) & 7) != 0))
+        return fail(TAM_E_INVAL, "rows must be 8-byte aligned, num_rows >= 0 and rows_stride >= ceil(V/64)");
+    tam_edits e{};
+    if (edits) e = *edits;
+    if (e.tokens && (e.history < 0 || e.history > TAM_MAX_HISTORY || e.tokens_stride < e.history))
+        return fail(TAM_E_INVAL, "history must be in 0 .. 2^19 - 1 and tokens_stride >= history");
+    if (!e.tokens) e.history = 0;
+    if ((e.bias_ids != nullptr) != (e.bias != nullptr)) return fail(TAM_E_INVAL, "bias_ids and bias go together");
+    if (e.bias_ids && (e.biases < 0 || e.biases > TAM_MAX_BIASES || e.bias_stride < e.biases))
+        return fail(TAM_E_INVAL, "biases must be in 0 .. 4095 and bias_stride >= biases");
+    if (h) {
+        tam_status st = check_device_handle(h);
+        if (st == TAM_OK) st = device_errors(h);
+        if (st != TAM_OK) return st;
+    }
+    if (B == 0) return TAM_OK;
+    const bool edit = (e.tokens && e.history > 0) || (e.bias_ids && e.biases > 0);
+    const bool dense = h && h->dt.table && !h->tails && !is_lazy(h);
+    if (!rows && !edit) return h ? tam_apply_mask(h, ids, B, logits, dtype, row_stride, stream) : TAM_OK;
+    TAM_HIP(hipGetLastError());
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (dense)
+        TAM_HIP(tam::launch_adjust(h->dt.table, h->N, h->Wp, ids, e, B, V, logits, dtype, row_stride, s));
+    else
+        TAM_HIP(tam::launch_adjust(rows, num_rows, rows_stride, rows ? ids : nullptr, e, B, V, logits, dtype,
+                                   row_stride, s));
+    return h && !dense ? tam_apply_mask(h, ids, B, logits, dtype, row_stride, stream) : TAM_OK;
 }
 
 tam_status tam_advance(const tam_handle *h, const int32_t *node_ids, const int32_t *token_ids, int64_t B,

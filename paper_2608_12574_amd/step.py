@@ -1,0 +1,291 @@
+"""What a decode step does beside the mask: edits of logits, and a paged K/V cache.
+
+As in ``tam``, this module marshals arguments only; every step runs in
+``libtam.so`` on the stream given, or torch's current stream.  Scratch comes from
+torch's caching allocator.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import tam as _tam
+from .tam import DTYPE_BF16, DTYPE_FP16, TAM_OK, Chunk, Edits, Pages, TamError, _calls, _check
+
+
+def _bad(where, what):
+    return TamError(-1, where, what)
+
+
+def _stream(c, stream):
+    return c.stream() if stream is None else stream.cuda_stream
+
+
+def _int32(where, name, t, shape=None, null=True):
+    """The pointer of a contiguous device int32 tensor (None: null)."""
+    if t is None:
+        if null:
+            return None
+        raise _bad(where, f"{name} is missing")
+    if t.dtype is not _calls().int32 or not t.is_cuda or not t.is_contiguous():
+        raise _bad(where, f"{name} must be a contiguous int32 tensor on the GPU")
+    if shape is not None and tuple(t.shape) != shape:
+        raise _bad(where, f"{name} has shape {tuple(t.shape)}, not {shape}")
+    return t.data_ptr()
+
+
+def _rows_of(where, name, t, B, dtype):
+    """(pointer, row stride, columns) of a device [B, n] tensor whose rows are contiguous."""
+    if t is None:
+        return None, 0, 0
+    if t.dtype is not dtype or not t.is_cuda or t.dim() != 2 or t.shape[0] != B or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on the GPU with contiguous rows")
+    return t.data_ptr(), max(t.stride(0), t.shape[1]) if B == 1 else t.stride(0), t.shape[1]
+
+
+def _adjust(logits, stream, handle=None, rows=None, ids=None, tokens=None, length=None, prompt=None, repetition=None,
+            frequency=None, presence=None, bias_ids=None, bias=None):
+    import torch
+    where = "tam_adjust_logits"
+    c = _tam._calls_made or _calls()
+    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in c.dtypes or (
+            logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise _bad(where, "logits must be a [B, V] fp32 or bf16 tensor on the GPU with contiguous rows")
+    B, V = logits.shape
+    if handle is not None:
+        if V < handle.vocab_size:
+            raise _bad(where, f"logits have {V} columns, the vocabulary {handle.vocab_size} tokens")
+        V = handle.vocab_size
+    masked = handle is not None or rows is not None
+    ids_p = _int32(where, "node_ids" if handle is not None else "row_ids", ids, (B,), null=not masked)
+    num_rows = stride = 0
+    rows_p = None
+    if rows is not None:
+        if rows.dtype is not torch.int64 or not rows.is_cuda or rows.dim() != 2 or rows.shape[1] < (V + 63) // 64 or (
+                rows.shape[1] > 1 and rows.stride(1) != 1):
+            raise _bad(where, f"rows must be an [R, {(V + 63) // 64}] int64 tensor on the GPU with contiguous rows")
+        rows_p, num_rows, stride = rows.data_ptr(), rows.shape[0], max(rows.stride(0), rows.shape[1])
+    e = Edits()
+    e.tokens, e.tokens_stride, e.history = _rows_of(where, "tokens", tokens, B, c.int32)
+    e.length = _int32(where, "length", length, (B,))
+    e.prompt = _int32(where, "prompt", prompt, (B,))
+    for name, t in (("repetition", repetition), ("frequency", frequency), ("presence", presence)):
+        if t is not None:
+            if t.dtype is not torch.float32 or not t.is_cuda or tuple(t.shape) != (B,) or not t.is_contiguous():
+                raise _bad(where, f"{name} must be a contiguous [{B}] fp32 tensor on the GPU")
+            setattr(e, name, t.data_ptr())
+    e.bias_ids, e.bias_stride, e.biases = _rows_of(where, "bias_ids", bias_ids, B, c.int32)
+    e.bias, other, n = _rows_of(where, "bias", bias, B, torch.float32)
+    if (e.bias_stride, e.biases) != (other, n):
+        raise _bad(where, "bias_ids and bias must have the same shape and strides")
+    rc = _tam.lib().tam_adjust_logits(handle._raw if handle is not None else None, rows_p, num_rows, stride, ids_p,
+                                      ctypes.byref(e), B, V, logits.data_ptr(), c.dtypes[logits.dtype],
+                                      logits.stride(0) if B > 1 else max(logits.stride(0), V), _stream(c, stream))
+    if rc != TAM_OK:
+        _check(rc, where)
+    return logits
+
+
+def adjust_logits(logits, tokens=None, length=None, prompt=None, repetition=None, frequency=None, presence=None,
+                  bias_ids=None, bias=None, rows=None, row_ids=None, stream=None):
+    """Penalties for repeated tokens, biases and a mask on ``logits`` [B, V] (fp32 or
+    bf16), in place and in one pass.  A token ``v`` of row ``b`` that occurs in
+    ``tokens[b, :length[b]]`` has its logit divided (multiplied where it is not
+    positive) by ``repetition[b]``; ``frequency[b]`` is subtracted for each time it occurs
+    after the first ``prompt[b]`` tokens, ``presence[b]`` once if it does; then the
+    ``bias`` of the last entry of ``bias_ids[b]`` that names it is added.  Ids outside
+    the vocabulary (-1 fills up rows) name no token.  ``rows`` [R, ceil(V/64)]: mask
+    rows as ``export_rows`` gives them (int64); row ``b`` keeps the tokens of mask
+    row ``row_ids[b]``, none when that is outside [0, R), and the others become -inf.
+    Everything but ``logits`` is optional; ``Handle.adjust_logits`` takes the mask from
+    a handle's nodes instead."""
+    return _adjust(logits, stream, rows=rows, ids=row_ids, tokens=tokens, length=length, prompt=prompt,
+                   repetition=repetition, frequency=frequency, presence=presence, bias_ids=bias_ids, bias=bias)
+
+
+class PageCache:
+    """A paged K/V cache.
+
+    ``data`` [2 * layers, pages, kv_heads, page_tokens, head_dim] (bf16 or fp16): plane
+    2 l is layer l's K, plane 2 l + 1 its V.  ``table`` [slots, max_pages] int32, ``length``
+    [slots] int32 and ``refs`` [pages] int32 are the sequences: token t of slot s lies in
+    page ``table[s, t // page_tokens]``; ``refs`` counts the table entries that name a
+    page, and a page at 0 is free.  The tensors are the caller's and change in
+    place; the tables change on the device, and nothing here waits for it.
+    """
+
+    def __init__(self, data, table, length, refs):
+        import torch
+        where = "PageCache"
+        if data.dim() != 5 or not data.is_cuda or data.dtype not in (torch.bfloat16, torch.float16):
+            raise _bad(where, "data must be a [2 * layers, pages, kv_heads, page_tokens, head_dim] bf16 or fp16 "
+                              "tensor on the GPU")
+        planes, pages, kv, page, dim = data.shape
+        if planes < 2 or planes % 2 or not data[0, 0].is_contiguous():
+            raise _bad(where, "data needs a K and a V plane per layer and contiguous pages")
+        if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_cuda or (
+                table.shape[1] > 1 and table.stride(1) != 1):
+            raise _bad(where, "table must be a [slots, max_pages] int32 tensor on the GPU with contiguous rows")
+        slots, width = table.shape
+        stride = max(table.stride(0), width)
+        length_p = _int32(where, "length", length, (slots,), null=False)
+        refs_p = _int32(where, "refs", refs, (pages,), null=False)
+        self.data, self.table, self.length, self.refs = data, table, length, refs
+        self.layers, self.kv_heads, self.page_tokens, self.head_dim = planes // 2, kv, page, dim
+        self._torch = torch
+        size = data.element_size()
+        self._pages = Pages(data.data_ptr(), planes, data.stride(0) * size, data.stride(1) * size, kv * page * dim * size,
+                            pages, page, table.data_ptr(), slots, width, stride, length_p, refs_p)
+        self._pages_ref = ctypes.byref(self._pages)
+        dtype = DTYPE_FP16 if data.dtype is torch.float16 else DTYPE_BF16
+        self._chunk = Chunk(None, None, data.stride(1), data.stride(2), data.stride(3), pages, page, kv, dim, dtype,
+                            table.data_ptr(), slots, width, stride, length_p)
+        self._chunk_ref = ctypes.byref(self._chunk)
+        if _tam.lib().tam_pages_work(self._pages_ref, 0) < 0:
+            _check(-1, where)
+
+    @classmethod
+    def empty(cls, layers, kv_heads, head_dim, pages, slots, max_pages, page_tokens=16, dtype=None, device="cuda"):
+        """A cache of ``pages`` free pages and ``slots`` empty sequences of at most ``max_pages`` pages."""
+        import torch
+        data = torch.empty((2 * layers, pages, kv_heads, page_tokens, head_dim), dtype=dtype or torch.bfloat16,
+                           device=device)
+        return cls(data, torch.full((slots, max_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(slots, dtype=torch.int32, device=device),
+                   torch.zeros(pages, dtype=torch.int32, device=device))
+
+    # -- pages -----------------------------------------------------------------
+    def _empty(self, shape, dtype, stream):
+        """Memory for a call on ``stream``: from that stream's share of torch's allocator, so that
+        nothing still running on another stream holds it."""
+        torch = self._torch
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.data.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.data.device)
+
+    def _work(self, n, stream):
+        size = _tam.lib().tam_pages_work(self._pages_ref, n)
+        if size < 0:
+            _check(-1, "tam_pages_work")
+        return self._empty(size, self._torch.uint8, stream)
+
+    def _on(self, stream):
+        return _stream(_tam._calls_made or _calls(), stream)
+
+    def fork(self, slots, parents, lengths=None, stream=None):
+        """Slot ``slots[i]`` becomes a copy of the first ``lengths[i]`` tokens (all of them without
+        ``lengths``) of slot ``parents[i]`` as it was before the call; a parent outside the
+        slots (-1) frees the slot.  Pages are shared, not copied."""
+        where = "tam_pages_fork"
+        n = slots.numel()
+        s, p = _int32(where, "slots", slots, (n,)), _int32(where, "parents", parents, (n,))
+        work = self._work(n, stream)
+        rc = _tam.lib().tam_pages_fork(self._pages_ref, s, p, _int32(where, "lengths", lengths, (n,)), n,
+                                       work.data_ptr(), self._on(stream))
+        if rc != TAM_OK:
+            _check(rc, where)
+
+    def free(self, slots, stream=None):
+        """The slots' sequences end; pages that no other slot names are free."""
+        parents = self._empty(slots.shape, slots.dtype, stream)
+        if stream is None:
+            parents.fill_(-1)
+        else:
+            with self._torch.cuda.stream(stream):
+                parents.fill_(-1)
+        self.fork(slots, parents, stream=stream)
+
+    def extend(self, slots, counts, stream=None):
+        """Room for ``counts[i]`` more tokens in slot ``slots[i]``, for all of them or for none;
+        a shared, partly filled last page is copied first.  Returns int32 [4] on the GPU: 1 if done
+        (else 0, and nothing has changed), pages needed, pages that were free, slots that
+        ``max_pages`` is too small for."""
+        where = "tam_pages_extend"
+        n = slots.numel()
+        s, c = _int32(where, "slots", slots, (n,)), _int32(where, "counts", counts, (n,))
+        work = self._work(n, stream)
+        info = self._empty(4, self._torch.int32, stream)
+        rc = _tam.lib().tam_pages_extend(self._pages_ref, s, c, n, info.data_ptr(), work.data_ptr(), self._on(stream))
+        if rc != TAM_OK:
+            _check(rc, where)
+        return info
+
+    def compact(self, stream=None):
+        """The pages in use move to the front of the pool.  Returns int32 [2] (pages in use,
+        pages moved) and int32 [pages] (each page's new number, -1 of a free one), both on the GPU."""
+        work = self._work(0, stream)
+        info = self._empty(2, self._torch.int32, stream)
+        moved = self._empty(self.refs.shape, self._torch.int32, stream)
+        rc = _tam.lib().tam_pages_compact(self._pages_ref, info.data_ptr(), moved.data_ptr(), work.data_ptr(),
+                                          self._on(stream))
+        if rc != TAM_OK:
+            _check(rc, "tam_pages_compact")
+        return info, moved
+
+    # -- a layer's new tokens ------------------------------------------------------
+    def _new(self, where, layer, tokens, offsets, slots, longest):
+        if not 0 <= layer < self.layers:
+            raise _bad(where, f"layer {layer} of {self.layers}")
+        c = self._chunk
+        c.offsets = _int32(where, "offsets", offsets)
+        if offsets is not None:
+            if offsets.dim() != 1 or offsets.numel() < 1:
+                raise _bad(where, "offsets must be [rows + 1]")
+            rows = offsets.numel() - 1
+        else:
+            rows = tokens
+        c.slot_ids = _int32(where, "slots", slots, (rows,))
+        plane = self._pages.plane_stride
+        c.k = self._pages.data + 2 * layer * plane
+        c.v = c.k + plane
+        c.rows, c.tokens, c.longest = rows, tokens, (1 if offsets is None else 0) if longest is None else longest
+        return self._chunk_ref
+
+    def _vectors(self, where, name, t, heads=None):
+        """(pointer, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
+        if (t.dim() != 3 or not t.is_cuda or t.dtype is not self.data.dtype or t.shape[2] != self.head_dim
+                or t.stride(2) != 1 or (heads is not None and t.shape[1] != heads)):
+            raise _bad(where, f"{name} must be a [tokens, {heads or 'heads'}, {self.head_dim}] {self.data.dtype} tensor "
+                              "on the GPU with contiguous vectors")
+        return t.data_ptr(), t.stride(0), t.stride(1)
+
+    def store(self, layer, k, v, offsets=None, slots=None, longest=None, stream=None):
+        """K and V [tokens, kv_heads, head_dim] of the new tokens into their pages.  Row i's tokens are
+        ``offsets[i]:offsets[i + 1]`` (one token per row without ``offsets``), the last ones of slot ``slots[i]``
+        (slot i without ``slots``), whose length counts them already (``extend``)."""
+        where = "tam_pages_store"
+        kp, vp = self._vectors(where, "k", k, self.kv_heads), self._vectors(where, "v", v, self.kv_heads)
+        if k.shape[0] != v.shape[0]:
+            raise _bad(where, "k and v have different numbers of tokens")
+        rc = _tam.lib().tam_pages_store(self._new(where, layer, k.shape[0], offsets, slots, longest), *kp, *vp,
+                                        self._on(stream))
+        if rc != TAM_OK:
+            _check(rc, where)
+
+    def attend(self, layer, q, offsets=None, slots=None, longest=None, scale=None, out=None, return_lse=False,
+               stream=None):
+        """Attention of the new tokens' queries ``q`` [tokens, heads, head_dim] over their sequences, each over the
+        tokens up to its own; ``heads`` is a multiple of ``kv_heads``.  Rows as for ``store``, whose tokens
+        have been stored.  ``scale``: of the products (1 / sqrt(head_dim)).  ``longest``: the tokens of the longest
+        row, or more, if the host knows (a hint).  Returns ``out`` (like ``q``; tokens of no row and the memory
+        between are not written) and with ``return_lse`` the fp32 [tokens, heads] logarithms of the sums."""
+        where = "tam_attend"
+        qp = self._vectors(where, "q", q)
+        T, heads = q.shape[0], q.shape[1]
+        if out is None:
+            out = self._empty((T, heads, self.head_dim), q.dtype, stream)
+        elif out.shape != q.shape:
+            raise _bad(where, "out must have q's shape")
+        op = self._vectors(where, "out", out)
+        lse = self._empty((T, heads), self._torch.float32, stream) if return_lse else None
+        chunk = self._new(where, layer, T, offsets, slots, longest)
+        lib = _tam.lib()
+        size = lib.tam_attend_work(chunk, heads)
+        if size < 0:
+            _check(-1, where)
+        work = self._empty(size, self._torch.uint8, stream) if size else None
+        rc = lib.tam_attend(chunk, *qp, heads, self.head_dim ** -0.5 if scale is None else scale, *op,
+                            lse.data_ptr() if return_lse else None, work.data_ptr() if size else None, self._on(stream))
+        if rc != TAM_OK:
+            _check(rc, where)
+        return (out, lse) if return_lse else out

@@ -21,7 +21,7 @@ LIB_PATH = os.environ.get("TAM_LIBRARY") or os.path.join(PKG, "libtam.so")
 
 TAM_OK = 0
 TAM_DEAD = -1
-DTYPE_FP32, DTYPE_BF16 = 0, 1
+DTYPE_FP32, DTYPE_BF16, DTYPE_FP16 = 0, 1, 2
 FLAG_HOST_ONLY, FLAG_NO_TABLE, FLAG_TIMING, FLAG_TAIL_LISTS, FLAG_LAZY_ROWS = 1, 2, 4, 8, 16
 PHASE_LISTS, PHASE_ZERO, PHASE_MARK, PHASE_COUNT = 1, 2, 4, 8
 PHASE_TABLE = PHASE_ZERO | PHASE_MARK
@@ -34,7 +34,9 @@ ENTRY_POINTS = ("tam_compile", "tam_vocab_create", "tam_compile_vocab", "tam_com
                 "tam_info_get", "tam_layout_get",
                 "tam_apply_mask", "tam_advance", "tam_export_rows", "tam_valid_counts", "tam_valid_pairs",
                 "tam_timing_get",
-                "tam_format_rows_noalloc", "tam_vocab_destroy", "tam_destroy", "tam_last_error")
+                "tam_format_rows_noalloc", "tam_vocab_destroy", "tam_destroy", "tam_last_error",
+                "tam_adjust_logits", "tam_pages_work", "tam_pages_fork", "tam_pages_extend", "tam_pages_compact",
+                "tam_pages_store", "tam_attend", "tam_attend_work")
 
 
 class TamError(RuntimeError):
@@ -74,6 +76,31 @@ class Layout(ctypes.Structure):
                 ("node_at", ctypes.POINTER(ctypes.c_int32)), ("depth", ctypes.POINTER(ctypes.c_int32)),
                 ("node_pos", ctypes.POINTER(ctypes.c_int32)), ("parent", ctypes.POINTER(ctypes.c_int32)),
                 ("errors", ctypes.c_int64)]
+
+
+class Edits(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("tokens_stride", ctypes.c_int64), ("history", ctypes.c_int64),
+                ("length", ctypes.c_void_p), ("prompt", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("bias_stride", ctypes.c_int64), ("biases", ctypes.c_int64)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("planes", ctypes.c_int64), ("plane_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("page_bytes", ctypes.c_int64), ("num_pages", ctypes.c_int64),
+                ("page_tokens", ctypes.c_int64), ("table", ctypes.c_void_p), ("slots", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("length", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p)]
+
+
+class Chunk(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("num_pages", ctypes.c_int64),
+                ("page_tokens", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("table", ctypes.c_void_p), ("slots", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("length", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("tokens", ctypes.c_int64), ("offsets", ctypes.c_void_p),
+                ("slot_ids", ctypes.c_void_p), ("longest", ctypes.c_int64)]
 
 
 class Timing(ctypes.Structure):
@@ -118,12 +145,22 @@ def lib() -> ctypes.CDLL:
         L.tam_valid_counts.argtypes = [P, P, i64, P, P]
         L.tam_valid_pairs.argtypes = [P, P, ctypes.POINTER(i64)]
         L.tam_timing_get.argtypes = [P, ctypes.POINTER(Timing)]
+        L.tam_adjust_logits.argtypes = [P, P, i64, i64, P, ctypes.POINTER(Edits), i64, i64, P, ctypes.c_int, i64, P]
+        pages, chunk = ctypes.POINTER(Pages), ctypes.POINTER(Chunk)
+        L.tam_pages_work.argtypes = [pages, i64]
+        L.tam_pages_fork.argtypes = [pages, P, P, P, i64, P, P]
+        L.tam_pages_extend.argtypes = [pages, P, P, i64, P, P, P]
+        L.tam_pages_compact.argtypes = [pages, P, P, P, P]
+        L.tam_pages_store.argtypes = [chunk, P, i64, i64, P, i64, i64, P]
+        L.tam_attend.argtypes = [chunk, P, i64, i64, i64, ctypes.c_float, P, i64, i64, P, P, P]
+        L.tam_attend_work.argtypes = [chunk, i64]
         L.tam_destroy.argtypes = [P]
         L.tam_destroy.restype = None
         L.tam_last_error.restype = ctypes.c_char_p
         for name in ENTRY_POINTS:
             if name not in ("tam_vocab_destroy", "tam_destroy", "tam_last_error"):
                 getattr(L, name).restype = ctypes.c_int
+        L.tam_pages_work.restype = L.tam_attend_work.restype = i64
         _lib = L
     return _lib
 
@@ -315,6 +352,12 @@ class Handle:
         if rc != TAM_OK:
             _check(rc, "tam_apply_mask")
         return logits
+
+    def adjust_logits(self, node_ids, logits, stream=None, **edits):
+        """In place: penalties for repeated tokens and biases (the keyword arguments of
+        ``adjust_logits``), then the mask of ``apply_mask``, in one call."""
+        from .step import _adjust
+        return _adjust(logits, stream, handle=self, ids=node_ids, **edits)
 
     def advance(self, node_ids, token_ids, out=None, stream=None):
         """out[b] = node reached from node_ids[b] by the bytes of token_ids[b], or -1."""
