@@ -1,8 +1,20 @@
 // Attention of a chunk of new tokens per sequence over a paged K/V cache.
 //
-// k_attend_rows: a wave per (token, head), 64 keys at a time: each lane takes one
-// key's product with the query, the running maximum and sum of the softmax go over the
-// wave, then every lane adds the weighted V of its dimensions.
+// Mathematics.  For a query q, o = sum_j w_j v_j / sum_j w_j with w_j = exp(scale (q k_j - m)),
+// for any m; in one pass over the keys m is the running maximum, and what was summed
+// under an older m is scaled when m grows.  Parts of the keys summed apart join the
+// same way.  m is let lag by up to 2^8 in w before it is moved, which the fp32 sums
+// and the 16-bit weights hold, so that the sums are scaled a few times per row and
+// not in each step.
+//
+// A tile is `tq` tokens of one row, times the heads that share a K/V head (their
+// rows of a product are side by side, so K and V are read once for all of them).
+// A unit is a tile's product with kKeys keys.  All units of a call, row after row,
+// head after head, tile after tile, are one line, cut into equal pieces for as
+// many blocks as the chip holds: any mix of long and short rows and chunks fills
+// it evenly.  A tile that a cut goes through leaves partial sums in the scratch, which
+// k_join adds up.  The lengths lie on the device: each block finds its piece from
+// them by a prefix sum over the rows.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -13,7 +25,17 @@
 namespace tam {
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
 constexpr int kWave = 64;
+constexpr int kThreads = 256;
+
+// Bad page numbers point here: K and V of zeros.
+__device__ const u32x4 kZeros[16] = {};
 
 struct Attend {
     const uint16_t *k, *v, *q;
@@ -24,105 +46,568 @@ struct Attend {
     int64_t table_stride, slots, max_pages, rows, tokens;
     int32_t pages, shift, heads, kv_heads, dim;
     float scale;
+    // the cut: tiles of `tq` tokens by `group` heads, `parts` of them per K/V head
+    int32_t tq, group, parts, blocks;
+    int32_t least;  // units of a block, at least
+    float *sums;    // [2 blocks][tile rows][DP] partial sums, then [2 blocks][tile rows][2] their m and sum of weights
 };
 
-template <bool kHalf>
-__device__ float wide(uint16_t h) {
-    if constexpr (kHalf) return (float)__builtin_bit_cast(_Float16, h);
-    return __uint_as_float((uint32_t)h << 16);
+// ------------------------------------------------------------------ the cut ---
+
+// sum of floor((a t + b) / m) over t in [0, n), by Euclid's steps on (a, m)
+__device__ inline int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
+    int64_t sum = 0;
+    while (true) {
+        if (a >= m) {
+            sum += (int64_t)n * (n - 1) / 2 * (a / m);
+            a %= m;
+        }
+        if (b >= m) {
+            sum += (int64_t)n * (b / m);
+            b %= m;
+        }
+        const uint64_t y = (uint64_t)a * n + b;
+        if (y < m) return sum;
+        n = (uint32_t)(y / m);
+        b = (uint32_t)(y % m);
+        const uint32_t t = m;
+        m = a;
+        a = t;
+    }
 }
+
+struct Row {
+    int32_t n, base;    // tokens of the chunk; tokens of the sequence before it (may be negative)
+    int32_t first;      // the chunk's first token
+    int64_t slot;
+};
+
+__device__ inline Row row_at(const Attend &a, int64_t i) {
+    Row r;
+    if (a.offsets) {
+        const int64_t lo = max((int64_t)a.offsets[i], (int64_t)0), hi = min((int64_t)a.offsets[i + 1], a.tokens);
+        r.first = (int32_t)lo;
+        r.n = (int32_t)max(hi - lo, (int64_t)0);
+    } else {
+        r.first = (int32_t)i;
+        r.n = i < a.tokens;
+    }
+    r.slot = a.slot_ids ? a.slot_ids[i] : i;
+    int64_t len = 0;
+    if (r.slot >= 0 && r.slot < a.slots) len = min(max((int64_t)a.length[r.slot], (int64_t)0), a.max_pages << a.shift);
+    r.base = (int32_t)(len - r.n);
+    return r;
+}
+
+// Units of the tiles before tile t of a row (all of them full).
+template <int kKeys>
+__device__ inline int64_t units_before(const Attend &a, const Row &r, uint32_t t) {
+    return t ? floor_sum(t, kKeys, a.tq, max(r.base, 0) + a.tq + kKeys - 1) : 0;
+}
+
+template <int kKeys>
+__device__ inline int64_t row_units(const Attend &a, const Row &r) {
+    if (r.n == 0) return 0;
+    const uint32_t tiles = (r.n + a.tq - 1) / a.tq;
+    return units_before<kKeys>(a, r, tiles - 1) + (max(r.base, 0) + r.n + kKeys - 1) / kKeys;
+}
+
+// A place on the line of units.
+struct Place {
+    int64_t row, total;   // the row; units of all rows
+    int64_t rest;         // units of the row before this place
+};
+
+// The place of unit number `share * piece` (share: this block's number), and the units of a
+// piece.  All threads of the block call it; row < 0 past the line's end.
+template <int kKeys>
+__device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
+    __shared__ int64_t sums[kThreads / kWave];
+    __shared__ int64_t found[2];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t per = (a.rows + kThreads - 1) / kThreads, lo = threadIdx.x * per, hi = min(lo + per, a.rows);
+    const int64_t heads = (int64_t)a.kv_heads * a.parts;
+    int64_t mine = 0;
+    for (int64_t i = lo; i < hi; ++i) mine += heads * row_units<kKeys>(a, row_at(a, i));
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int64_t up = __shfl_up(upto, d);
+        if (lane >= d) upto += up;
+    }
+    if (lane == kWave - 1) sums[wave] = upto;
+    if (threadIdx.x == 0) found[0] = -1;
+    __syncthreads();
+    Place p;
+    p.total = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / kWave; ++w) {
+        if (w < wave) upto += sums[w];
+        p.total += sums[w];
+    }
+    *piece = max((int64_t)a.least, (p.total + a.blocks - 1) / a.blocks);
+    const int64_t at = share * *piece;
+    if (at >= upto - mine && at < upto) {  // one thread: walk its rows
+        int64_t rest = at - (upto - mine);
+        int64_t i = lo;
+        for (; i < hi; ++i) {
+            const int64_t u = heads * row_units<kKeys>(a, row_at(a, i));
+            if (rest < u) break;
+            rest -= u;
+        }
+        found[0] = i;
+        found[1] = rest;
+    }
+    __syncthreads();
+    p.row = found[0];
+    p.rest = found[1];
+    return p;
+}
+
+// A tile, and the units of it before the place.
+struct Tile {
+    int32_t head, part, tile;     // K/V head and part of its group; number in the row
+    int32_t first, n;             // its first token in the chunk, and its tokens
+    int32_t heads;                // query heads of the part
+    int64_t units, done;
+};
+
+template <int kKeys>
+__device__ inline Tile tile_at(const Attend &a, const Row &r, int64_t rest) {
+    const int64_t u = row_units<kKeys>(a, r);
+    const int64_t vh = rest / u;
+    rest -= vh * u;
+    const uint32_t tiles = (r.n + a.tq - 1) / a.tq;
+    uint32_t lo = 0, hi = tiles;  // units_before(lo) <= rest < units_before(hi)
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (units_before<kKeys>(a, r, mid) <= rest) lo = mid;
+        else hi = mid;
+    }
+    Tile t;
+    t.head = (int32_t)(vh / a.parts);
+    t.part = (int32_t)(vh - (int64_t)t.head * a.parts);
+    t.tile = (int32_t)lo;
+    t.first = t.tile * a.tq;
+    t.n = min(a.tq, r.n - t.first);
+    t.heads = min(a.group, a.heads / a.kv_heads - t.part * a.group);
+    t.done = rest - units_before<kKeys>(a, r, lo);
+    t.units = (max(r.base, 0) + min((int32_t)((lo + 1) * a.tq), r.n) + kKeys - 1) / kKeys;
+    return t;
+}
+
+// ------------------------------------------------------------------ products ---
+
 template <bool kHalf>
-__device__ uint16_t narrow(float x) {
-    if constexpr (kHalf) return __builtin_bit_cast(uint16_t, (_Float16)x);
-    return __builtin_bit_cast(uint16_t, (__bf16)x);
+__device__ inline f32x4 mfma16(u32x4 x, u32x4 y, f32x4 z) {
+    if constexpr (kHalf)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), z, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), z, 0, 0, 0);
 }
 
 template <bool kHalf>
-__global__ void __launch_bounds__(kWave) k_attend_rows(Attend a) {
-    __shared__ float weight[kWave];
-    __shared__ int64_t place[kWave];
-    const int64_t t = blockIdx.x;
-    const int h = blockIdx.y, lane = threadIdx.x;
-    int64_t row = t, j = 0, n = 1;
-    if (a.offsets) {
-        if (t < a.offsets[0] || t >= a.offsets[a.rows]) return;
-        int64_t hi = a.rows;
-        row = 0;
-        while (hi - row > 1) {
-            const int64_t mid = (row + hi) >> 1;
-            if (a.offsets[mid] <= t) row = mid;
-            else hi = mid;
-        }
-        j = t - a.offsets[row];
-        n = (int64_t)a.offsets[row + 1] - a.offsets[row];
-    } else if (t >= a.rows) {
-        return;
+__device__ inline uint32_t pack(float x, float y) {  // rounded to nearest, ties to even
+    if constexpr (kHalf) {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, h2{(_Float16)x, (_Float16)y});
+    } else {
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, b2{(__bf16)x, (__bf16)y});
     }
-    const int64_t slot = a.slot_ids ? a.slot_ids[row] : row;
-    const int64_t most = a.max_pages << a.shift;
-    const int64_t len = slot >= 0 && slot < a.slots ? a.length[slot] : 0;
-    const int64_t keys = min(len - n + j + 1, most);  // visible keys
-    const uint16_t *q = a.q + t * a.q_token + h * a.q_head;
-    const int kvh = h / (a.heads / a.kv_heads);
-    float top = -INFINITY, sum = 0.f, acc[2] = {0.f, 0.f};
-    for (int64_t k0 = 0; k0 < keys; k0 += kWave) {
-        const int64_t key = k0 + lane;
-        float s = -INFINITY;
-        int64_t at = -1;
-        if (key < keys) {
-            const int32_t page = a.table[slot * a.table_stride + (key >> a.shift)];
-            if ((uint32_t)page < (uint32_t)a.pages) {
-                at = page * a.page_stride + kvh * a.head_stride + (key & ((1ll << a.shift) - 1)) * a.token_stride;
-                s = 0.f;
-                for (int d = 0; d < a.dim; ++d) s += wide<kHalf>(q[d]) * wide<kHalf>(a.k[at + d]);
-                s *= a.scale;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLag = 8.f;  // m may lag by this much, in powers of two
+
+// A tile of at most 16 kBlocks kRowWaves rows by all its keys, 32 keys per wave and
+// step; kRowWaves waves share the rows and the others the keys of a unit.  The bytes of
+// K and V bound it, so the fragments come straight from memory into registers, the next
+// step's while this one is computed, and LDS only joins the waves' sums at the end.
+// S^T = K Q^T leaves each lane the weights of one query, for the same eight keys that it
+// then holds as the second factor of O^T = V^T P^T: no weight changes lanes.  V's columns
+// are paired in registers (v_perm).
+template <int DP, int kBlocks, int kRowWaves, bool kHalf>
+__global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narrow(Attend a) {
+    constexpr int kKeyWaves = 4 / kRowWaves, kKeys = 32 * kKeyWaves;
+    constexpr int kSteps = DP / 32;  // products of 32 dimensions
+    constexpr int kCols = DP / 16;   // dimensions per lane of 16: adjacent ones
+    constexpr int kRows = 16 * kBlocks * kRowWaves;
+    __shared__ float joint[4][16][DP + 4];
+    __shared__ float tops[4][16 * kBlocks], weights[4][16 * kBlocks];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int rw = wave / kKeyWaves, kw = wave % kKeyWaves;
+    const int col = lane % 16, grp = lane / 16;
+    int64_t piece;
+    Place p = find<kKeys>(a, blockIdx.x, &piece);
+    if (p.row < 0) return;
+    const int64_t from = blockIdx.x * piece;
+    int64_t left = min(piece, p.total - from);
+    const float c = a.scale * kLog2e;
+    while (left > 0) {
+        const Row r = row_at(a, p.row);
+        const int64_t in_row = row_units<kKeys>(a, r) * a.kv_heads * a.parts;
+        if (p.rest >= in_row) {
+            ++p.row;
+            p.rest = 0;
+            continue;
+        }
+        const Tile t = tile_at<kKeys>(a, r, p.rest);
+        const int64_t take = min(t.units - t.done, left);
+        // queries, one per lane of 16 and block; rows past the tile's see no key.  Lanes
+        // past the last dimension read others of the vector (queries: zero).
+        u32x4 q[kBlocks][kSteps];
+        int32_t seen[kBlocks];  // keys that the query sees
+        const int32_t all = max(0, r.base + r.n);  // tokens of the sequence, chunk included
+        const int32_t most = max(0, min(r.base + t.first + t.n, all)), least = max(0, min(r.base + t.first + 1, all));
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            const int row = 16 * (kBlocks * rw + b) + col, tok = row / t.heads, h = row - tok * t.heads;
+            const bool is = tok < t.n;
+            seen[b] = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
+            const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
+                                  (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const int d = 32 * s + 8 * grp;
+                q[b][s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(src + d) : u32x4{0, 0, 0, 0};
             }
         }
-        float m = s;
-        for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-        m = fmaxf(m, top);
-        const float p = m == -INFINITY ? 0.f : __expf(s - m), keep = m == -INFINITY ? 1.f : __expf(top - m);
-        float total = p;
-        for (int d = 1; d < kWave; d <<= 1) total += __shfl_xor(total, d);
-        sum = sum * keep + total;
-        top = m;
-        weight[lane] = p;
-        place[lane] = at;
-        __syncthreads();
-        for (int i = 0; i < 2; ++i) {
-            const int d = lane + i * kWave;
-            acc[i] *= keep;
-            if (d < a.dim)
-                for (int x = 0; x < kWave; ++x)
-                    if (place[x] >= 0) acc[i] += weight[x] * wide<kHalf>(a.v[place[x] + d]);
+        f32x4 o[kBlocks][kCols];
+        float m[kBlocks], l[kBlocks];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            m[b] = -INFINITY;
+            l[b] = 0.f;
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) o[b][j] = f32x4{0, 0, 0, 0};
+        }
+        const uint16_t *kh = a.k + (int64_t)t.head * a.head_stride;
+        const uint16_t *vh = a.v + (int64_t)t.head * a.head_stride + (kCols * col < a.dim ? kCols * col : 0);
+        const int32_t *pages = a.table + r.slot * a.table_stride;
+        const int32_t place = (1 << a.shift) - 1;
+
+        struct Step {
+            u32x4 k[2][kSteps];
+            u32x4 v[8];  // kCols * 2 bytes of each are used
+            uint32_t bad;  // bit j: key j of the lane's eight lies in no page
+        };
+        // The keys of a step; those past the last one that the tile sees stand for it.
+        auto load = [&](int32_t k0, Step &x) {
+            x.bad = 0;
+            const uint16_t *src[8];
+            const int32_t first = k0 + 4 * grp;
+            if (k0 + 32 <= most && a.shift >= 2) {  // four keys lie side by side
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int32_t key = first + 16 * i, page = pages[key >> a.shift];
+                    const bool ok = (uint32_t)page < (uint32_t)a.pages;
+                    if (!ok) x.bad |= 15u << 4 * i;
+                    const uint16_t *at = ok ? vh + (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride
+                                            : reinterpret_cast<const uint16_t *>(kZeros);
+                    const int64_t step = ok ? a.token_stride : 0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) src[4 * i + j] = at + j * step;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int32_t key = min(first + 16 * (j / 4) + j % 4, most - 1), page = pages[key >> a.shift];
+                    const bool ok = (uint32_t)page < (uint32_t)a.pages;
+                    if (!ok) x.bad |= 1u << j;
+                    src[j] = ok ? vh + (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride
+                                : reinterpret_cast<const uint16_t *>(kZeros);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int32_t key = min(k0 + 16 * i + col, most - 1), page = pages[key >> a.shift];
+                const uint16_t *at = kh + (int64_t)((uint32_t)page < (uint32_t)a.pages ? page : 0) * a.page_stride +
+                                     (int64_t)(key & place) * a.token_stride;
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    const int d = 32 * s + 8 * grp;
+                    x.k[i][s] = *reinterpret_cast<const u32x4 *>(at + (d < a.dim ? d : 0));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (kCols == 8) {
+                    x.v[j] = *reinterpret_cast<const u32x4 *>(src[j]);
+                } else {
+                    const u32x2 y = *reinterpret_cast<const u32x2 *>(src[j]);
+                    x.v[j] = u32x4{y[0], y[1], 0, 0};
+                }
+            }
+        };
+        auto compute = [&](int32_t k0, const Step &x) {
+            u32x4 v[kCols];
+#pragma unroll
+            for (int j = 0; j < kCols; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[j][i] = __builtin_amdgcn_perm(x.v[2 * i + 1][j / 2], x.v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+            const bool masked = k0 + 32 > least || __any(x.bad);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int d = 0; d < kSteps; ++d) s[i] = mfma16<kHalf>(x.k[i][d], q[b][d], s[i]);
+                if (masked) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (k0 + 16 * (j / 4) + 4 * grp + j % 4 >= seen[b] || (x.bad >> j & 1)) s[j / 4][j % 4] = -INFINITY;
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                if (__any((top - m[b]) * c > kLag)) {  // NaN (both -inf): no
+                    const float now = fmaxf(m[b], top);
+                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
+                    m[b] = now;
+                    l[b] *= keep;
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) o[b][j] *= keep;
+                }
+                const float mc = m[b] == -INFINITY ? 0.f : m[b] * c;
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j % 4], c, -mc));
+                    l[b] += w[j];
+                }
+                u32x4 pw;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pw[i] = pack<kHalf>(w[2 * i], w[2 * i + 1]);
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) o[b][j] = mfma16<kHalf>(v[j], pw, o[b][j]);
+            }
+        };
+        const int32_t k_end = (int32_t)min((t.done + take) * kKeys, (int64_t)most);
+        int32_t k0 = (int32_t)(t.done * kKeys) + 32 * kw;
+        if (k0 < k_end) {
+            Step x, y;
+            load(k0, x);
+            while (true) {
+                int32_t k1 = k0 + kKeys;
+                if (k1 < k_end) load(k1, y);
+                compute(k0, x);
+                if (k1 >= k_end) break;
+                k0 = k1 + kKeys;
+                if (k0 < k_end) load(k0, x);
+                compute(k1, y);
+                if (k0 >= k_end) break;
+            }
+        }
+        // join the waves that shared the keys: the largest m, then the sums under it
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            l[b] += __shfl_xor(l[b], 16);
+            l[b] += __shfl_xor(l[b], 32);
+            if (grp == 0) {
+                tops[wave][16 * b + col] = m[b];
+                weights[wave][16 * b + col] = l[b];
+            }
         }
         __syncthreads();
+        const bool whole = take == t.units;
+        const int64_t at = 2 * (int64_t)blockIdx.x + (t.done == 0);  // a cut tile's partial sums
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kKeyWaves; ++w) top = fmaxf(top, tops[rw * kKeyWaves + w][16 * b + col]);
+            const float keep = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[b] - top) * c);
+            // o[b][j][i] is dimension kCols (4 grp + i) + j of query `col`
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < kCols; j += 4)
+                    *reinterpret_cast<f32x4 *>(&joint[wave][col][kCols * (4 * grp + i) + j]) =
+                        f32x4{o[b][j][i], o[b][j + 1][i], o[b][j + 2][i], o[b][j + 3][i]} * keep;
+            __syncthreads();
+            // a thread takes one query of each wave's rows and kCols dimensions
+            const int qr = threadIdx.x / 16, d0 = kCols * (threadIdx.x % 16);
+#pragma unroll
+            for (int x = 0; x < kRowWaves; ++x) {
+                const int out_row = 16 * (kBlocks * x + b) + qr, tok = out_row / t.heads, h = out_row - tok * t.heads;
+                if (tok >= t.n) continue;
+                float sum[kCols] = {}, lsum = 0.f, mx = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < kKeyWaves; ++w) mx = fmaxf(mx, tops[x * kKeyWaves + w][16 * b + qr]);
+#pragma unroll
+                for (int w = 0; w < kKeyWaves; ++w) {
+                    const int of = x * kKeyWaves + w;
+                    const float mw = tops[of][16 * b + qr];
+                    if (mw > -INFINITY) lsum += weights[of][16 * b + qr] * __builtin_amdgcn_exp2f((mw - mx) * c);
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) sum[j] += joint[of][qr][d0 + j];
+                }
+                if (whole) {
+                    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+                    const int64_t token = r.first + t.first + tok;
+                    const int64_t head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
+                    uint16_t *dst = a.out + token * a.out_token + head * a.out_head + d0;
+                    if (d0 < a.dim) {
+                        uint32_t y[kCols / 2];
+#pragma unroll
+                        for (int j = 0; j < kCols / 2; ++j) y[j] = pack<kHalf>(sum[2 * j] * inv, sum[2 * j + 1] * inv);
+                        if constexpr (kCols == 8) *reinterpret_cast<u32x4 *>(dst) = u32x4{y[0], y[1], y[2], y[3]};
+                        else *reinterpret_cast<u32x2 *>(dst) = u32x2{y[0], y[1]};
+                    }
+                    if (a.lse && d0 == 0)
+                        a.lse[token * a.heads + head] = lsum > 0.f ? mx * a.scale + logf(lsum) : -INFINITY;
+                } else {
+                    float *dst = a.sums + (at * kRows + out_row) * DP + d0;
+#pragma unroll
+                    for (int j = 0; j < kCols; j += 4)
+                        *reinterpret_cast<f32x4 *>(dst + j) = f32x4{sum[j], sum[j + 1], sum[j + 2], sum[j + 3]};
+                    if (d0 == 0) {
+                        float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP + (at * kRows + out_row) * 2;
+                        ml[0] = mx;
+                        ml[1] = lsum;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        p.rest += take;
+        left -= take;
     }
-    for (int i = 0; i < 2; ++i) {
-        const int d = lane + i * kWave;
-        if (d < a.dim)
-            a.out[t * a.out_token + h * a.out_head + d] = narrow<kHalf>(sum > 0.f ? acc[i] / sum : 0.f);
+}
+
+// ---------------------------------------------------------------------- join ---
+
+// Partial sums of the tiles that a cut goes through.  blockIdx.x is the cut after
+// block x, and works on the tile it is the first cut of; blockIdx.y takes kJoin rows of it.
+// Eight threads' groups take the pieces in turn, then their sums meet in LDS.
+constexpr int kJoin = 4;
+
+template <int DP, int kRows, int kKeys, bool kHalf>
+__global__ void __launch_bounds__(kThreads) k_join(Attend a) {
+    constexpr int kLanes = DP / 4, kGroups = kThreads / kLanes;
+    __shared__ float part[kGroups][DP];
+    __shared__ float part_l[kGroups];
+    int64_t piece;
+    const int64_t cut = blockIdx.x + 1;
+    const Place p = find<kKeys>(a, cut, &piece);
+    if (p.row < 0) return;
+    const Row r = row_at(a, p.row);
+    const Tile t = tile_at<kKeys>(a, r, p.rest);
+    if (t.done == 0 || t.done > piece) return;  // between two tiles, or not the tile's first cut
+    const int64_t last = cut + (t.units - t.done - 1) / piece;  // the block with the tile's end
+    const float c = a.scale * kLog2e;
+    const float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP;
+    const int lane = threadIdx.x % kLanes, g = threadIdx.x / kLanes;
+    // the first piece begins the tile, the others go on with it
+    auto slot_of = [&](int64_t i) { return i < cut ? 2 * i + 1 : 2 * i; };
+    for (int row = blockIdx.y * kJoin; row < min((int)(blockIdx.y + 1) * kJoin, kRows); ++row) {
+        const int tok = row / t.heads, h = row - tok * t.heads;
+        if (tok >= t.n) break;
+        float mx = -INFINITY;
+        for (int64_t i = cut - 1 + threadIdx.x % kWave; i <= last; i += kWave) mx = fmaxf(mx, ml[(slot_of(i) * kRows + row) * 2]);
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+        f32x4 sum{0, 0, 0, 0};
+        float lsum = 0.f;
+#pragma unroll 4
+        for (int64_t i = cut - 1 + g; i <= last; i += kGroups) {
+            const int64_t at = slot_of(i) * kRows + row;
+            const float mi = ml[at * 2], li = ml[at * 2 + 1];
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(a.sums + at * DP + 4 * lane);
+            const float keep = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi - mx) * c);
+            sum += x * keep;
+            lsum += li * keep;
+        }
+        __syncthreads();
+        *reinterpret_cast<f32x4 *>(&part[g][4 * lane]) = sum;
+        if (lane == 0) part_l[g] = lsum;
+        __syncthreads();
+        if (threadIdx.x < kLanes) {
+            f32x4 x{0, 0, 0, 0};
+            float y = 0.f;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                x += *reinterpret_cast<const f32x4 *>(&part[i][4 * lane]);
+                y += part_l[i];
+            }
+            const float inv = y > 0.f ? 1.f / y : 0.f;
+            const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
+            if (4 * lane < a.dim)
+                *reinterpret_cast<u32x2 *>(a.out + token * a.out_token + head * a.out_head + 4 * lane) =
+                    u32x2{pack<kHalf>(x[0] * inv, x[1] * inv), pack<kHalf>(x[2] * inv, x[3] * inv)};
+            if (a.lse && lane == 0) a.lse[token * a.heads + head] = y > 0.f ? mx * a.scale + logf(y) : -INFINITY;
+        }
     }
-    if (lane == 0 && a.lse) a.lse[t * a.heads + h] = sum > 0.f ? top + __logf(sum) : -INFINITY;
+}
+
+// -------------------------------------------------------------------- launch ---
+
+struct Shape {
+    int blocks, row_waves;  // of k_attend_narrow
+    int grid;
+    int rows() const { return 16 * blocks * row_waves; }
+};
+
+Shape shape_of(const tam_chunk &c, int64_t heads) {
+    const int64_t longest = c.longest ? std::min(c.longest, c.tokens) : c.tokens;
+    const int64_t rows = longest * (heads / c.kv_heads);
+    if (rows <= 16) return Shape{1, 1, 512};
+    if (rows <= 32) return Shape{2, 1, 256};
+    if (rows <= 64) return Shape{2, 2, 256};
+    return Shape{2, 4, 256};
+}
+
+int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
+
+template <int DP, int kBlocks, int kRowWaves, bool kHalf>
+hipError_t launch_narrow(const Attend &a, hipStream_t s) {
+    constexpr int kRows = 16 * kBlocks * kRowWaves, kKeys = 32 * (4 / kRowWaves);
+    hipLaunchKernelGGL((k_attend_narrow<DP, kBlocks, kRowWaves, kHalf>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_join<DP, kRows, kKeys, kHalf>), dim3((unsigned)a.blocks - 1, (unsigned)(kRows / kJoin)),
+                       dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+template <int DP, bool kHalf>
+hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
+    if (sh.rows() == 16) return launch_narrow<DP, 1, 1, kHalf>(a, s);
+    if (sh.rows() == 32) return launch_narrow<DP, 2, 1, kHalf>(a, s);
+    if (sh.rows() == 64) return launch_narrow<DP, 2, 2, kHalf>(a, s);
+    return launch_narrow<DP, 2, 4, kHalf>(a, s);
 }
 
 }  // namespace
 
-int64_t attend_work_bytes(const tam_chunk &, int64_t) { return 0; }
+int64_t attend_work_bytes(const tam_chunk &c, int64_t heads) {
+    const Shape sh = shape_of(c, heads);
+    return 2 * (int64_t)sh.grid * sh.rows() * (padded(c.head_dim) + 2) * 4;
+}
 
-hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *, hipStream_t s) {
-    const Attend a{static_cast<const uint16_t *>(c.k), static_cast<const uint16_t *>(c.v),
-                   static_cast<const uint16_t *>(q.q), static_cast<uint16_t *>(q.out), q.lse, c.page_stride,
-                   c.head_stride, c.token_stride, q.q_token, q.q_head, q.out_token, q.out_head, c.table, c.length,
-                   c.offsets, c.slot_ids, c.table_stride, c.slots, c.max_pages, c.rows, c.tokens, (int32_t)c.num_pages,
-                   __builtin_ctzll((unsigned long long)c.page_tokens), (int32_t)q.heads, (int32_t)c.kv_heads,
-                   (int32_t)c.head_dim, q.scale};
-    const dim3 grid((unsigned)c.tokens, (unsigned)q.heads);
-    if (c.dtype == TAM_DTYPE_FP16)
-        hipLaunchKernelGGL((k_attend_rows<true>), grid, dim3(kWave), 0, s, a);
-    else
-        hipLaunchKernelGGL((k_attend_rows<false>), grid, dim3(kWave), 0, s, a);
-    return hipGetLastError();
+hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipStream_t s) {
+    const Shape sh = shape_of(c, q.heads);
+    const int64_t group = q.heads / c.kv_heads;
+    Attend a{static_cast<const uint16_t *>(c.k), static_cast<const uint16_t *>(c.v),
+             static_cast<const uint16_t *>(q.q), static_cast<uint16_t *>(q.out), q.lse, c.page_stride,
+             c.head_stride, c.token_stride, q.q_token, q.q_head, q.out_token, q.out_head, c.table, c.length,
+             c.offsets, c.slot_ids, c.table_stride, c.slots, c.max_pages, c.rows, c.tokens, (int32_t)c.num_pages,
+             __builtin_ctzll((unsigned long long)c.page_tokens), (int32_t)q.heads, (int32_t)c.kv_heads,
+             (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, nullptr};
+    a.group = (int32_t)std::min<int64_t>(group, sh.rows());
+    a.parts = (int32_t)((group + a.group - 1) / a.group);
+    a.tq = sh.rows() / a.group;
+    a.blocks = sh.grid;
+    a.least = 1;
+    a.sums = static_cast<float *>(work);
+    const bool half = c.dtype == TAM_DTYPE_FP16;
+    if (padded(c.head_dim) == 64) return half ? launch<64, true>(a, sh, s) : launch<64, false>(a, sh, s);
+    return half ? launch<128, true>(a, sh, s) : launch<128, false>(a, sh, s);
 }
 
 }  // namespace tam
