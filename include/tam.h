@@ -548,7 +548,7 @@ typedef struct {
     int64_t page_tokens;   /* a power of two, 1 .. 65536 */
     int32_t *table;        /* device [slots][table_stride] */
     int64_t slots;
-    int64_t max_pages;     /* pages that a slot can hold: columns of the table */
+    int64_t max_pages;     /* pages that a slot can hold: columns of the table; max_pages * page_tokens <= 2^30 */
     int64_t table_stride;  /* elements between rows, >= max_pages */
     int32_t *length;       /* device [slots] */
     int32_t *refs;         /* device [num_pages] */

@@ -28,6 +28,8 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int16_t i16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -204,6 +206,14 @@ __device__ inline f32x4 mfma16(u32x4 x, u32x4 y, f32x4 z) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), z, 0, 0, 0);
     else
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), z, 0, 0, 0);
+}
+
+template <bool kHalf>
+__device__ inline f32x16 mfma32(u32x4 x, u32x4 y, f32x16 z) {
+    if constexpr (kHalf)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), z, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), z, 0, 0, 0);
 }
 
 template <bool kHalf>
@@ -480,6 +490,301 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
     }
 }
 
+// -------------------------------------------------------------------- wide ---
+
+// A tile of 256 rows, 64 to a wave, by 64 keys a unit: the matrix products bound it.
+// K and V come into LDS straight from memory, two units of each, the next one's while
+// this one is computed; their 16-byte pieces lie in an order that leaves no bank asked
+// twice, laid out by which piece a lane loads.  As above S^T = K Q^T, O^T = V^T P^T (V
+// read from LDS by columns), so the weights stay in their lanes.  A wave has
+// its matrix unit to itself; so that it never waits for the softmax, a half unit (32
+// keys) is in three stages at once: the products of the next half's scores and of the last
+// half's weights with V run beside this half's exponentials.
+constexpr int kWideKeys = 64, kWideRows = 256;
+
+template <int DP, bool kHalf>
+__global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
+    constexpr int kPieces = DP / 8;            // 16-byte pieces of a key
+    constexpr int kSteps = DP / 16;            // products over 16 dimensions
+    constexpr int kCols = DP / 32;             // blocks of 32 output dimensions
+    constexpr int kLoads = kPieces * kWideKeys / kThreads;
+    __shared__ __align__(16) uint16_t kbuf[2][kWideKeys * DP], vbuf[2][kWideKeys * DP];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int col = lane % 32, half = lane / 32;
+    // blocks go to the eight dies in turn: neighbouring pieces, which share K and V, to one die
+    const int64_t block = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    int64_t piece;
+    Place p = find<kWideKeys>(a, block, &piece);
+    if (p.row < 0) return;
+    int64_t left = min(piece, p.total - block * piece);
+    const float c = a.scale * kLog2e;
+    const int32_t place = (1 << a.shift) - 1;
+
+    // where piece x of key k lies in its row of LDS
+    auto k_at = [](int key, int x) { return x ^ (kPieces == 16 ? key & 15 : (key >> 1) & 7); };
+    auto v_at = [](int key, int x) { return x ^ (kPieces == 16 ? 2 * (key & 7) : 2 * ((key >> 1) & 3)); };
+    // this lane's reads: K rows as the first factor; V by columns: four keys of one dimension
+    int k_read[kSteps], v_read[kCols];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) k_read[s] = col * DP + 8 * k_at(col, 2 * s + half);
+    const int vk = 4 * half + (lane % 16) / 4;  // key of the lane's 8 bytes (+ 8, 16, 24)
+#pragma unroll
+    for (int d = 0; d < kCols; ++d) {
+        const int dim = 32 * d + 16 * (lane / 16 % 2) + 4 * (lane % 4);
+        v_read[d] = vk * DP + 8 * v_at(vk, dim / 8) + dim % 8;
+    }
+
+    while (left > 0) {
+        const Row r = row_at(a, p.row);
+        const int64_t in_row = row_units<kWideKeys>(a, r) * a.kv_heads * a.parts;
+        if (p.rest >= in_row) {
+            ++p.row;
+            p.rest = 0;
+            continue;
+        }
+        const Tile t = tile_at<kWideKeys>(a, r, p.rest);
+        const int64_t take = min(t.units - t.done, left);
+        const int32_t all = max(0, r.base + r.n);
+        const int32_t most = max(0, min(r.base + t.first + t.n, all));
+        u32x4 q[2][kSteps];
+        int32_t seen[2];
+        int32_t least = INT_MAX;  // keys that every query of the wave's sees
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int row = 64 * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
+            const bool is = tok < t.n;
+            seen[b] = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
+            const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
+                                  (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const int d = 16 * s + 8 * half;
+                q[b][s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(src + d) : u32x4{0, 0, 0, 0};
+            }
+        }
+        {
+            const int tok = 64 * wave / t.heads;
+            least = tok < t.n && (64 * wave + 63) / t.heads < t.n ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
+        }
+        f32x16 o[2][kCols], sa[2], sb[2];
+        u32x4 pa[2][2], pb[2][2];
+        float m[2], l[2] = {0.f, 0.f}, top[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int d = 0; d < kCols; ++d) o[b][d] = f32x16{};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pa[b][i] = u32x4{0, 0, 0, 0};
+        }
+        const uint16_t *kh = a.k + (int64_t)t.head * a.head_stride, *vh = a.v + (int64_t)t.head * a.head_stride;
+        const int32_t *pages = a.table + r.slot * a.table_stride;
+
+        // A unit's keys, one per lane: where its vectors lie (-1: in no page).  Keys past the last
+        // one that the tile sees stand for it.
+        auto place_of = [&](int64_t unit) -> int64_t {
+            const int32_t key = min((int32_t)(unit * kWideKeys) + lane, most - 1), page = pages[key >> a.shift];
+            return (uint32_t)page < (uint32_t)a.pages
+                       ? (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride : -1;
+        };
+        auto load = [&](bool is_k, uint16_t *to, int64_t where) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int at = i * kThreads + threadIdx.x, key = at / kPieces, x = at % kPieces;
+                const int64_t off = __shfl(where, key);
+                const int d = 8 * (is_k ? k_at(key, x) : v_at(key, x));
+                const uint16_t *src = (is_k ? kh : vh) + max(off, (int64_t)0) + (d < a.dim ? d : 0);
+                if (!is_k && off < 0) src = reinterpret_cast<const uint16_t *>(kZeros);
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void *)src,
+                    (__attribute__((address_space(3))) void *)(to + (i * kThreads + wave * kWave) * 8), 16, 0, 0);
+            }
+        };
+        auto read_k = [&](const uint16_t *from, int s) { return *reinterpret_cast<const u32x4 *>(from + k_read[s]); };
+        auto read_v = [&](const uint16_t *from, int d, int i) -> u32x4 {  // keys 16 i + 4 half + (0..3, 8..11)
+            typedef __attribute__((address_space(3))) i16x4 lds;
+            const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + v_read[d] + 16 * i * DP));
+            // eight keys on: the same place of the swizzle (16 pieces), or of its other half (8)
+            const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + v_read[d] + (16 * i + 8) * DP));
+            const u32x2 u = __builtin_bit_cast(u32x2, x), w = __builtin_bit_cast(u32x2, y);
+            return u32x4{u[0], u[1], w[0], w[1]};
+        };
+        auto highest = [&](const f32x16 &s) {
+            float x = fmaxf(s[0], s[1]);
+#pragma unroll
+            for (int i = 2; i < 16; ++i) x = fmaxf(x, s[i]);
+            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+            return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+        };
+        auto scores = [&](const uint16_t *from, f32x16 (&s)[2]) {
+            s[0] = s[1] = f32x16{};
+#pragma unroll
+            for (int d = 0; d < kSteps; ++d) {
+                const u32x4 k = read_k(from, d);
+                s[0] = mfma32<kHalf>(k, q[0][d], s[0]);
+                s[1] = mfma32<kHalf>(k, q[1][d], s[1]);
+            }
+        };
+        auto gather = [&](const uint16_t *from, const u32x4 (&w)[2][2]) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < kCols; ++d) {
+                    const u32x4 v = read_v(from, d, i);
+                    o[0][d] = mfma32<kHalf>(v, w[0][i], o[0][d]);
+                    o[1][d] = mfma32<kHalf>(v, w[1][i], o[1][d]);
+                }
+        };
+        // scores of the half unit at key k0: those not seen are -inf, the highest of each query
+        auto settle = [&](int32_t k0, uint32_t ok, f32x16 (&s)[2]) {
+            if (k0 + 32 > least || ~ok) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int32_t rest = seen[b] - k0 - 4 * half;
+                    const uint32_t have = ok >> 4 * half;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = 8 * (i / 4) + i % 4;
+                        if (key >= rest || !(have >> key & 1)) s[b][i] = -INFINITY;
+                    }
+                    top[b] = highest(s[b]);
+                }
+            }
+        };
+        // m follows when it lags too far; the weights w, which are under the old one, go to O first
+        auto follow = [&](const uint16_t *v, u32x4 (&w)[2][2]) {
+            if (__any((top[0] - m[0]) * c > kLag || (top[1] - m[1]) * c > kLag)) {
+                gather(v, w);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const float now = fmaxf(m[b], top[b]);
+                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
+                    m[b] = now;
+                    l[b] *= keep;
+#pragma unroll
+                    for (int d = 0; d < kCols; ++d) o[b][d] *= keep;
+                    w[b][0] = w[b][1] = u32x4{0, 0, 0, 0};
+                }
+            }
+        };
+        // one half unit: its weights from s into w, the next scores into s1, the last weights w0 into O
+        auto stage = [&](const f32x16 (&s)[2], u32x4 (&w)[2][2], const uint16_t *k, f32x16 (&s1)[2], const uint16_t *v,
+                         const u32x4 (&w0)[2][2]) {
+            const float mc[2] = {m[0] == -INFINITY ? 0.f : m[0] * c, m[1] == -INFINITY ? 0.f : m[1] * c};
+            scores(k, s1);
+            gather(v, w0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * i + j], c, -mc[b]));
+                        l[b] += x[j];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[b][i][j] = pack<kHalf>(x[2 * j], x[2 * j + 1]);
+                }
+            top[0] = highest(s1[0]);
+            top[1] = highest(s1[1]);
+#pragma unroll
+            for (int i = 0; i < 4 * kSteps; ++i) {  // one product, then as much else as runs beside it
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            }
+        };
+
+        const int64_t u0 = t.done, u1 = u0 + take;
+        if (u0 * kWideKeys < most) {
+            int64_t where = place_of(u0);
+            uint64_t ok = __ballot(where >= 0), ok1 = ~0ull;  // keys of this unit, of the next one, in a page
+            load(true, kbuf[0], where);
+            load(false, vbuf[0], where);
+            int64_t v_where = 0;  // the next unit's
+            if (u0 + 1 < u1) {
+                v_where = place_of(u0 + 1);
+                ok1 = __ballot(v_where >= 0);
+                load(true, kbuf[1], v_where);
+            }
+            int64_t k_where = u0 + 2 < u1 ? place_of(u0 + 2) : 0;  // the one's after it
+            __syncthreads();
+            scores(kbuf[0], sa);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) top[b] = highest(sa[b]);
+            settle((int32_t)(u0 * kWideKeys), (uint32_t)ok, sa);
+            m[0] = top[0];
+            m[1] = top[1];
+            for (int64_t u = u0; u < u1; ++u) {
+                const int x = (int)(u - u0) & 1;
+                const int32_t key = (int32_t)(u * kWideKeys);
+                stage(sa, pb, kbuf[x] + 32 * DP, sb, u > u0 ? vbuf[x ^ 1] + 32 * DP : vbuf[0], pa);
+                settle(key + 32, (uint32_t)(ok >> 32), sb);
+                __syncthreads();  // the next unit's K and this one's V are there, the buffers behind them free
+                if (u + 2 < u1) load(true, kbuf[x], k_where);
+                if (u + 1 < u1) load(false, vbuf[x ^ 1], v_where);
+                v_where = k_where;
+                ok = ok1;
+                ok1 = __ballot(k_where >= 0);
+                if (u + 3 < u1) k_where = place_of(u + 3);
+                follow(vbuf[x], pb);
+                stage(sb, pa, kbuf[x ^ 1], sa, vbuf[x], pb);
+                if (u + 1 < u1) {
+                    settle(key + 64, (uint32_t)ok, sa);
+                    follow(vbuf[x] + 32 * DP, pa);
+                }
+            }
+            gather(vbuf[(u1 - 1 - u0) & 1] + 32 * DP, pa);
+            __syncthreads();  // the next tile's loads go to the same buffers
+        } else {
+            m[0] = m[1] = -INFINITY;
+        }
+        // o[b][d][i] is dimension 32 d + 8 (i / 4) + 4 half + i % 4 of query `col`
+        const bool whole = take == t.units;
+        const int64_t at = 2 * block + (t.done == 0);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[b]), __float_as_uint(l[b]), false, false);
+            const float sum = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+            const int row = 64 * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
+            if (tok >= t.n) continue;
+            if (whole) {
+                const float inv = sum > 0.f ? 1.f / sum : 0.f;
+                const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
+                uint16_t *dst = a.out + token * a.out_token + head * a.out_head;
+#pragma unroll
+                for (int d = 0; d < kCols; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const int dim = 32 * d + 2 * i + 4 * half;
+                        if (dim < a.dim)
+                            *reinterpret_cast<u32x2 *>(dst + dim) =
+                                u32x2{pack<kHalf>(o[b][d][i] * inv, o[b][d][i + 1] * inv),
+                                      pack<kHalf>(o[b][d][i + 2] * inv, o[b][d][i + 3] * inv)};
+                    }
+                if (a.lse && half == 0)
+                    a.lse[token * a.heads + head] = sum > 0.f ? m[b] * a.scale + logf(sum) : -INFINITY;
+            } else {
+                float *dst = a.sums + (at * kWideRows + row) * DP;
+#pragma unroll
+                for (int d = 0; d < kCols; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<f32x4 *>(dst + 32 * d + 2 * i + 4 * half) =
+                            f32x4{o[b][d][i], o[b][d][i + 1], o[b][d][i + 2], o[b][d][i + 3]};
+                if (half == 0) {
+                    float *ml = a.sums + 2 * (int64_t)a.blocks * kWideRows * DP + (at * kWideRows + row) * 2;
+                    ml[0] = m[b];
+                    ml[1] = sum;
+                }
+            }
+        }
+        p.rest += take;
+        left -= take;
+    }
+}
+
 // ---------------------------------------------------------------------- join ---
 
 // Partial sums of the tiles that a cut goes through.  blockIdx.x is the cut after
@@ -548,7 +853,7 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
 // -------------------------------------------------------------------- launch ---
 
 struct Shape {
-    int blocks, row_waves;  // of k_attend_narrow
+    int blocks, row_waves;  // of k_attend_narrow; 256 rows are k_attend_wide's
     int grid;
     int rows() const { return 16 * blocks * row_waves; }
 };
@@ -559,7 +864,8 @@ Shape shape_of(const tam_chunk &c, int64_t heads) {
     if (rows <= 16) return Shape{1, 1, 512};
     if (rows <= 32) return Shape{2, 1, 256};
     if (rows <= 64) return Shape{2, 2, 256};
-    return Shape{2, 4, 256};
+    if (rows <= 128) return Shape{2, 4, 256};
+    return Shape{4, 4, 256};
 }
 
 int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
@@ -580,7 +886,13 @@ hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
     if (sh.rows() == 16) return launch_narrow<DP, 1, 1, kHalf>(a, s);
     if (sh.rows() == 32) return launch_narrow<DP, 2, 1, kHalf>(a, s);
     if (sh.rows() == 64) return launch_narrow<DP, 2, 2, kHalf>(a, s);
-    return launch_narrow<DP, 2, 4, kHalf>(a, s);
+    if (sh.rows() == 128) return launch_narrow<DP, 2, 4, kHalf>(a, s);
+    hipLaunchKernelGGL((k_attend_wide<DP, kHalf>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_join<DP, kWideRows, kWideKeys, kHalf>), dim3((unsigned)a.blocks - 1, kWideRows / kJoin),
+                       dim3(kThreads), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace

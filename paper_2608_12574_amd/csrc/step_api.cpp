@@ -26,8 +26,8 @@ const char *tables_wrong(const void *table, const void *length, int64_t slots, i
     if (slots < 0 || slots >= INT32_MAX) return "slots must be in 0 .. 2^31 - 2";
     if (pages < 1 || pages >= INT32_MAX) return "num_pages must be in 1 .. 2^31 - 2";
     if (!power_of_two(page_tokens) || page_tokens > 65536) return "page_tokens must be a power of two, at most 65536";
-    if (max_pages < 0 || max_pages > (INT32_MAX - 1) / page_tokens)
-        return "max_pages must be >= 0, and max_pages * page_tokens < 2^31";
+    if (max_pages < 0 || max_pages > (1 << 30) / page_tokens)
+        return "max_pages must be >= 0, and max_pages * page_tokens at most 2^30";
     if (stride < max_pages) return "table_stride must be >= max_pages";
     if (slots > 0 && (!length || (max_pages > 0 && !table))) return "null table or length";
     if (!aligned(table, 4) || !aligned(length, 4)) return "table and length must be 4-byte aligned";
