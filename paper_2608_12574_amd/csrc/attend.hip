@@ -122,12 +122,12 @@ struct Place {
 
 // The place of unit number `share * piece` (share: this block's number), and the units of a
 // piece.  All threads of the block call it; row < 0 past the line's end.
-template <int kKeys>
+template <int kKeys, int kN = kThreads>
 __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
-    __shared__ int64_t sums[kThreads / kWave];
+    __shared__ int64_t sums[kN / kWave];
     __shared__ int64_t found[2];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t per = (a.rows + kThreads - 1) / kThreads, lo = threadIdx.x * per, hi = min(lo + per, a.rows);
+    const int64_t per = (a.rows + kN - 1) / kN, lo = threadIdx.x * per, hi = min(lo + per, a.rows);
     const int64_t heads = (int64_t)a.kv_heads * a.parts;
     int64_t mine = 0;
     for (int64_t i = lo; i < hi; ++i) mine += heads * row_units<kKeys>(a, row_at(a, i));
@@ -143,7 +143,7 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
     Place p;
     p.total = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / kWave; ++w) {
+    for (int w = 0; w < kN / kWave; ++w) {
         if (w < wave) upto += sums[w];
         p.total += sums[w];
     }
@@ -492,29 +492,27 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
 
 // -------------------------------------------------------------------- wide ---
 
-// A tile of 256 rows, 64 to a wave, by 64 keys a unit: the matrix products bound it.
-// K and V come into LDS straight from memory, two units of each, the next one's while
-// this one is computed; their 16-byte pieces lie in an order that leaves no bank asked
-// twice, laid out by which piece a lane loads.  As above S^T = K Q^T, O^T = V^T P^T (V
-// read from LDS by columns), so the weights stay in their lanes.  A wave has
-// its matrix unit to itself; so that it never waits for the softmax, a half unit (32
-// keys) is in three stages at once: the products of the next half's scores and of the last
-// half's weights with V run beside this half's exponentials.
-constexpr int kWideKeys = 64, kWideRows = 256;
+// A tile of 256 rows, 32 to a wave, by 64 keys a unit: the matrix products bound it.
+// K and V go through LDS, two units of each: the next one's bytes are on their way in
+// registers while this one is computed.  Their 16-byte pieces lie in an order that leaves
+// no bank asked twice.  As above S^T = K Q^T, O^T = V^T P^T (V read from LDS by columns),
+// so the weights stay in their lanes.  Two waves share a matrix unit: one's products run
+// beside the other's exponentials.
+constexpr int kWideKeys = 64, kWideRows = 256, kWideThreads = 512;
 
 template <int DP, bool kHalf>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
+__global__ void __launch_bounds__(kWideThreads, 2) k_attend_wide(Attend a) {
     constexpr int kPieces = DP / 8;            // 16-byte pieces of a key
     constexpr int kSteps = DP / 16;            // products over 16 dimensions
     constexpr int kCols = DP / 32;             // blocks of 32 output dimensions
-    constexpr int kLoads = kPieces * kWideKeys / kThreads;
+    constexpr int kLoads = kPieces * kWideKeys / kWideThreads;
     __shared__ __align__(16) uint16_t kbuf[2][kWideKeys * DP], vbuf[2][kWideKeys * DP];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int col = lane % 32, half = lane / 32;
     // blocks go to the eight dies in turn: neighbouring pieces, which share K and V, to one die
     const int64_t block = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     int64_t piece;
-    Place p = find<kWideKeys>(a, block, &piece);
+    Place p = find<kWideKeys, kWideThreads>(a, block, &piece);
     if (p.row < 0) return;
     int64_t left = min(piece, p.total - block * piece);
     const float c = a.scale * kLog2e;
@@ -524,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
     auto k_at = [](int key, int x) { return x ^ (kPieces == 16 ? key & 15 : (key >> 1) & 7); };
     auto v_at = [](int key, int x) { return x ^ (kPieces == 16 ? 2 * (key & 7) : 2 * ((key >> 1) & 3)); };
     // this lane's reads: K rows as the first factor; V by columns: four keys of one dimension
-    int k_read[kSteps], v_read[kCols];
+    uint32_t k_read[kSteps], v_read[kCols];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) k_read[s] = col * DP + 8 * k_at(col, 2 * s + half);
     const int vk = 4 * half + (lane % 16) / 4;  // key of the lane's 8 bytes (+ 8, 16, 24)
@@ -546,36 +544,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         const int64_t take = min(t.units - t.done, left);
         const int32_t all = max(0, r.base + r.n);
         const int32_t most = max(0, min(r.base + t.first + t.n, all));
-        u32x4 q[2][kSteps];
-        int32_t seen[2];
-        int32_t least = INT_MAX;  // keys that every query of the wave's sees
+        const int row = 32 * wave + col, tok = row / t.heads, h = row - tok * t.heads;
+        const bool is = tok < t.n;
+        const int32_t seen = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
+        // keys that every query of the wave's sees
+        const int32_t least = (32 * wave + 31) / t.heads < t.n
+                                  ? max(0, min(r.base + t.first + 32 * wave / t.heads + 1, all)) : 0;
+        const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
+        u32x4 q[kSteps];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int row = 64 * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
-            const bool is = tok < t.n;
-            seen[b] = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
-            const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
-                                  (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const int d = 16 * s + 8 * half;
-                q[b][s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(src + d) : u32x4{0, 0, 0, 0};
-            }
+        for (int s = 0; s < kSteps; ++s) {
+            const int d = 16 * s + 8 * half;
+            q[s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(a.q + token * a.q_token + head * a.q_head + d)
+                                   : u32x4{0, 0, 0, 0};
         }
-        {
-            const int tok = 64 * wave / t.heads;
-            least = tok < t.n && (64 * wave + 63) / t.heads < t.n ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
-        }
-        f32x16 o[2][kCols], sa[2], sb[2];
-        u32x4 pa[2][2], pb[2][2];
-        float m[2], l[2] = {0.f, 0.f}, top[2];
+        f32x16 o[kCols];
+        float m = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-#pragma unroll
-            for (int d = 0; d < kCols; ++d) o[b][d] = f32x16{};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) pa[b][i] = u32x4{0, 0, 0, 0};
-        }
+        for (int d = 0; d < kCols; ++d) o[d] = f32x16{};
         const uint16_t *kh = a.k + (int64_t)t.head * a.head_stride, *vh = a.v + (int64_t)t.head * a.head_stride;
         const int32_t *pages = a.table + r.slot * a.table_stride;
 
@@ -586,198 +572,124 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
             return (uint32_t)page < (uint32_t)a.pages
                        ? (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride : -1;
         };
-        auto load = [&](bool is_k, uint16_t *to, int64_t where) {
+        u32x4 k_in[kLoads], v_in[kLoads];
+        auto load = [&](int64_t where) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int at = i * kThreads + threadIdx.x, key = at / kPieces, x = at % kPieces;
-                const int64_t off = __shfl(where, key);
-                const int d = 8 * (is_k ? k_at(key, x) : v_at(key, x));
-                const uint16_t *src = (is_k ? kh : vh) + max(off, (int64_t)0) + (d < a.dim ? d : 0);
-                if (!is_k && off < 0) src = reinterpret_cast<const uint16_t *>(kZeros);
-                __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void *)src,
-                    (__attribute__((address_space(3))) void *)(to + (i * kThreads + wave * kWave) * 8), 16, 0, 0);
+                const int at = i * kWideThreads + threadIdx.x, key = at / kPieces, d = 8 * (at % kPieces);
+                const int64_t off = __shfl(where, key), to = max(off, (int64_t)0) + (d < a.dim ? d : 0);
+                k_in[i] = *reinterpret_cast<const u32x4 *>(kh + to);
+                v_in[i] = *reinterpret_cast<const u32x4 *>(off < 0 ? reinterpret_cast<const uint16_t *>(kZeros) : vh + to);
             }
         };
-        auto read_k = [&](const uint16_t *from, int s) { return *reinterpret_cast<const u32x4 *>(from + k_read[s]); };
+        auto store = [&](uint16_t *k, uint16_t *v) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int at = i * kWideThreads + threadIdx.x, key = at / kPieces, x = at % kPieces;
+                *reinterpret_cast<u32x4 *>(k + key * DP + 8 * k_at(key, x)) = k_in[i];
+                *reinterpret_cast<u32x4 *>(v + key * DP + 8 * v_at(key, x)) = v_in[i];
+            }
+        };
         auto read_v = [&](const uint16_t *from, int d, int i) -> u32x4 {  // keys 16 i + 4 half + (0..3, 8..11)
             typedef __attribute__((address_space(3))) i16x4 lds;
             const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + v_read[d] + 16 * i * DP));
-            // eight keys on: the same place of the swizzle (16 pieces), or of its other half (8)
             const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + v_read[d] + (16 * i + 8) * DP));
             const u32x2 u = __builtin_bit_cast(u32x2, x), w = __builtin_bit_cast(u32x2, y);
             return u32x4{u[0], u[1], w[0], w[1]};
-        };
-        auto highest = [&](const f32x16 &s) {
-            float x = fmaxf(s[0], s[1]);
-#pragma unroll
-            for (int i = 2; i < 16; ++i) x = fmaxf(x, s[i]);
-            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-            return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
-        };
-        auto scores = [&](const uint16_t *from, f32x16 (&s)[2]) {
-            s[0] = s[1] = f32x16{};
-#pragma unroll
-            for (int d = 0; d < kSteps; ++d) {
-                const u32x4 k = read_k(from, d);
-                s[0] = mfma32<kHalf>(k, q[0][d], s[0]);
-                s[1] = mfma32<kHalf>(k, q[1][d], s[1]);
-            }
-        };
-        auto gather = [&](const uint16_t *from, const u32x4 (&w)[2][2]) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int d = 0; d < kCols; ++d) {
-                    const u32x4 v = read_v(from, d, i);
-                    o[0][d] = mfma32<kHalf>(v, w[0][i], o[0][d]);
-                    o[1][d] = mfma32<kHalf>(v, w[1][i], o[1][d]);
-                }
-        };
-        // scores of the half unit at key k0: those not seen are -inf, the highest of each query
-        auto settle = [&](int32_t k0, uint32_t ok, f32x16 (&s)[2]) {
-            if (k0 + 32 > least || ~ok) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int32_t rest = seen[b] - k0 - 4 * half;
-                    const uint32_t have = ok >> 4 * half;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int key = 8 * (i / 4) + i % 4;
-                        if (key >= rest || !(have >> key & 1)) s[b][i] = -INFINITY;
-                    }
-                    top[b] = highest(s[b]);
-                }
-            }
-        };
-        // m follows when it lags too far; the weights w, which are under the old one, go to O first
-        auto follow = [&](const uint16_t *v, u32x4 (&w)[2][2]) {
-            if (__any((top[0] - m[0]) * c > kLag || (top[1] - m[1]) * c > kLag)) {
-                gather(v, w);
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const float now = fmaxf(m[b], top[b]);
-                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
-                    m[b] = now;
-                    l[b] *= keep;
-#pragma unroll
-                    for (int d = 0; d < kCols; ++d) o[b][d] *= keep;
-                    w[b][0] = w[b][1] = u32x4{0, 0, 0, 0};
-                }
-            }
-        };
-        // one half unit: its weights from s into w, the next scores into s1, the last weights w0 into O
-        auto stage = [&](const f32x16 (&s)[2], u32x4 (&w)[2][2], const uint16_t *k, f32x16 (&s1)[2], const uint16_t *v,
-                         const u32x4 (&w0)[2][2]) {
-            const float mc[2] = {m[0] == -INFINITY ? 0.f : m[0] * c, m[1] == -INFINITY ? 0.f : m[1] * c};
-            scores(k, s1);
-            gather(v, w0);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    float x[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * i + j], c, -mc[b]));
-                        l[b] += x[j];
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) w[b][i][j] = pack<kHalf>(x[2 * j], x[2 * j + 1]);
-                }
-            top[0] = highest(s1[0]);
-            top[1] = highest(s1[1]);
-#pragma unroll
-            for (int i = 0; i < 4 * kSteps; ++i) {  // one product, then as much else as runs beside it
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
-            }
         };
 
         const int64_t u0 = t.done, u1 = u0 + take;
         if (u0 * kWideKeys < most) {
             int64_t where = place_of(u0);
-            uint64_t ok = __ballot(where >= 0), ok1 = ~0ull;  // keys of this unit, of the next one, in a page
-            load(true, kbuf[0], where);
-            load(false, vbuf[0], where);
-            int64_t v_where = 0;  // the next unit's
-            if (u0 + 1 < u1) {
-                v_where = place_of(u0 + 1);
-                ok1 = __ballot(v_where >= 0);
-                load(true, kbuf[1], v_where);
-            }
-            int64_t k_where = u0 + 2 < u1 ? place_of(u0 + 2) : 0;  // the one's after it
+            uint64_t ok = __ballot(where >= 0);  // the unit's keys that lie in a page
+            load(where);
+            if (u0 + 1 < u1) where = place_of(u0 + 1);
+            store(kbuf[0], vbuf[0]);
             __syncthreads();
-            scores(kbuf[0], sa);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) top[b] = highest(sa[b]);
-            settle((int32_t)(u0 * kWideKeys), (uint32_t)ok, sa);
-            m[0] = top[0];
-            m[1] = top[1];
             for (int64_t u = u0; u < u1; ++u) {
                 const int x = (int)(u - u0) & 1;
-                const int32_t key = (int32_t)(u * kWideKeys);
-                stage(sa, pb, kbuf[x] + 32 * DP, sb, u > u0 ? vbuf[x ^ 1] + 32 * DP : vbuf[0], pa);
-                settle(key + 32, (uint32_t)(ok >> 32), sb);
-                __syncthreads();  // the next unit's K and this one's V are there, the buffers behind them free
-                if (u + 2 < u1) load(true, kbuf[x], k_where);
-                if (u + 1 < u1) load(false, vbuf[x ^ 1], v_where);
-                v_where = k_where;
-                ok = ok1;
-                ok1 = __ballot(k_where >= 0);
-                if (u + 3 < u1) k_where = place_of(u + 3);
-                follow(vbuf[x], pb);
-                stage(sb, pa, kbuf[x ^ 1], sa, vbuf[x], pb);
-                if (u + 1 < u1) {
-                    settle(key + 64, (uint32_t)ok, sa);
-                    follow(vbuf[x] + 32 * DP, pa);
+                const int32_t key0 = (int32_t)(u * kWideKeys);
+                const uint64_t ok1 = __ballot(where >= 0);
+                if (u + 1 < u1) load(where);
+                if (u + 2 < u1) where = place_of(u + 2);
+                f32x16 s[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+                for (int d = 0; d < kSteps; ++d)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        s[i] = mfma32<kHalf>(*reinterpret_cast<const u32x4 *>(&kbuf[x][k_read[d] + 32 * i * DP]), q[d], s[i]);
+                if (key0 + kWideKeys > least || ~ok) {
+                    const int32_t rest = seen - key0 - 4 * half;
+                    const uint64_t have = ok >> 4 * half;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int key = 8 * (i / 4) + i % 4;
+                        if (key >= rest || !(have >> key & 1)) s[i / 16][i % 16] = -INFINITY;
+                    }
                 }
+                float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
+                const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+                top = fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1]));
+                if (__any((top - m) * c > kLag)) {
+                    const float now = fmaxf(m, top);
+                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - now) * c);
+                    m = now;
+                    l *= keep;
+#pragma unroll
+                    for (int d = 0; d < kCols; ++d) o[d] *= keep;
+                }
+                const float mc = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float w[8];
+                    u32x4 pw;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][8 * (i % 2) + j], c, -mc));
+                        l += w[j];
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) pw[j] = pack<kHalf>(w[2 * j], w[2 * j + 1]);
+#pragma unroll
+                    for (int d = 0; d < kCols; ++d) o[d] = mfma32<kHalf>(read_v(vbuf[x], d, i), pw, o[d]);
+                }
+                if (u + 1 < u1) store(kbuf[x ^ 1], vbuf[x ^ 1]);
+                ok = ok1;
+                __syncthreads();
             }
-            gather(vbuf[(u1 - 1 - u0) & 1] + 32 * DP, pa);
-            __syncthreads();  // the next tile's loads go to the same buffers
-        } else {
-            m[0] = m[1] = -INFINITY;
         }
-        // o[b][d][i] is dimension 32 d + 8 (i / 4) + 4 half + i % 4 of query `col`
+        // o[d][i] is dimension 32 d + 8 (i / 4) + 4 half + i % 4 of query `col`
         const bool whole = take == t.units;
         const int64_t at = 2 * block + (t.done == 0);
+        const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(other[0]) + __uint_as_float(other[1]);
+        if (is && whole) {
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            uint16_t *dst = a.out + token * a.out_token + head * a.out_head;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[b]), __float_as_uint(l[b]), false, false);
-            const float sum = __uint_as_float(y[0]) + __uint_as_float(y[1]);
-            const int row = 64 * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
-            if (tok >= t.n) continue;
-            if (whole) {
-                const float inv = sum > 0.f ? 1.f / sum : 0.f;
-                const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
-                uint16_t *dst = a.out + token * a.out_token + head * a.out_head;
+            for (int d = 0; d < kCols; ++d)
 #pragma unroll
-                for (int d = 0; d < kCols; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const int dim = 32 * d + 2 * i + 4 * half;
-                        if (dim < a.dim)
-                            *reinterpret_cast<u32x2 *>(dst + dim) =
-                                u32x2{pack<kHalf>(o[b][d][i] * inv, o[b][d][i + 1] * inv),
-                                      pack<kHalf>(o[b][d][i + 2] * inv, o[b][d][i + 3] * inv)};
-                    }
-                if (a.lse && half == 0)
-                    a.lse[token * a.heads + head] = sum > 0.f ? m[b] * a.scale + logf(sum) : -INFINITY;
-            } else {
-                float *dst = a.sums + (at * kWideRows + row) * DP;
-#pragma unroll
-                for (int d = 0; d < kCols; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        *reinterpret_cast<f32x4 *>(dst + 32 * d + 2 * i + 4 * half) =
-                            f32x4{o[b][d][i], o[b][d][i + 1], o[b][d][i + 2], o[b][d][i + 3]};
-                if (half == 0) {
-                    float *ml = a.sums + 2 * (int64_t)a.blocks * kWideRows * DP + (at * kWideRows + row) * 2;
-                    ml[0] = m[b];
-                    ml[1] = sum;
+                for (int i = 0; i < 16; i += 4) {
+                    const int dim = 32 * d + 2 * i + 4 * half;
+                    if (dim < a.dim)
+                        *reinterpret_cast<u32x2 *>(dst + dim) = u32x2{pack<kHalf>(o[d][i] * inv, o[d][i + 1] * inv),
+                                                                      pack<kHalf>(o[d][i + 2] * inv, o[d][i + 3] * inv)};
                 }
+            if (a.lse && half == 0) a.lse[token * a.heads + head] = l > 0.f ? m * a.scale + logf(l) : -INFINITY;
+        } else if (is) {
+            float *dst = a.sums + (at * kWideRows + row) * DP;
+#pragma unroll
+            for (int d = 0; d < kCols; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f32x4 *>(dst + 32 * d + 2 * i + 4 * half) =
+                        f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+            if (half == 0) {
+                float *ml = a.sums + 2 * (int64_t)a.blocks * kWideRows * DP + (at * kWideRows + row) * 2;
+                ml[0] = m;
+                ml[1] = l;
             }
         }
         p.rest += take;
@@ -887,7 +799,7 @@ hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
     if (sh.rows() == 32) return launch_narrow<DP, 2, 1, kHalf>(a, s);
     if (sh.rows() == 64) return launch_narrow<DP, 2, 2, kHalf>(a, s);
     if (sh.rows() == 128) return launch_narrow<DP, 2, 4, kHalf>(a, s);
-    hipLaunchKernelGGL((k_attend_wide<DP, kHalf>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_attend_wide<DP, kHalf>), dim3((unsigned)a.blocks), dim3(kWideThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((k_join<DP, kWideRows, kWideKeys, kHalf>), dim3((unsigned)a.blocks - 1, kWideRows / kJoin),
