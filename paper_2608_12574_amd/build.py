@@ -33,6 +33,10 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-pthread", "-Wall", "-Wno-unused-result
 # The packed-FP32 VALU forms are switched off for every GPU compile.
 GPU = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
+# attend.hip: matrix results in ordinary registers where there is room, since the softmax's
+# instructions cannot read the accumulation registers (8 copies per half unit instead of 100).
+FILE_FLAGS = {"attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cpp", ".hip")))
@@ -46,7 +50,7 @@ SANITIZE_DIR = os.path.join(BUILD, "sanitize")
 
 def _compile(src: str, out_dir: str, extra: list) -> str:
     obj = os.path.join(out_dir, os.path.basename(src) + ".o")
-    cmd = [HIPCC, *COMMON, *extra, *GPU, "-c", src, "-o", obj]
+    cmd = [HIPCC, *COMMON, *extra, *GPU, *FILE_FLAGS.get(os.path.basename(src), []), "-c", src, "-o", obj]
     subprocess.run(cmd, check=True, capture_output=True, text=True)
     return obj
 

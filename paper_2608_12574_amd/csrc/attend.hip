@@ -36,8 +36,13 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kWave = 64;
 constexpr int kThreads = 256;
 
-// Bad page numbers point here: K and V of zeros.
-__device__ const u32x4 kZeros[16] = {};
+// Bad page numbers point here: V of zeros.  (Addresses of memory are told from those of LDS
+// here, so that a load does not wait as if it could be of either.)
+__device__ u32x4 kZeros[16];
+typedef __attribute__((address_space(1))) const uint16_t global_u16;
+typedef __attribute__((address_space(1))) const u32x4 global_u32x4;
+typedef __attribute__((address_space(1))) const u32x2 global_u32x2;
+__device__ inline global_u16 *zeros() { return (global_u16 *)kZeros; }
 
 struct Attend {
     const uint16_t *k, *v, *q;
@@ -53,6 +58,12 @@ struct Attend {
     int32_t least;  // units of a block, at least
     float *sums;    // [2 blocks][tile rows][DP] partial sums, then [2 blocks][tile rows][2] their m and sum of weights
 };
+
+// a value that is the same in all lanes, to the compiler too
+__device__ inline int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+    return (int64_t)(uint32_t)uniform((int32_t)x) | (int64_t)uniform((int32_t)(x >> 32)) << 32;
+}
 
 // ------------------------------------------------------------------ the cut ---
 
@@ -98,6 +109,16 @@ __device__ inline Row row_at(const Attend &a, int64_t i) {
     int64_t len = 0;
     if (r.slot >= 0 && r.slot < a.slots) len = min(max((int64_t)a.length[r.slot], (int64_t)0), a.max_pages << a.shift);
     r.base = (int32_t)(len - r.n);
+    return r;
+}
+
+// the same for a row number that all lanes share
+__device__ inline Row shared_row(const Attend &a, int64_t i) {
+    Row r = row_at(a, i);
+    r.n = uniform(r.n);
+    r.base = uniform(r.base);
+    r.first = uniform(r.first);
+    r.slot = uniform(r.slot);
     return r;
 }
 
@@ -147,6 +168,7 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
         if (w < wave) upto += sums[w];
         p.total += sums[w];
     }
+    p.total = uniform(p.total);
     *piece = max((int64_t)a.least, (p.total + a.blocks - 1) / a.blocks);
     const int64_t at = share * *piece;
     if (at >= upto - mine && at < upto) {  // one thread: walk its rows
@@ -161,8 +183,8 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
         found[1] = rest;
     }
     __syncthreads();
-    p.row = found[0];
-    p.rest = found[1];
+    p.row = uniform(found[0]);
+    p.rest = uniform(found[1]);
     return p;
 }
 
@@ -245,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
     constexpr int kRows = 16 * kBlocks * kRowWaves;
     __shared__ float joint[4][16][DP + 4];
     __shared__ float tops[4][16 * kBlocks], weights[4][16 * kBlocks];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = uniform((int32_t)threadIdx.x / kWave);
     const int rw = wave / kKeyWaves, kw = wave % kKeyWaves;
     const int col = lane % 16, grp = lane / 16;
     int64_t piece;
@@ -255,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
     int64_t left = min(piece, p.total - from);
     const float c = a.scale * kLog2e;
     while (left > 0) {
-        const Row r = row_at(a, p.row);
+        const Row r = shared_row(a, p.row);
         const int64_t in_row = row_units<kKeys>(a, r) * a.kv_heads * a.parts;
         if (p.rest >= in_row) {
             ++p.row;
@@ -292,8 +314,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
 #pragma unroll
             for (int j = 0; j < kCols; ++j) o[b][j] = f32x4{0, 0, 0, 0};
         }
-        const uint16_t *kh = a.k + (int64_t)t.head * a.head_stride;
-        const uint16_t *vh = a.v + (int64_t)t.head * a.head_stride + (kCols * col < a.dim ? kCols * col : 0);
+        global_u16 *kh = (global_u16 *)(a.k + (int64_t)t.head * a.head_stride);
+        global_u16 *vh = (global_u16 *)(a.v + (int64_t)t.head * a.head_stride + (kCols * col < a.dim ? kCols * col : 0));
         const int32_t *pages = a.table + r.slot * a.table_stride;
         const int32_t place = (1 << a.shift) - 1;
 
@@ -305,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
         // The keys of a step; those past the last one that the tile sees stand for it.
         auto load = [&](int32_t k0, Step &x) {
             x.bad = 0;
-            const uint16_t *src[8];
+            global_u16 *src[8];
             const int32_t first = k0 + 4 * grp;
             if (k0 + 32 <= most && a.shift >= 2) {  // four keys lie side by side
 #pragma unroll
@@ -313,8 +335,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
                     const int32_t key = first + 16 * i, page = pages[key >> a.shift];
                     const bool ok = (uint32_t)page < (uint32_t)a.pages;
                     if (!ok) x.bad |= 15u << 4 * i;
-                    const uint16_t *at = ok ? vh + (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride
-                                            : reinterpret_cast<const uint16_t *>(kZeros);
+                    global_u16 *at = ok ? vh + (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride : zeros();
                     const int64_t step = ok ? a.token_stride : 0;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) src[4 * i + j] = at + j * step;
@@ -325,27 +346,26 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
                     const int32_t key = min(first + 16 * (j / 4) + j % 4, most - 1), page = pages[key >> a.shift];
                     const bool ok = (uint32_t)page < (uint32_t)a.pages;
                     if (!ok) x.bad |= 1u << j;
-                    src[j] = ok ? vh + (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride
-                                : reinterpret_cast<const uint16_t *>(kZeros);
+                    src[j] = ok ? vh + (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride : zeros();
                 }
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int32_t key = min(k0 + 16 * i + col, most - 1), page = pages[key >> a.shift];
-                const uint16_t *at = kh + (int64_t)((uint32_t)page < (uint32_t)a.pages ? page : 0) * a.page_stride +
+                global_u16 *at = kh + (int64_t)((uint32_t)page < (uint32_t)a.pages ? page : 0) * a.page_stride +
                                      (int64_t)(key & place) * a.token_stride;
 #pragma unroll
                 for (int s = 0; s < kSteps; ++s) {
                     const int d = 32 * s + 8 * grp;
-                    x.k[i][s] = *reinterpret_cast<const u32x4 *>(at + (d < a.dim ? d : 0));
+                    x.k[i][s] = *(global_u32x4 *)(at + (d < a.dim ? d : 0));
                 }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if constexpr (kCols == 8) {
-                    x.v[j] = *reinterpret_cast<const u32x4 *>(src[j]);
+                    x.v[j] = *(global_u32x4 *)src[j];
                 } else {
-                    const u32x2 y = *reinterpret_cast<const u32x2 *>(src[j]);
+                    const u32x2 y = *(global_u32x2 *)src[j];
                     x.v[j] = u32x4{y[0], y[1], 0, 0};
                 }
             }
@@ -492,48 +512,53 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
 
 // -------------------------------------------------------------------- wide ---
 
-// A tile of 256 rows, 32 to a wave, by 64 keys a unit: the matrix products bound it.
-// K and V go through LDS, two units of each: the next one's bytes are on their way in
+// A tile of 256 rows, 64 to a wave, by 64 keys a unit: the matrix products bound it.
+// K and V go through LDS, two units of each; the next one's bytes are on their way in
 // registers while this one is computed.  Their 16-byte pieces lie in an order that leaves
 // no bank asked twice.  As above S^T = K Q^T, O^T = V^T P^T (V read from LDS by columns),
-// so the weights stay in their lanes.  Two waves share a matrix unit: one's products run
-// beside the other's exponentials.
-constexpr int kWideKeys = 64, kWideRows = 256, kWideThreads = 512;
+// so the weights stay in their lanes.  A wave has its matrix unit to itself, and 64 rows,
+// since with 32 the reads of K and V from LDS take as long as the products.  So that the
+// matrix unit does not wait for the softmax, a half unit (32 keys) is in three stages at
+// once: the products of the next half's scores and of the last half's weights with V run
+// beside this half's exponentials.
+constexpr int kWideKeys = 64, kWideRows = 256;
 
 template <int DP, bool kHalf>
-__global__ void __launch_bounds__(kWideThreads, 2) k_attend_wide(Attend a) {
+__global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
     constexpr int kPieces = DP / 8;            // 16-byte pieces of a key
     constexpr int kSteps = DP / 16;            // products over 16 dimensions
     constexpr int kCols = DP / 32;             // blocks of 32 output dimensions
-    constexpr int kLoads = kPieces * kWideKeys / kWideThreads;
-    __shared__ __align__(16) uint16_t kbuf[2][kWideKeys * DP], vbuf[2][kWideKeys * DP];
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    constexpr int kLoads = kPieces * kWideKeys / kThreads;
+    constexpr uint32_t kUnit = kWideKeys * DP;
+    __shared__ __align__(16) uint16_t bufs[4 * kUnit];  // two units of K, two of V
+    uint16_t *const kbuf = bufs, *const vbuf = bufs + 2 * kUnit;
+    const int lane = threadIdx.x % kWave, wave = uniform((int32_t)threadIdx.x / kWave);
     const int col = lane % 32, half = lane / 32;
     // blocks go to the eight dies in turn: neighbouring pieces, which share K and V, to one die
     const int64_t block = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     int64_t piece;
-    Place p = find<kWideKeys, kWideThreads>(a, block, &piece);
+    Place p = find<kWideKeys>(a, block, &piece);
     if (p.row < 0) return;
     int64_t left = min(piece, p.total - block * piece);
     const float c = a.scale * kLog2e;
     const int32_t place = (1 << a.shift) - 1;
 
     // where piece x of key k lies in its row of LDS
-    auto k_at = [](int key, int x) { return x ^ (kPieces == 16 ? key & 15 : (key >> 1) & 7); };
-    auto v_at = [](int key, int x) { return x ^ (kPieces == 16 ? 2 * (key & 7) : 2 * ((key >> 1) & 3)); };
+    auto k_at = [](uint32_t key, uint32_t x) { return x ^ (kPieces == 16 ? key & 15 : (key >> 1) & 7); };
+    auto v_at = [](uint32_t key, uint32_t x) { return x ^ (kPieces == 16 ? 2 * (key & 7) : 2 * ((key >> 1) & 3)); };
     // this lane's reads: K rows as the first factor; V by columns: four keys of one dimension
     uint32_t k_read[kSteps], v_read[kCols];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) k_read[s] = col * DP + 8 * k_at(col, 2 * s + half);
-    const int vk = 4 * half + (lane % 16) / 4;  // key of the lane's 8 bytes (+ 8, 16, 24)
+    const uint32_t vk = 4 * half + (lane % 16) / 4;  // key of the lane's 8 bytes (+ 8, 16, 24)
 #pragma unroll
     for (int d = 0; d < kCols; ++d) {
-        const int dim = 32 * d + 16 * (lane / 16 % 2) + 4 * (lane % 4);
+        const uint32_t dim = 32 * d + 16 * (lane / 16 % 2) + 4 * (lane % 4);
         v_read[d] = vk * DP + 8 * v_at(vk, dim / 8) + dim % 8;
     }
 
     while (left > 0) {
-        const Row r = row_at(a, p.row);
+        const Row r = shared_row(a, p.row);
         const int64_t in_row = row_units<kWideKeys>(a, r) * a.kv_heads * a.parts;
         if (p.rest >= in_row) {
             ++p.row;
@@ -544,152 +569,292 @@ __global__ void __launch_bounds__(kWideThreads, 2) k_attend_wide(Attend a) {
         const int64_t take = min(t.units - t.done, left);
         const int32_t all = max(0, r.base + r.n);
         const int32_t most = max(0, min(r.base + t.first + t.n, all));
-        const int row = 32 * wave + col, tok = row / t.heads, h = row - tok * t.heads;
-        const bool is = tok < t.n;
-        const int32_t seen = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
-        // keys that every query of the wave's sees
-        const int32_t least = (32 * wave + 31) / t.heads < t.n
-                                  ? max(0, min(r.base + t.first + 32 * wave / t.heads + 1, all)) : 0;
-        const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
-        u32x4 q[kSteps];
+        u32x4 q[2][kSteps];
+        int32_t seen[2];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int d = 16 * s + 8 * half;
-            q[s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(a.q + token * a.q_token + head * a.q_head + d)
-                                   : u32x4{0, 0, 0, 0};
+        for (int b = 0; b < 2; ++b) {
+            const int row = 64 * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
+            const bool is = tok < t.n;
+            seen[b] = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
+            const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
+                                  (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const int d = 16 * s + 8 * half;
+                q[b][s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(src + d) : u32x4{0, 0, 0, 0};
+            }
         }
-        f32x16 o[kCols];
-        float m = -INFINITY, l = 0.f;
+        // keys that every query of the wave's sees
+        const int32_t least = (64 * wave + 63) / t.heads < t.n
+                                  ? max(0, min(r.base + t.first + 64 * wave / t.heads + 1, all)) : 0;
+        f32x16 o[2][kCols], sa[2], sb[2];
+        u32x4 pa[2][2], pb[2][2];
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, top[2];
 #pragma unroll
-        for (int d = 0; d < kCols; ++d) o[d] = f32x16{};
-        const uint16_t *kh = a.k + (int64_t)t.head * a.head_stride, *vh = a.v + (int64_t)t.head * a.head_stride;
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int d = 0; d < kCols; ++d) o[b][d] = f32x16{};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) pa[b][i] = u32x4{0, 0, 0, 0};
+        }
+        global_u16 *kh = (global_u16 *)(a.k + (int64_t)t.head * a.head_stride);
+        global_u16 *vh = (global_u16 *)(a.v + (int64_t)t.head * a.head_stride);
         const int32_t *pages = a.table + r.slot * a.table_stride;
 
-        // A unit's keys, one per lane: where its vectors lie (-1: in no page).  Keys past the last
-        // one that the tile sees stand for it.
-        auto place_of = [&](int64_t unit) -> int64_t {
-            const int32_t key = min((int32_t)(unit * kWideKeys) + lane, most - 1), page = pages[key >> a.shift];
+        // A unit's keys, one per lane: its page, and where its vectors lie (-1: in no page).  Keys past
+        // the last one that the tile sees stand for it.
+        auto key_of = [&](int32_t unit) { return min(unit * kWideKeys + lane, most - 1); };
+        auto page_of = [&](int32_t unit) { return pages[key_of(unit) >> a.shift]; };
+        auto place_of = [&](int32_t unit, int32_t page) -> int64_t {
             return (uint32_t)page < (uint32_t)a.pages
-                       ? (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride : -1;
+                       ? (int64_t)page * a.page_stride + (int64_t)(key_of(unit) & place) * a.token_stride : -1;
         };
         u32x4 k_in[kLoads], v_in[kLoads];
-        auto load = [&](int64_t where) {
+        auto load_k = [&](int64_t where) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int at = i * kWideThreads + threadIdx.x, key = at / kPieces, d = 8 * (at % kPieces);
-                const int64_t off = __shfl(where, key), to = max(off, (int64_t)0) + (d < a.dim ? d : 0);
-                k_in[i] = *reinterpret_cast<const u32x4 *>(kh + to);
-                v_in[i] = *reinterpret_cast<const u32x4 *>(off < 0 ? reinterpret_cast<const uint16_t *>(kZeros) : vh + to);
+                const int at = i * kThreads + threadIdx.x, d = 8 * (at % kPieces);
+                const int64_t off = __shfl(where, at / kPieces);
+                k_in[i] = *(global_u32x4 *)(kh + max(off, (int64_t)0) + (d < a.dim ? d : 0));
             }
         };
-        auto store = [&](uint16_t *k, uint16_t *v) {
+        auto load_v = [&](int64_t where) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int at = i * kWideThreads + threadIdx.x, key = at / kPieces, x = at % kPieces;
-                *reinterpret_cast<u32x4 *>(k + key * DP + 8 * k_at(key, x)) = k_in[i];
-                *reinterpret_cast<u32x4 *>(v + key * DP + 8 * v_at(key, x)) = v_in[i];
+                const int at = i * kThreads + threadIdx.x, d = 8 * (at % kPieces);
+                const int64_t off = __shfl(where, at / kPieces);
+                v_in[i] = *(global_u32x4 *)(off < 0 ? zeros() : vh + off + (d < a.dim ? d : 0));
             }
         };
-        auto read_v = [&](const uint16_t *from, int d, int i) -> u32x4 {  // keys 16 i + 4 half + (0..3, 8..11)
+        auto store_k = [&](uint32_t buf) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const uint32_t at = i * kThreads + threadIdx.x, key = at / kPieces;
+                *reinterpret_cast<u32x4 *>(kbuf + buf + key * DP + 8 * k_at(key, at % kPieces)) = k_in[i];
+            }
+        };
+        auto store_v = [&](uint32_t buf) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const uint32_t at = i * kThreads + threadIdx.x, key = at / kPieces;
+                *reinterpret_cast<u32x4 *>(vbuf + buf + key * DP + 8 * v_at(key, at % kPieces)) = v_in[i];
+            }
+        };
+        auto read_k = [&](uint32_t at, int s) { return *reinterpret_cast<const u32x4 *>(kbuf + at + k_read[s]); };
+        auto read_v = [&](uint32_t at, int d, int i) -> u32x4 {  // keys 16 i + 4 half + (0..3, 8..11)
             typedef __attribute__((address_space(3))) i16x4 lds;
-            const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + v_read[d] + 16 * i * DP));
-            const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + v_read[d] + (16 * i + 8) * DP));
-            const u32x2 u = __builtin_bit_cast(u32x2, x), w = __builtin_bit_cast(u32x2, y);
-            return u32x4{u[0], u[1], w[0], w[1]};
+            const uint16_t *from = vbuf + at + v_read[d] + 16 * i * DP;
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)from));
+            const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + 8 * DP)));
+            return u32x4{x[0], x[1], y[0], y[1]};
+        };
+        auto highest = [&](const f32x16 &s) {
+            float x = s[0];
+#pragma unroll
+            for (int i = 1; i < 15; i += 2) x = fmaxf(fmaxf(x, s[i]), s[i + 1]);
+            x = fmaxf(x, s[15]);
+            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+            return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+        };
+        auto scores = [&](uint32_t at, f32x16 (&s)[2]) {
+            s[0] = s[1] = f32x16{};
+#pragma unroll
+            for (int d = 0; d < kSteps; ++d) {
+                const u32x4 k = read_k(at, d);
+                s[0] = mfma32<kHalf>(k, q[0][d], s[0]);
+                s[1] = mfma32<kHalf>(k, q[1][d], s[1]);
+            }
+        };
+        auto gather = [&](uint32_t at, const u32x4 (&w)[2][2]) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int d = 0; d < kCols; ++d) {
+                    const u32x4 v = read_v(at, d, i);
+                    o[0][d] = mfma32<kHalf>(v, w[0][i], o[0][d]);
+                    o[1][d] = mfma32<kHalf>(v, w[1][i], o[1][d]);
+                }
+        };
+        // scores of the half unit at key k0: those not seen are -inf
+        auto settle = [&](int32_t k0, uint32_t ok, f32x16 (&s)[2]) {
+            if (k0 + 32 > least || ~ok) {
+                asm volatile("");  // a branch, not selections in every turn
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int32_t rest = seen[b] - k0 - 4 * half;
+                    const uint32_t have = ok >> 4 * half;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = 8 * (i / 4) + i % 4;
+                        if (key >= rest || !(have >> key & 1)) s[b][i] = -INFINITY;
+                    }
+                    top[b] = highest(s[b]);
+                }
+            }
+        };
+        // m follows when it lags too far; the weights w, which are under the old one, go to O first
+        auto follow = [&](uint32_t at, u32x4 (&w)[2][2]) {
+            if (__any((top[0] - m[0]) * c > kLag || (top[1] - m[1]) * c > kLag)) {
+                asm volatile("");
+                gather(at, w);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const float now = fmaxf(m[b], top[b]);
+                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
+                    m[b] = now;
+                    l[b] *= keep;
+#pragma unroll
+                    for (int d = 0; d < kCols; ++d) o[b][d] *= keep;
+                    w[b][0] = w[b][1] = u32x4{0, 0, 0, 0};
+                }
+            }
+        };
+        // One half unit: its weights from s into w, the next scores into s1, the last weights w0 into O.
+        // A step is the two products with one fragment of K or V, the reads of a fragment further on, and
+        // a share of the softmax; the compiler keeps to the steps' order, which feeds the matrix unit.
+        auto stage = [&](const f32x16 (&s)[2], u32x4 (&w)[2][2], uint32_t k, f32x16 (&s1)[2], uint32_t v,
+                         const u32x4 (&w0)[2][2]) {
+            constexpr int kFrags = kSteps + 2 * kCols, kAhead = 2, kEach = 32 / kFrags;
+            constexpr int kTop = (16 + kFrags - kSteps - 2) / (kFrags - kSteps - 1);  // scores looked at in a step
+            const float mc[2] = {m[0] == -INFINITY ? 0.f : m[0] * c, m[1] == -INFINITY ? 0.f : m[1] * c};
+            u32x4 frag[kAhead + 1];
+            auto fetch = [&](int f) {
+                frag[f % (kAhead + 1)] = f < kSteps ? read_k(k, f) : read_v(v, (f - kSteps) % kCols, (f - kSteps) / kCols);
+            };
+            auto multiply = [&](int f, int b) {
+                const u32x4 x = frag[f % (kAhead + 1)];
+                if (f < kSteps) {
+                    s1[b] = mfma32<kHalf>(x, q[b][f], f == 0 ? f32x16{} : s1[b]);
+                } else {
+                    const int d = (f - kSteps) % kCols, i = (f - kSteps) / kCols;
+                    o[b][d] = mfma32<kHalf>(x, w0[b][i], o[b][d]);
+                }
+            };
+            float odd;
+            auto weigh = [&](int e) {  // element e of the half unit's weights; two are packed together
+                const int b = e / 16, i = e % 16;
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], c, -mc[b]));
+                l[b] += x;
+                if (i % 2 == 0) odd = x;
+                else {
+                    uint32_t y = pack<kHalf>(odd, x);
+                    asm volatile("" : "+v"(y));  // here, not where it is first used
+                    w[b][i / 8][i % 8 / 2] = y;
+                }
+            };
+#pragma unroll
+            for (int f = 0; f < kAhead; ++f) fetch(f);
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) {
+                if (f + kAhead < kFrags) fetch(f + kAhead);
+#pragma unroll
+                for (int e = 0; e < kEach / 2; ++e) weigh(kEach * f + e);
+                multiply(f, 0);
+#pragma unroll
+                for (int e = kEach / 2; e < kEach; ++e) weigh(kEach * f + e);
+                multiply(f, 1);
+                if (f > kSteps) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int i = kTop * (f - kSteps - 1); i < min(16, kTop * (f - kSteps)); ++i)
+                            top[b] = i ? fmaxf(top[b], s1[b][i]) : s1[b][0];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[b]), __float_as_uint(top[b]), false, false);
+                top[b] = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+            }
         };
 
-        const int64_t u0 = t.done, u1 = u0 + take;
+        const int32_t u0 = (int32_t)t.done, u1 = (int32_t)(u0 + take);
         if (u0 * kWideKeys < most) {
-            int64_t where = place_of(u0);
-            uint64_t ok = __ballot(where >= 0);  // the unit's keys that lie in a page
-            load(where);
-            if (u0 + 1 < u1) where = place_of(u0 + 1);
-            store(kbuf[0], vbuf[0]);
+            int32_t page0 = page_of(u0), page1 = page_of(u0 + 1), page2 = page_of(u0 + 2);
+            int64_t where = place_of(u0, page0);
+            uint64_t ok = __ballot(where >= 0);  // keys of unit u, of the one after it, that lie in a page
+            load_k(where);
+            load_v(where);
+            int64_t v_where = place_of(u0 + 1, page1);
+            uint64_t ok1 = __ballot(v_where >= 0);
+            __syncthreads();  // the last tile is done with the buffers
+            store_k(0);
+            store_v(0);
+            load_k(v_where);
+            // the half unit before the first has weights of zero and a V of zeros
+#pragma unroll
+            for (int i = 0; i < 32 * DP / 8 / kThreads; ++i)
+                *reinterpret_cast<u32x4 *>(vbuf + kUnit + 32 * DP + 8 * (i * kThreads + threadIdx.x)) = u32x4{0, 0, 0, 0};
+            store_k(kUnit);
             __syncthreads();
-            for (int64_t u = u0; u < u1; ++u) {
-                const int x = (int)(u - u0) & 1;
-                const int32_t key0 = (int32_t)(u * kWideKeys);
-                const uint64_t ok1 = __ballot(where >= 0);
-                if (u + 1 < u1) load(where);
-                if (u + 2 < u1) where = place_of(u + 2);
-                f32x16 s[2] = {f32x16{}, f32x16{}};
+            scores(0, sa);
 #pragma unroll
-                for (int d = 0; d < kSteps; ++d)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        s[i] = mfma32<kHalf>(*reinterpret_cast<const u32x4 *>(&kbuf[x][k_read[d] + 32 * i * DP]), q[d], s[i]);
-                if (key0 + kWideKeys > least || ~ok) {
-                    const int32_t rest = seen - key0 - 4 * half;
-                    const uint64_t have = ok >> 4 * half;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int key = 8 * (i / 4) + i % 4;
-                        if (key >= rest || !(have >> key & 1)) s[i / 16][i % 16] = -INFINITY;
-                    }
-                }
-                float top = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(fmaxf(top, s[0][i]), s[1][i]);
-                const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-                top = fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1]));
-                if (__any((top - m) * c > kLag)) {
-                    const float now = fmaxf(m, top);
-                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - now) * c);
-                    m = now;
-                    l *= keep;
-#pragma unroll
-                    for (int d = 0; d < kCols; ++d) o[d] *= keep;
-                }
-                const float mc = m == -INFINITY ? 0.f : m * c;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float w[8];
-                    u32x4 pw;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][8 * (i % 2) + j], c, -mc));
-                        l += w[j];
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) pw[j] = pack<kHalf>(w[2 * j], w[2 * j + 1]);
-#pragma unroll
-                    for (int d = 0; d < kCols; ++d) o[d] = mfma32<kHalf>(read_v(vbuf[x], d, i), pw, o[d]);
-                }
-                if (u + 1 < u1) store(kbuf[x ^ 1], vbuf[x ^ 1]);
+            for (int b = 0; b < 2; ++b) top[b] = highest(sa[b]);
+            settle(u0 * kWideKeys, (uint32_t)ok, sa);
+            m[0] = top[0];
+            m[1] = top[1];
+            uint32_t x = 0;  // of unit u's buffers
+            for (int32_t u = u0; u < u1; ++u) {
+                const uint32_t y = kUnit - x;
+                const int64_t k_where = place_of(u + 2, page2);
+                load_k(k_where);
+                load_v(v_where);
+                page2 = page_of(u + 3);
+                stage(sa, pb, x + 32 * DP, sb, y + 32 * DP, pa);
+                settle(u * kWideKeys + 32, (uint32_t)(ok >> 32), sb);
+                __syncthreads();  // the next unit's K and this one's V are there, the buffers behind them free
+                follow(x, pb);
+                v_where = k_where;
                 ok = ok1;
-                __syncthreads();
+                ok1 = __ballot(k_where >= 0);
+                stage(sb, pa, y, sa, x, pb);
+                settle(u * kWideKeys + 64, (uint32_t)ok, sa);
+                if (u + 1 < u1) follow(x + 32 * DP, pa);
+                store_k(x);  // unit u + 2
+                store_v(y);  // unit u + 1
+                x = y;
             }
+            gather(kUnit - x + 32 * DP, pa);
         }
-        // o[d][i] is dimension 32 d + 8 (i / 4) + 4 half + i % 4 of query `col`
+        // o[b][d][i] is dimension 32 d + 8 (i / 4) + 4 half + i % 4 of query `col`
         const bool whole = take == t.units;
         const int64_t at = 2 * block + (t.done == 0);
-        const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-        l = __uint_as_float(other[0]) + __uint_as_float(other[1]);
-        if (is && whole) {
-            const float inv = l > 0.f ? 1.f / l : 0.f;
-            uint16_t *dst = a.out + token * a.out_token + head * a.out_head;
 #pragma unroll
-            for (int d = 0; d < kCols; ++d)
+        for (int b = 0; b < 2; ++b) {
+            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[b]), __float_as_uint(l[b]), false, false);
+            const float sum = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+            const int row = 64 * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
+            if (tok >= t.n) continue;
+            if (whole) {
+                const float inv = sum > 0.f ? 1.f / sum : 0.f;
+                const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
+                uint16_t *dst = a.out + token * a.out_token + head * a.out_head;
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const int dim = 32 * d + 2 * i + 4 * half;
-                    if (dim < a.dim)
-                        *reinterpret_cast<u32x2 *>(dst + dim) = u32x2{pack<kHalf>(o[d][i] * inv, o[d][i + 1] * inv),
-                                                                      pack<kHalf>(o[d][i + 2] * inv, o[d][i + 3] * inv)};
+                for (int d = 0; d < kCols; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const int dim = 32 * d + 2 * i + 4 * half;
+                        if (dim < a.dim)
+                            *reinterpret_cast<u32x2 *>(dst + dim) =
+                                u32x2{pack<kHalf>(o[b][d][i] * inv, o[b][d][i + 1] * inv),
+                                      pack<kHalf>(o[b][d][i + 2] * inv, o[b][d][i + 3] * inv)};
+                    }
+                if (a.lse && half == 0)
+                    a.lse[token * a.heads + head] = sum > 0.f ? m[b] * a.scale + logf(sum) : -INFINITY;
+            } else {
+                float *dst = a.sums + (at * kWideRows + row) * DP;
+#pragma unroll
+                for (int d = 0; d < kCols; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<f32x4 *>(dst + 32 * d + 2 * i + 4 * half) =
+                            f32x4{o[b][d][i], o[b][d][i + 1], o[b][d][i + 2], o[b][d][i + 3]};
+                if (half == 0) {
+                    float *ml = a.sums + 2 * (int64_t)a.blocks * kWideRows * DP + (at * kWideRows + row) * 2;
+                    ml[0] = m[b];
+                    ml[1] = sum;
                 }
-            if (a.lse && half == 0) a.lse[token * a.heads + head] = l > 0.f ? m * a.scale + logf(l) : -INFINITY;
-        } else if (is) {
-            float *dst = a.sums + (at * kWideRows + row) * DP;
-#pragma unroll
-            for (int d = 0; d < kCols; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<f32x4 *>(dst + 32 * d + 2 * i + 4 * half) =
-                        f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
-            if (half == 0) {
-                float *ml = a.sums + 2 * (int64_t)a.blocks * kWideRows * DP + (at * kWideRows + row) * 2;
-                ml[0] = m;
-                ml[1] = l;
             }
         }
         p.rest += take;
@@ -713,7 +878,7 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     const int64_t cut = blockIdx.x + 1;
     const Place p = find<kKeys>(a, cut, &piece);
     if (p.row < 0) return;
-    const Row r = row_at(a, p.row);
+    const Row r = shared_row(a, p.row);
     const Tile t = tile_at<kKeys>(a, r, p.rest);
     if (t.done == 0 || t.done > piece) return;  // between two tiles, or not the tile's first cut
     const int64_t last = cut + (t.units - t.done - 1) / piece;  // the block with the tile's end
@@ -799,7 +964,7 @@ hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
     if (sh.rows() == 32) return launch_narrow<DP, 2, 1, kHalf>(a, s);
     if (sh.rows() == 64) return launch_narrow<DP, 2, 2, kHalf>(a, s);
     if (sh.rows() == 128) return launch_narrow<DP, 2, 4, kHalf>(a, s);
-    hipLaunchKernelGGL((k_attend_wide<DP, kHalf>), dim3((unsigned)a.blocks), dim3(kWideThreads), 0, s, a);
+    hipLaunchKernelGGL((k_attend_wide<DP, kHalf>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((k_join<DP, kWideRows, kWideKeys, kHalf>), dim3((unsigned)a.blocks - 1, kWideRows / kJoin),
