@@ -57,6 +57,13 @@ struct Attend {
     int32_t tq, group, parts, blocks;
     int32_t least;  // units of a block, at least
     float *sums;    // [2 blocks][tile rows][DP] partial sums, then [2 blocks][tile rows][2] their m and sum of weights
+    struct Cut *cuts;  // [blocks] what each block's piece begins with
+};
+
+// The tile that a block's piece begins in, if in its middle (units done before it: > 0).
+struct Cut {
+    int64_t done, units, piece;
+    int32_t token, n, head, heads;  // its first token and query head, and how many
 };
 
 // a value that is the same in all lanes, to the compiler too
@@ -220,6 +227,13 @@ __device__ inline Tile tile_at(const Attend &a, const Row &r, int64_t rest) {
     return t;
 }
 
+// What the block's piece begins with, for k_join.
+__device__ inline void note(const Attend &a, int64_t block, const Row &r, const Tile &t, int64_t piece) {
+    if (threadIdx.x == 0)
+        a.cuts[block] = Cut{t.done, t.units, piece, r.first + t.first, t.n,
+                            t.head * (a.heads / a.kv_heads) + t.part * a.group, t.heads};
+}
+
 // ------------------------------------------------------------------ products ---
 
 template <bool kHalf>
@@ -272,9 +286,13 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
     const int col = lane % 16, grp = lane / 16;
     int64_t piece;
     Place p = find<kKeys>(a, blockIdx.x, &piece);
-    if (p.row < 0) return;
+    if (p.row < 0) {
+        if (threadIdx.x == 0) a.cuts[blockIdx.x].done = 0;
+        return;
+    }
     const int64_t from = blockIdx.x * piece;
-    int64_t left = min(piece, p.total - from);
+    const int64_t whole_piece = min(piece, p.total - from);
+    int64_t left = whole_piece;
     const float c = a.scale * kLog2e;
     while (left > 0) {
         const Row r = shared_row(a, p.row);
@@ -286,6 +304,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
         }
         const Tile t = tile_at<kKeys>(a, r, p.rest);
         const int64_t take = min(t.units - t.done, left);
+        if (left == whole_piece) note(a, blockIdx.x, r, t, piece);
         // queries, one per lane of 16 and block; rows past the tile's see no key.  Lanes
         // past the last dimension read others of the vector (queries: zero).
         u32x4 q[kBlocks][kSteps];
@@ -538,8 +557,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
     const int64_t block = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     int64_t piece;
     Place p = find<kWideKeys>(a, block, &piece);
-    if (p.row < 0) return;
-    int64_t left = min(piece, p.total - block * piece);
+    if (p.row < 0) {
+        if (threadIdx.x == 0) a.cuts[block].done = 0;
+        return;
+    }
+    const int64_t whole_piece = min(piece, p.total - block * piece);
+    int64_t left = whole_piece;
     const float c = a.scale * kLog2e;
     const int32_t place = (1 << a.shift) - 1;
 
@@ -567,6 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         }
         const Tile t = tile_at<kWideKeys>(a, r, p.rest);
         const int64_t take = min(t.units - t.done, left);
+        if (left == whole_piece) note(a, block, r, t, piece);
         const int32_t all = max(0, r.base + r.n);
         const int32_t most = max(0, min(r.base + t.first + t.n, all));
         u32x4 q[2][kSteps];
@@ -866,36 +890,57 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
 
 // Partial sums of the tiles that a cut goes through.  blockIdx.x is the cut after
 // block x, and works on the tile it is the first cut of; blockIdx.y takes kJoin rows of it.
-// Eight threads' groups take the pieces in turn, then their sums meet in LDS.
-constexpr int kJoin = 4;
-
-template <int DP, int kRows, int kKeys, bool kHalf>
+// A group of threads takes a row; where the tile is in many pieces, all groups share a
+// row's pieces and their sums meet in LDS.  The partial sums' bytes bound it.
+template <int DP, int kRows, int kJoin, bool kHalf>
 __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     constexpr int kLanes = DP / 4, kGroups = kThreads / kLanes;
     __shared__ float part[kGroups][DP];
     __shared__ float part_l[kGroups];
-    int64_t piece;
     const int64_t cut = blockIdx.x + 1;
-    const Place p = find<kKeys>(a, cut, &piece);
-    if (p.row < 0) return;
-    const Row r = shared_row(a, p.row);
-    const Tile t = tile_at<kKeys>(a, r, p.rest);
-    if (t.done == 0 || t.done > piece) return;  // between two tiles, or not the tile's first cut
-    const int64_t last = cut + (t.units - t.done - 1) / piece;  // the block with the tile's end
+    const Cut t = a.cuts[cut];
+    if (t.done == 0 || t.done > t.piece) return;  // between two tiles, or not the tile's first cut
+    const int row0 = blockIdx.y * kJoin, row1 = min(row0 + kJoin, t.n * t.heads);
+    if (row0 >= row1) return;
+    const int64_t last = cut + (t.units - t.done - 1) / t.piece;  // the block with the tile's end
     const float c = a.scale * kLog2e;
     const float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP;
     const int lane = threadIdx.x % kLanes, g = threadIdx.x / kLanes;
     // the first piece begins the tile, the others go on with it
     auto slot_of = [&](int64_t i) { return i < cut ? 2 * i + 1 : 2 * i; };
-    for (int row = blockIdx.y * kJoin; row < min((int)(blockIdx.y + 1) * kJoin, kRows); ++row) {
+    auto write = [&](int row, f32x4 x, float l, float mx) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
         const int tok = row / t.heads, h = row - tok * t.heads;
-        if (tok >= t.n) break;
+        const int64_t token = t.token + tok, head = t.head + h;
+        if (4 * lane < a.dim)
+            *reinterpret_cast<u32x2 *>(a.out + token * a.out_token + head * a.out_head + 4 * lane) =
+                u32x2{pack<kHalf>(x[0] * inv, x[1] * inv), pack<kHalf>(x[2] * inv, x[3] * inv)};
+        if (a.lse && lane == 0) a.lse[token * a.heads + head] = l > 0.f ? mx * a.scale + logf(l) : -INFINITY;
+    };
+    if (last - cut < 4) {
+        for (int row = row0 + g; row < row1; row += kGroups) {
+            float mx = -INFINITY;
+            for (int64_t i = cut - 1; i <= last; ++i) mx = fmaxf(mx, ml[(slot_of(i) * kRows + row) * 2]);
+            f32x4 sum{0, 0, 0, 0};
+            float l = 0.f;
+            for (int64_t i = cut - 1; i <= last; ++i) {
+                const int64_t at = slot_of(i) * kRows + row;
+                const float mi = ml[at * 2];
+                const float keep = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi - mx) * c);
+                sum += *reinterpret_cast<const f32x4 *>(a.sums + at * DP + 4 * lane) * keep;
+                l += ml[at * 2 + 1] * keep;
+            }
+            write(row, sum, l, mx);
+        }
+        return;
+    }
+    for (int row = row0; row < row1; ++row) {
         float mx = -INFINITY;
         for (int64_t i = cut - 1 + threadIdx.x % kWave; i <= last; i += kWave) mx = fmaxf(mx, ml[(slot_of(i) * kRows + row) * 2]);
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
         f32x4 sum{0, 0, 0, 0};
-        float lsum = 0.f;
+        float l = 0.f;
 #pragma unroll 4
         for (int64_t i = cut - 1 + g; i <= last; i += kGroups) {
             const int64_t at = slot_of(i) * kRows + row;
@@ -903,11 +948,11 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
             const f32x4 x = *reinterpret_cast<const f32x4 *>(a.sums + at * DP + 4 * lane);
             const float keep = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi - mx) * c);
             sum += x * keep;
-            lsum += li * keep;
+            l += li * keep;
         }
         __syncthreads();
         *reinterpret_cast<f32x4 *>(&part[g][4 * lane]) = sum;
-        if (lane == 0) part_l[g] = lsum;
+        if (lane == 0) part_l[g] = l;
         __syncthreads();
         if (threadIdx.x < kLanes) {
             f32x4 x{0, 0, 0, 0};
@@ -917,12 +962,7 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
                 x += *reinterpret_cast<const f32x4 *>(&part[i][4 * lane]);
                 y += part_l[i];
             }
-            const float inv = y > 0.f ? 1.f / y : 0.f;
-            const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
-            if (4 * lane < a.dim)
-                *reinterpret_cast<u32x2 *>(a.out + token * a.out_token + head * a.out_head + 4 * lane) =
-                    u32x2{pack<kHalf>(x[0] * inv, x[1] * inv), pack<kHalf>(x[2] * inv, x[3] * inv)};
-            if (a.lse && lane == 0) a.lse[token * a.heads + head] = y > 0.f ? mx * a.scale + logf(y) : -INFINITY;
+            write(row, x, y, mx);
         }
     }
 }
@@ -949,11 +989,11 @@ int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
 
 template <int DP, int kBlocks, int kRowWaves, bool kHalf>
 hipError_t launch_narrow(const Attend &a, hipStream_t s) {
-    constexpr int kRows = 16 * kBlocks * kRowWaves, kKeys = 32 * (4 / kRowWaves);
+    constexpr int kRows = 16 * kBlocks * kRowWaves, kJoin = 4;
     hipLaunchKernelGGL((k_attend_narrow<DP, kBlocks, kRowWaves, kHalf>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_join<DP, kRows, kKeys, kHalf>), dim3((unsigned)a.blocks - 1, (unsigned)(kRows / kJoin)),
+    hipLaunchKernelGGL((k_join<DP, kRows, kJoin, kHalf>), dim3((unsigned)a.blocks - 1, (unsigned)(kRows / kJoin)),
                        dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
@@ -967,7 +1007,7 @@ hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
     hipLaunchKernelGGL((k_attend_wide<DP, kHalf>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_join<DP, kWideRows, kWideKeys, kHalf>), dim3((unsigned)a.blocks - 1, kWideRows / kJoin),
+    hipLaunchKernelGGL((k_join<DP, kWideRows, 32, kHalf>), dim3((unsigned)a.blocks - 1, kWideRows / 32),
                        dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
@@ -976,7 +1016,7 @@ hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
 
 int64_t attend_work_bytes(const tam_chunk &c, int64_t heads) {
     const Shape sh = shape_of(c, heads);
-    return 2 * (int64_t)sh.grid * sh.rows() * (padded(c.head_dim) + 2) * 4;
+    return 2 * (int64_t)sh.grid * sh.rows() * (padded(c.head_dim) + 2) * 4 + sh.grid * (int64_t)sizeof(Cut);
 }
 
 hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipStream_t s) {
@@ -987,13 +1027,14 @@ hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipSt
              c.head_stride, c.token_stride, q.q_token, q.q_head, q.out_token, q.out_head, c.table, c.length,
              c.offsets, c.slot_ids, c.table_stride, c.slots, c.max_pages, c.rows, c.tokens, (int32_t)c.num_pages,
              __builtin_ctzll((unsigned long long)c.page_tokens), (int32_t)q.heads, (int32_t)c.kv_heads,
-             (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, nullptr};
+             (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, nullptr, nullptr};
     a.group = (int32_t)std::min<int64_t>(group, sh.rows());
     a.parts = (int32_t)((group + a.group - 1) / a.group);
     a.tq = sh.rows() / a.group;
     a.blocks = sh.grid;
     a.least = 1;
     a.sums = static_cast<float *>(work);
+    a.cuts = reinterpret_cast<Cut *>(a.sums + 2 * (int64_t)sh.grid * sh.rows() * (padded(c.head_dim) + 2));
     const bool half = c.dtype == TAM_DTYPE_FP16;
     if (padded(c.head_dim) == 64) return half ? launch<64, true>(a, sh, s) : launch<64, false>(a, sh, s);
     return half ? launch<128, true>(a, sh, s) : launch<128, false>(a, sh, s);
