@@ -9,12 +9,12 @@
 //
 // A tile is `tq` tokens of one row, times the heads that share a K/V head (their
 // rows of a product are side by side, so K and V are read once for all of them).
-// A unit is a tile's product with kKeys keys.  All units of a call, row after row,
-// head after head, tile after tile, are one line, cut into equal pieces for as
+// A unit is a tile's product with kKeys keys.  The keys that the tiles of a call see, row
+// after row, head after head, tile after tile, are one line, cut into equal pieces for as
 // many blocks as the chip holds: any mix of long and short rows and chunks fills
-// it evenly.  A tile that a cut goes through leaves partial sums in the scratch, which
-// k_join adds up.  The lengths lie on the device: each block finds its piece from
-// them by a prefix sum over the rows.
+// it evenly.  A cut inside a tile moves back to the unit it falls in; the tile's parts
+// leave partial sums in the scratch, which k_join adds up.  The lengths lie on the
+// device: each block finds its piece from them by a prefix sum over the rows.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -55,15 +55,16 @@ struct Attend {
     float scale;
     // the cut: tiles of `tq` tokens by `group` heads, `parts` of them per K/V head
     int32_t tq, group, parts, blocks;
-    int32_t least;  // units of a block, at least
+    int32_t unit;   // keys of a unit, a power of two
     float *sums;    // [2 blocks][tile rows][DP] partial sums, then [2 blocks][tile rows][2] their m and sum of weights
     struct Cut *cuts;  // [blocks] what each block's piece begins with
 };
 
-// The tile that a block's piece begins in, if in its middle (units done before it: > 0).
+// The tile in whose middle a block's piece begins.
 struct Cut {
-    int64_t done, units, piece;
-    int32_t token, n, head, heads;  // its first token and query head, and how many
+    int32_t is;       // this is the first cut of a tile
+    int32_t more;     // the blocks after this one that have parts of the tile
+    int32_t token, n, head, heads;  // the tile's first token and query head, and how many
 };
 
 // a value that is the same in all lanes, to the compiler too
@@ -73,28 +74,6 @@ __device__ inline int64_t uniform(int64_t x) {
 }
 
 // ------------------------------------------------------------------ the cut ---
-
-// sum of floor((a t + b) / m) over t in [0, n), by Euclid's steps on (a, m)
-__device__ inline int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
-    int64_t sum = 0;
-    while (true) {
-        if (a >= m) {
-            sum += (int64_t)n * (n - 1) / 2 * (a / m);
-            a %= m;
-        }
-        if (b >= m) {
-            sum += (int64_t)n * (b / m);
-            b %= m;
-        }
-        const uint64_t y = (uint64_t)a * n + b;
-        if (y < m) return sum;
-        n = (uint32_t)(y / m);
-        b = (uint32_t)(y % m);
-        const uint32_t t = m;
-        m = a;
-        a = t;
-    }
-}
 
 struct Row {
     int32_t n, base;    // tokens of the chunk; tokens of the sequence before it (may be negative)
@@ -129,36 +108,35 @@ __device__ inline Row shared_row(const Attend &a, int64_t i) {
     return r;
 }
 
-// Units of the tiles before tile t of a row (all of them full).
-template <int kKeys>
-__device__ inline int64_t units_before(const Attend &a, const Row &r, uint32_t t) {
-    return t ? floor_sum(t, kKeys, a.tq, max(r.base, 0) + a.tq + kKeys - 1) : 0;
+// Keys on the line before tile t of a row and head: tile i < t sees base + (i + 1) tq.
+__device__ inline int64_t keys_before(const Attend &a, const Row &r, int64_t t) {
+    return t * max(r.base, 0) + a.tq * (t * (t + 1) / 2);
 }
 
-template <int kKeys>
-__device__ inline int64_t row_units(const Attend &a, const Row &r) {
-    if (r.n == 0) return 0;
-    const uint32_t tiles = (r.n + a.tq - 1) / a.tq;
-    return units_before<kKeys>(a, r, tiles - 1) + (max(r.base, 0) + r.n + kKeys - 1) / kKeys;
+// Keys on the line of a row and head.  A row of one tile takes whole units, so that a
+// batch of them is cut between units.
+__device__ inline int64_t row_keys(const Attend &a, const Row &r) {
+    const int64_t all = max(r.base, 0) + r.n;
+    if (r.n <= a.tq) return r.n ? (all + a.unit - 1) & -(int64_t)a.unit : 0;
+    return keys_before(a, r, (r.n - 1) / a.tq) + all;
 }
 
-// A place on the line of units.
+// A place on the line.
 struct Place {
-    int64_t row, total;   // the row; units of all rows
-    int64_t rest;         // units of the row before this place
+    int64_t row, total;   // the row; keys on the whole line
+    int64_t rest;         // keys of the row before this place
 };
 
-// The place of unit number `share * piece` (share: this block's number), and the units of a
-// piece.  All threads of the block call it; row < 0 past the line's end.
-template <int kKeys, int kN = kThreads>
+// Where piece number `share` (this block's) begins, and the keys of a piece.  All threads of
+// the block call it; row < 0 past the line's end.
 __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
-    __shared__ int64_t sums[kN / kWave];
+    __shared__ int64_t sums[kThreads / kWave];
     __shared__ int64_t found[2];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t per = (a.rows + kN - 1) / kN, lo = threadIdx.x * per, hi = min(lo + per, a.rows);
+    const int64_t per = (a.rows + kThreads - 1) / kThreads, lo = threadIdx.x * per, hi = min(lo + per, a.rows);
     const int64_t heads = (int64_t)a.kv_heads * a.parts;
     int64_t mine = 0;
-    for (int64_t i = lo; i < hi; ++i) mine += heads * row_units<kKeys>(a, row_at(a, i));
+    for (int64_t i = lo; i < hi; ++i) mine += heads * row_keys(a, row_at(a, i));
     int64_t upto = mine;
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) {
@@ -171,18 +149,18 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
     Place p;
     p.total = 0;
 #pragma unroll
-    for (int w = 0; w < kN / kWave; ++w) {
+    for (int w = 0; w < kThreads / kWave; ++w) {
         if (w < wave) upto += sums[w];
         p.total += sums[w];
     }
     p.total = uniform(p.total);
-    *piece = max((int64_t)a.least, (p.total + a.blocks - 1) / a.blocks);
+    *piece = max((int64_t)1, (p.total + (int64_t)a.blocks * a.unit - 1) / ((int64_t)a.blocks * a.unit)) * a.unit;
     const int64_t at = share * *piece;
     if (at >= upto - mine && at < upto) {  // one thread: walk its rows
         int64_t rest = at - (upto - mine);
         int64_t i = lo;
         for (; i < hi; ++i) {
-            const int64_t u = heads * row_units<kKeys>(a, row_at(a, i));
+            const int64_t u = heads * row_keys(a, row_at(a, i));
             if (rest < u) break;
             rest -= u;
         }
@@ -195,43 +173,56 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
     return p;
 }
 
-// A tile, and the units of it before the place.
+// A tile, and the place in it.
 struct Tile {
     int32_t head, part, tile;     // K/V head and part of its group; number in the row
     int32_t first, n;             // its first token in the chunk, and its tokens
     int32_t heads;                // query heads of the part
-    int64_t units, done;
+    int64_t rest, keys;           // keys of it before the place, and all that it sees
 };
 
-template <int kKeys>
 __device__ inline Tile tile_at(const Attend &a, const Row &r, int64_t rest) {
-    const int64_t u = row_units<kKeys>(a, r);
-    const int64_t vh = rest / u;
+    const int64_t u = row_keys(a, r);
+    const int32_t vh = (int32_t)(rest / u);
     rest -= vh * u;
-    const uint32_t tiles = (r.n + a.tq - 1) / a.tq;
-    uint32_t lo = 0, hi = tiles;  // units_before(lo) <= rest < units_before(hi)
+    int32_t lo = 0, hi = (r.n + a.tq - 1) / a.tq;  // keys_before(lo) <= rest < keys_before(hi)
     while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) >> 1;
-        if (units_before<kKeys>(a, r, mid) <= rest) lo = mid;
+        const int32_t mid = (lo + hi) >> 1;
+        if (keys_before(a, r, mid) <= rest) lo = mid;
         else hi = mid;
     }
     Tile t;
-    t.head = (int32_t)(vh / a.parts);
-    t.part = (int32_t)(vh - (int64_t)t.head * a.parts);
-    t.tile = (int32_t)lo;
-    t.first = t.tile * a.tq;
+    t.head = vh / a.parts;
+    t.part = vh - t.head * a.parts;
+    t.tile = lo;
+    t.first = lo * a.tq;
     t.n = min(a.tq, r.n - t.first);
     t.heads = min(a.group, a.heads / a.kv_heads - t.part * a.group);
-    t.done = rest - units_before<kKeys>(a, r, lo);
-    t.units = (max(r.base, 0) + min((int32_t)((lo + 1) * a.tq), r.n) + kKeys - 1) / kKeys;
+    t.rest = rest - keys_before(a, r, lo);
+    t.keys = r.n <= a.tq ? u : max(r.base, 0) + t.first + t.n;
     return t;
 }
 
+// The units of a tile that are a block's: from .. to of all.
+struct Share {
+    int32_t from, to, all;
+};
+
+template <int kKeys>
+__device__ inline Share share_of(const Tile &t, int64_t left) {
+    Share s;
+    s.all = (int32_t)((t.keys + kKeys - 1) / kKeys);
+    s.from = (int32_t)(t.rest / kKeys);
+    s.to = left >= t.keys - t.rest ? s.all : (int32_t)((t.rest + left) / kKeys);
+    return s;
+}
+
 // What the block's piece begins with, for k_join.
+template <int kKeys>
 __device__ inline void note(const Attend &a, int64_t block, const Row &r, const Tile &t, int64_t piece) {
     if (threadIdx.x == 0)
-        a.cuts[block] = Cut{t.done, t.units, piece, r.first + t.first, t.n,
-                            t.head * (a.heads / a.kv_heads) + t.part * a.group, t.heads};
+        a.cuts[block] = Cut{t.rest >= kKeys && t.rest - piece < kKeys, (int32_t)((t.keys - t.rest - 1) / piece),
+                            r.first + t.first, t.n, t.head * (a.heads / a.kv_heads) + t.part * a.group, t.heads};
 }
 
 // ------------------------------------------------------------------ products ---
@@ -285,9 +276,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
     const int rw = wave / kKeyWaves, kw = wave % kKeyWaves;
     const int col = lane % 16, grp = lane / 16;
     int64_t piece;
-    Place p = find<kKeys>(a, blockIdx.x, &piece);
+    Place p = find(a, blockIdx.x, &piece);
     if (p.row < 0) {
-        if (threadIdx.x == 0) a.cuts[blockIdx.x].done = 0;
+        if (threadIdx.x == 0) a.cuts[blockIdx.x].is = 0;
         return;
     }
     const int64_t from = blockIdx.x * piece;
@@ -296,15 +287,18 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
     const float c = a.scale * kLog2e;
     while (left > 0) {
         const Row r = shared_row(a, p.row);
-        const int64_t in_row = row_units<kKeys>(a, r) * a.kv_heads * a.parts;
+        const int64_t in_row = row_keys(a, r) * a.kv_heads * a.parts;
         if (p.rest >= in_row) {
             ++p.row;
             p.rest = 0;
             continue;
         }
-        const Tile t = tile_at<kKeys>(a, r, p.rest);
-        const int64_t take = min(t.units - t.done, left);
-        if (left == whole_piece) note(a, blockIdx.x, r, t, piece);
+        const Tile t = tile_at(a, r, p.rest);
+        const Share share = share_of<kKeys>(t, left);
+        if (left == whole_piece) note<kKeys>(a, blockIdx.x, r, t, piece);
+        p.rest += t.keys - t.rest;
+        left -= t.keys - t.rest;
+        if (share.from == share.to) continue;  // (the piece ends in the tile's first unit)
         // queries, one per lane of 16 and block; rows past the tile's see no key.  Lanes
         // past the last dimension read others of the vector (queries: zero).
         u32x4 q[kBlocks][kSteps];
@@ -436,8 +430,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
                 for (int j = 0; j < kCols; ++j) o[b][j] = mfma16<kHalf>(v[j], pw, o[b][j]);
             }
         };
-        const int32_t k_end = (int32_t)min((t.done + take) * kKeys, (int64_t)most);
-        int32_t k0 = (int32_t)(t.done * kKeys) + 32 * kw;
+        const int32_t k_end = min(share.to * kKeys, most);
+        int32_t k0 = share.from * kKeys + 32 * kw;
         if (k0 < k_end) {
             Step x, y;
             load(k0, x);
@@ -463,8 +457,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
             }
         }
         __syncthreads();
-        const bool whole = take == t.units;
-        const int64_t at = 2 * (int64_t)blockIdx.x + (t.done == 0);  // a cut tile's partial sums
+        const bool whole = share.to - share.from == share.all;
+        const int64_t at = 2 * (int64_t)blockIdx.x + (share.from == 0);  // a cut tile's partial sums
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
             float top = -INFINITY;
@@ -524,8 +518,6 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
             }
             __syncthreads();
         }
-        p.rest += take;
-        left -= take;
     }
 }
 
@@ -533,8 +525,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
 
 // A tile of 256 rows, 64 to a wave, by 64 keys a unit: the matrix products bound it.
 // K and V go through LDS, two units of each; the next one's bytes are on their way in
-// registers while this one is computed.  Their 16-byte pieces lie in an order that leaves
-// no bank asked twice.  As above S^T = K Q^T, O^T = V^T P^T (V read from LDS by columns),
+// registers while this one is computed.  Keys lie apart in LDS by their bytes and 16 (K) or
+// 32 (V) more, which leaves no bank asked twice and every read at a fixed distance from
+// one address.  As above S^T = K Q^T, O^T = V^T P^T (V read from LDS by columns),
 // so the weights stay in their lanes.  A wave has its matrix unit to itself, and 64 rows,
 // since with 32 the reads of K and V from LDS take as long as the products.  So that the
 // matrix unit does not wait for the softmax, a half unit (32 keys) is in three stages at
@@ -542,55 +535,56 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
 // beside this half's exponentials.
 constexpr int kWideKeys = 64, kWideRows = 256;
 
-template <int DP, bool kHalf>
+// kRuns: the 16 keys of a write lie side by side in one page (pages of 16 tokens or more, strides of 32
+// bits), so that its number and where they begin are the same for all lanes.
+template <int DP, bool kHalf, bool kRuns>
 __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
     constexpr int kPieces = DP / 8;            // 16-byte pieces of a key
     constexpr int kSteps = DP / 16;            // products over 16 dimensions
     constexpr int kCols = DP / 32;             // blocks of 32 output dimensions
     constexpr int kLoads = kPieces * kWideKeys / kThreads;
-    constexpr uint32_t kUnit = kWideKeys * DP;
-    __shared__ __align__(16) uint16_t bufs[4 * kUnit];  // two units of K, two of V
-    uint16_t *const kbuf = bufs, *const vbuf = bufs + 2 * kUnit;
+    constexpr int kKStride = DP + 8, kVStride = DP + 16;
+    constexpr uint32_t kKUnit = kWideKeys * kKStride, kVUnit = kWideKeys * kVStride;
+    extern __shared__ __align__(16) uint16_t bufs[];  // two units of K, two of V
+    uint16_t *const kbuf = bufs, *const vbuf = bufs + 2 * kKUnit;
     const int lane = threadIdx.x % kWave, wave = uniform((int32_t)threadIdx.x / kWave);
     const int col = lane % 32, half = lane / 32;
     // blocks go to the eight dies in turn: neighbouring pieces, which share K and V, to one die
     const int64_t block = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     int64_t piece;
-    Place p = find<kWideKeys>(a, block, &piece);
+    Place p = find(a, block, &piece);
     if (p.row < 0) {
-        if (threadIdx.x == 0) a.cuts[block].done = 0;
+        if (threadIdx.x == 0) a.cuts[block].is = 0;
         return;
     }
     const int64_t whole_piece = min(piece, p.total - block * piece);
     int64_t left = whole_piece;
     const float c = a.scale * kLog2e;
-    const int32_t place = (1 << a.shift) - 1;
+    const uint32_t place = (1u << a.shift) - 1;
 
-    // where piece x of key k lies in its row of LDS
-    auto k_at = [](uint32_t key, uint32_t x) { return x ^ (kPieces == 16 ? key & 15 : (key >> 1) & 7); };
-    auto v_at = [](uint32_t key, uint32_t x) { return x ^ (kPieces == 16 ? 2 * (key & 7) : 2 * ((key >> 1) & 3)); };
     // this lane's reads: K rows as the first factor; V by columns: four keys of one dimension
-    uint32_t k_read[kSteps], v_read[kCols];
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) k_read[s] = col * DP + 8 * k_at(col, 2 * s + half);
-    const uint32_t vk = 4 * half + (lane % 16) / 4;  // key of the lane's 8 bytes (+ 8, 16, 24)
-#pragma unroll
-    for (int d = 0; d < kCols; ++d) {
-        const uint32_t dim = 32 * d + 16 * (lane / 16 % 2) + 4 * (lane % 4);
-        v_read[d] = vk * DP + 8 * v_at(vk, dim / 8) + dim % 8;
-    }
+    const uint16_t *const k_read = kbuf + col * kKStride + 8 * half;
+    const uint16_t *const v_read = vbuf + (4 * half + (lane % 16) / 4) * kVStride + 16 * (lane / 16 % 2) + 4 * (lane % 4);
+    // and its writes: piece `mine` of keys `key`, `key` + kApart, ...
+    constexpr int kApart = kThreads / kPieces;
+    const int key = threadIdx.x / kPieces, mine = threadIdx.x % kPieces;
+    uint16_t *const k_write = kbuf + key * kKStride + 8 * mine, *const v_write = vbuf + key * kVStride + 8 * mine;
+    const uint32_t in_run = (uint32_t)(key % 16) * (uint32_t)a.token_stride + (8 * mine < a.dim ? 8 * mine : 0);
 
     while (left > 0) {
         const Row r = shared_row(a, p.row);
-        const int64_t in_row = row_units<kWideKeys>(a, r) * a.kv_heads * a.parts;
+        const int64_t in_row = row_keys(a, r) * a.kv_heads * a.parts;
         if (p.rest >= in_row) {
             ++p.row;
             p.rest = 0;
             continue;
         }
-        const Tile t = tile_at<kWideKeys>(a, r, p.rest);
-        const int64_t take = min(t.units - t.done, left);
-        if (left == whole_piece) note(a, block, r, t, piece);
+        const Tile t = tile_at(a, r, p.rest);
+        const Share share = share_of<kWideKeys>(t, left);
+        if (left == whole_piece) note<kWideKeys>(a, block, r, t, piece);
+        p.rest += t.keys - t.rest;
+        left -= t.keys - t.rest;
+        if (share.from == share.to) continue;  // (the piece ends in the tile's first unit)
         const int32_t all = max(0, r.base + r.n);
         const int32_t most = max(0, min(r.base + t.first + t.n, all));
         u32x4 q[2][kSteps];
@@ -613,7 +607,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                                   ? max(0, min(r.base + t.first + 64 * wave / t.heads + 1, all)) : 0;
         f32x16 o[2][kCols], sa[2], sb[2];
         u32x4 pa[2][2], pb[2][2];
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, top[2];
+        // m and m c; the score above which m follows; sums of weights; the highest of the last scores (this lane's)
+        float m[2] = {-INFINITY, -INFINITY}, mc[2] = {0.f, 0.f}, bound[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, top[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
 #pragma unroll
@@ -621,75 +616,76 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) pa[b][i] = u32x4{0, 0, 0, 0};
         }
-        global_u16 *kh = (global_u16 *)(a.k + (int64_t)t.head * a.head_stride);
-        global_u16 *vh = (global_u16 *)(a.v + (int64_t)t.head * a.head_stride);
-        const int32_t *pages = a.table + r.slot * a.table_stride;
+        global_u16 *const kh = (global_u16 *)(a.k + (int64_t)t.head * a.head_stride);
+        global_u16 *const vh = (global_u16 *)(a.v + (int64_t)t.head * a.head_stride);
+        const int32_t *const pages = a.table + r.slot * a.table_stride;
+        int32_t clear = least;  // keys that need no look at the mask; 0 once a page number is bad
 
-        // A unit's keys, one per lane: its page, and where its vectors lie (-1: in no page).  Keys past
-        // the last one that the tile sees stand for it.
-        auto key_of = [&](int32_t unit) { return min(unit * kWideKeys + lane, most - 1); };
-        auto page_of = [&](int32_t unit) { return pages[key_of(unit) >> a.shift]; };
-        auto place_of = [&](int32_t unit, int32_t page) -> int64_t {
-            return (uint32_t)page < (uint32_t)a.pages
-                       ? (int64_t)page * a.page_stride + (int64_t)(key_of(unit) & place) * a.token_stride : -1;
+        // A unit's keys, one per lane; those past the last one that the tile sees stand for it.  `id`: the
+        // pages they lie in.
+        auto key_of = [&](int32_t k0) { return min(k0 + lane, most - 1); };
+        auto page_of = [&](int32_t k0) { return pages[(uint32_t)key_of(k0) >> a.shift]; };
+        // where the keys lie, in elements
+        auto place_of = [&](int32_t k0, int32_t id) -> uint64_t {
+            const bool is = (uint32_t)id < (uint32_t)a.pages;
+            if (!__all(is)) clear = 0;
+            const uint32_t in = (uint32_t)key_of(k0) & place;
+            if constexpr (kRuns)
+                return (uint64_t)(is ? id : 0) * (uint32_t)a.page_stride + (in & ~15u) * (uint32_t)a.token_stride;
+            else
+                return (uint64_t)(is ? id : 0) * (uint64_t)a.page_stride + in * (uint64_t)a.token_stride;
         };
         u32x4 k_in[kLoads], v_in[kLoads];
-        auto load_k = [&](int64_t where) {
+        // this lane's pieces of a unit's K (or V)
+        auto load = [&](global_u16 *from, uint64_t at, u32x4 (&in)[kLoads]) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int at = i * kThreads + threadIdx.x, d = 8 * (at % kPieces);
-                const int64_t off = __shfl(where, at / kPieces);
-                k_in[i] = *(global_u32x4 *)(kh + max(off, (int64_t)0) + (d < a.dim ? d : 0));
+                if constexpr (kRuns) {
+                    const int j = kApart * i + (kApart > 16 ? wave / 2 * 16 : 0);  // the 16 keys' first
+                    const uint64_t begin = (uint32_t)__builtin_amdgcn_readlane((uint32_t)at, j) |
+                                           (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(at >> 32), j) << 32;
+                    in[i] = *(global_u32x4 *)(from + begin + in_run);
+                } else {
+                    in[i] = *(global_u32x4 *)(from + __shfl(at, kApart * i + key) + (8 * mine < a.dim ? 8 * mine : 0));
+                }
             }
         };
-        auto load_v = [&](int64_t where) {
+        auto store_k = [&](int buf) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int at = i * kThreads + threadIdx.x, d = 8 * (at % kPieces);
-                const int64_t off = __shfl(where, at / kPieces);
-                v_in[i] = *(global_u32x4 *)(off < 0 ? zeros() : vh + off + (d < a.dim ? d : 0));
-            }
+            for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4 *>(k_write + buf * kKUnit + i * kApart * kKStride) = k_in[i];
         };
-        auto store_k = [&](uint32_t buf) {
+        // V of keys that no query sees or that lie in no page: zeros (their weights are zero, and what
+        // lies there may be anything)
+        auto store_v = [&](int buf, int32_t k0, int32_t id) {
+            if (k0 + kWideKeys > most || clear == 0) {
+                asm volatile("");
+                const uint64_t ok = __ballot((uint32_t)id < (uint32_t)a.pages);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const uint32_t at = i * kThreads + threadIdx.x, key = at / kPieces;
-                *reinterpret_cast<u32x4 *>(kbuf + buf + key * DP + 8 * k_at(key, at % kPieces)) = k_in[i];
+                for (int i = 0; i < kLoads; ++i) {
+                    const int j = kApart * i + key;
+                    if (k0 + j >= most || !(ok >> j & 1)) v_in[i] = u32x4{0, 0, 0, 0};
+                }
             }
-        };
-        auto store_v = [&](uint32_t buf) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const uint32_t at = i * kThreads + threadIdx.x, key = at / kPieces;
-                *reinterpret_cast<u32x4 *>(vbuf + buf + key * DP + 8 * v_at(key, at % kPieces)) = v_in[i];
-            }
+            for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4 *>(v_write + buf * kVUnit + i * kApart * kVStride) = v_in[i];
         };
-        auto read_k = [&](uint32_t at, int s) { return *reinterpret_cast<const u32x4 *>(kbuf + at + k_read[s]); };
-        auto read_v = [&](uint32_t at, int d, int i) -> u32x4 {  // keys 16 i + 4 half + (0..3, 8..11)
+        auto read_k = [&](const uint16_t *at, int s) { return *reinterpret_cast<const u32x4 *>(at + 16 * s); };
+        auto read_v = [&](const uint16_t *at, int d, int i) -> u32x4 {  // keys 16 i + 4 half + (0..3, 8..11)
             typedef __attribute__((address_space(3))) i16x4 lds;
-            const uint16_t *from = vbuf + at + v_read[d] + 16 * i * DP;
+            const uint16_t *from = at + 32 * d + 16 * i * kVStride;
             const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)from));
-            const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + 8 * DP)));
+            const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds *)(from + 8 * kVStride)));
             return u32x4{x[0], x[1], y[0], y[1]};
         };
+        auto k_half = [&](int buf, int h) { return k_read + buf * kKUnit + h * 32 * kKStride; };
+        auto v_half = [&](int buf, int h) { return v_read + buf * kVUnit + h * 32 * kVStride; };
         auto highest = [&](const f32x16 &s) {
             float x = s[0];
 #pragma unroll
             for (int i = 1; i < 15; i += 2) x = fmaxf(fmaxf(x, s[i]), s[i + 1]);
-            x = fmaxf(x, s[15]);
-            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-            return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+            return fmaxf(x, s[15]);
         };
-        auto scores = [&](uint32_t at, f32x16 (&s)[2]) {
-            s[0] = s[1] = f32x16{};
-#pragma unroll
-            for (int d = 0; d < kSteps; ++d) {
-                const u32x4 k = read_k(at, d);
-                s[0] = mfma32<kHalf>(k, q[0][d], s[0]);
-                s[1] = mfma32<kHalf>(k, q[1][d], s[1]);
-            }
-        };
-        auto gather = [&](uint32_t at, const u32x4 (&w)[2][2]) {
+        auto gather = [&](const uint16_t *at, const u32x4 (&w)[2][2]) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -699,33 +695,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                     o[1][d] = mfma32<kHalf>(v, w[1][i], o[1][d]);
                 }
         };
-        // scores of the half unit at key k0: those not seen are -inf
-        auto settle = [&](int32_t k0, uint32_t ok, f32x16 (&s)[2]) {
-            if (k0 + 32 > least || ~ok) {
+        // scores of the half unit h at key k0, of a unit in pages `id`: those not seen are -inf
+        auto settle = [&](int32_t k0, int h, int32_t id, f32x16 (&s)[2]) {
+            if (k0 + 32 > clear) {
                 asm volatile("");  // a branch, not selections in every turn
+                const uint32_t ok = (uint32_t)(__ballot((uint32_t)id < (uint32_t)a.pages) >> 32 * h);
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const int32_t rest = seen[b] - k0 - 4 * half;
                     const uint32_t have = ok >> 4 * half;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int key = 8 * (i / 4) + i % 4;
-                        if (key >= rest || !(have >> key & 1)) s[b][i] = -INFINITY;
+                        const int x = 8 * (i / 4) + i % 4;
+                        if (x >= rest || !(have >> x & 1)) s[b][i] = -INFINITY;
                     }
                     top[b] = highest(s[b]);
                 }
             }
         };
         // m follows when it lags too far; the weights w, which are under the old one, go to O first
-        auto follow = [&](uint32_t at, u32x4 (&w)[2][2]) {
-            if (__any((top[0] - m[0]) * c > kLag || (top[1] - m[1]) * c > kLag)) {
+        auto follow = [&](const uint16_t *at, u32x4 (&w)[2][2]) {
+            if (__any(top[0] > bound[0] || top[1] > bound[1])) {
                 asm volatile("");
                 gather(at, w);
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const float now = fmaxf(m[b], top[b]);
+                    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[b]), __float_as_uint(top[b]), false, false);
+                    const float now = fmaxf(m[b], fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
                     const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
                     m[b] = now;
+                    bound[b] = now + kLag / c;
+                    mc[b] = now == -INFINITY ? 0.f : now * c;
                     l[b] *= keep;
 #pragma unroll
                     for (int d = 0; d < kCols; ++d) o[b][d] *= keep;
@@ -736,11 +736,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         // One half unit: its weights from s into w, the next scores into s1, the last weights w0 into O.
         // A step is the two products with one fragment of K or V, the reads of a fragment further on, and
         // a share of the softmax; the compiler keeps to the steps' order, which feeds the matrix unit.
-        auto stage = [&](const f32x16 (&s)[2], u32x4 (&w)[2][2], uint32_t k, f32x16 (&s1)[2], uint32_t v,
+        auto stage = [&](const f32x16 (&s)[2], u32x4 (&w)[2][2], const uint16_t *k, f32x16 (&s1)[2], const uint16_t *v,
                          const u32x4 (&w0)[2][2]) {
             constexpr int kFrags = kSteps + 2 * kCols, kAhead = 2, kEach = 32 / kFrags;
             constexpr int kTop = (16 + kFrags - kSteps - 2) / (kFrags - kSteps - 1);  // scores looked at in a step
-            const float mc[2] = {m[0] == -INFINITY ? 0.f : m[0] * c, m[1] == -INFINITY ? 0.f : m[1] * c};
             u32x4 frag[kAhead + 1];
             auto fetch = [&](int f) {
                 frag[f % (kAhead + 1)] = f < kSteps ? read_k(k, f) : read_v(v, (f - kSteps) % kCols, (f - kSteps) / kCols);
@@ -786,64 +785,64 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[b]), __float_as_uint(top[b]), false, false);
-                top[b] = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
-            }
         };
 
-        const int32_t u0 = (int32_t)t.done, u1 = (int32_t)(u0 + take);
-        if (u0 * kWideKeys < most) {
-            int32_t page0 = page_of(u0), page1 = page_of(u0 + 1), page2 = page_of(u0 + 2);
-            int64_t where = place_of(u0, page0);
-            uint64_t ok = __ballot(where >= 0);  // keys of unit u, of the one after it, that lie in a page
-            load_k(where);
-            load_v(where);
-            int64_t v_where = place_of(u0 + 1, page1);
-            uint64_t ok1 = __ballot(v_where >= 0);
+        const int32_t k0 = share.from * kWideKeys, k1 = share.to * kWideKeys;
+        if (k0 < most) {
+            // the pages of the unit at hand and of those after it, and where they lie
+            int32_t id0 = page_of(k0), id1 = page_of(k0 + kWideKeys), id2 = page_of(k0 + 2 * kWideKeys), id3 = 0;
+            const uint64_t at = place_of(k0, id0);
+            load(kh, at, k_in);
+            load(vh, at, v_in);
+            uint64_t at1 = place_of(k0 + kWideKeys, id1);
             __syncthreads();  // the last tile is done with the buffers
             store_k(0);
-            store_v(0);
-            load_k(v_where);
+            store_v(0, k0, id0);
+            load(kh, at1, k_in);
             // the half unit before the first has weights of zero and a V of zeros
 #pragma unroll
-            for (int i = 0; i < 32 * DP / 8 / kThreads; ++i)
-                *reinterpret_cast<u32x4 *>(vbuf + kUnit + 32 * DP + 8 * (i * kThreads + threadIdx.x)) = u32x4{0, 0, 0, 0};
-            store_k(kUnit);
+            for (int i = 0; i < kLoads; ++i)
+                *reinterpret_cast<u32x4 *>(v_write + kVUnit + i * kApart * kVStride) = u32x4{0, 0, 0, 0};
+            store_k(1);
             __syncthreads();
-            scores(0, sa);
+#pragma unroll
+            for (int f = 0; f < kSteps; ++f) {
+                const u32x4 x = read_k(k_half(0, 0), f);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) sa[b] = mfma32<kHalf>(x, q[b][f], f == 0 ? f32x16{} : sa[b]);
+            }
 #pragma unroll
             for (int b = 0; b < 2; ++b) top[b] = highest(sa[b]);
-            settle(u0 * kWideKeys, (uint32_t)ok, sa);
-            m[0] = top[0];
-            m[1] = top[1];
-            uint32_t x = 0;  // of unit u's buffers
-            for (int32_t u = u0; u < u1; ++u) {
-                const uint32_t y = kUnit - x;
-                const int64_t k_where = place_of(u + 2, page2);
-                load_k(k_where);
-                load_v(v_where);
-                page2 = page_of(u + 3);
-                stage(sa, pb, x + 32 * DP, sb, y + 32 * DP, pa);
-                settle(u * kWideKeys + 32, (uint32_t)(ok >> 32), sb);
+            settle(k0, 0, id0, sa);
+            follow(v_half(1, 1), pa);
+            // The unit at key k, whose buffers are number x.  The next one's K is in the others, its V and the K of
+            // the one after it are on their way.
+            int x = 0;
+            for (int32_t k = k0; k < k1; k += kWideKeys) {
+                const uint64_t at2 = place_of(k + 2 * kWideKeys, id2);
+                load(kh, at2, k_in);
+                load(vh, at1, v_in);
+                id3 = page_of(k + 3 * kWideKeys);
+                stage(sa, pb, k_half(x, 1), sb, v_half(x ^ 1, 1), pa);
+                settle(k + 32, 1, id0, sb);
                 __syncthreads();  // the next unit's K and this one's V are there, the buffers behind them free
-                follow(x, pb);
-                v_where = k_where;
-                ok = ok1;
-                ok1 = __ballot(k_where >= 0);
-                stage(sb, pa, y, sa, x, pb);
-                settle(u * kWideKeys + 64, (uint32_t)ok, sa);
-                if (u + 1 < u1) follow(x + 32 * DP, pa);
-                store_k(x);  // unit u + 2
-                store_v(y);  // unit u + 1
-                x = y;
+                follow(v_half(x, 0), pb);
+                stage(sb, pa, k_half(x ^ 1, 0), sa, v_half(x, 0), pb);
+                settle(k + 64, 0, id1, sa);
+                if (k + kWideKeys < k1) follow(v_half(x, 1), pa);
+                store_k(x);                          // of the unit at k + 2 kWideKeys
+                store_v(x ^ 1, k + kWideKeys, id1);  // of the one at k + kWideKeys
+                id0 = id1;
+                id1 = id2;
+                id2 = id3;
+                at1 = at2;
+                x ^= 1;
             }
-            gather(kUnit - x + 32 * DP, pa);
+            gather(v_half(x ^ 1, 1), pa);
         }
         // o[b][d][i] is dimension 32 d + 8 (i / 4) + 4 half + i % 4 of query `col`
-        const bool whole = take == t.units;
-        const int64_t at = 2 * block + (t.done == 0);
+        const bool whole = share.to - share.from == share.all;
+        const int64_t at = 2 * block + (share.from == 0);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[b]), __float_as_uint(l[b]), false, false);
@@ -881,8 +880,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                 }
             }
         }
-        p.rest += take;
-        left -= take;
     }
 }
 
@@ -899,10 +896,10 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     __shared__ float part_l[kGroups];
     const int64_t cut = blockIdx.x + 1;
     const Cut t = a.cuts[cut];
-    if (t.done == 0 || t.done > t.piece) return;  // between two tiles, or not the tile's first cut
+    if (!t.is) return;
     const int row0 = blockIdx.y * kJoin, row1 = min(row0 + kJoin, t.n * t.heads);
     if (row0 >= row1) return;
-    const int64_t last = cut + (t.units - t.done - 1) / t.piece;  // the block with the tile's end
+    const int64_t last = cut + t.more;  // the block with the tile's end
     const float c = a.scale * kLog2e;
     const float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP;
     const int lane = threadIdx.x % kLanes, g = threadIdx.x / kLanes;
@@ -973,6 +970,7 @@ struct Shape {
     int blocks, row_waves;  // of k_attend_narrow; 256 rows are k_attend_wide's
     int grid;
     int rows() const { return 16 * blocks * row_waves; }
+    int keys() const { return rows() == kWideRows ? kWideKeys : 32 * (4 / row_waves); }
 };
 
 Shape shape_of(const tam_chunk &c, int64_t heads) {
@@ -1004,7 +1002,11 @@ hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
     if (sh.rows() == 32) return launch_narrow<DP, 2, 1, kHalf>(a, s);
     if (sh.rows() == 64) return launch_narrow<DP, 2, 2, kHalf>(a, s);
     if (sh.rows() == 128) return launch_narrow<DP, 2, 4, kHalf>(a, s);
-    hipLaunchKernelGGL((k_attend_wide<DP, kHalf>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
+    constexpr size_t kLds = 2 * kWideKeys * (DP + 8 + DP + 16) * sizeof(uint16_t);
+    if (a.shift >= 4 && a.page_stride <= INT32_MAX && (a.token_stride << a.shift) <= INT32_MAX)
+        hipLaunchKernelGGL((k_attend_wide<DP, kHalf, true>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
+    else
+        hipLaunchKernelGGL((k_attend_wide<DP, kHalf, false>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((k_join<DP, kWideRows, 32, kHalf>), dim3((unsigned)a.blocks - 1, kWideRows / 32),
@@ -1032,7 +1034,7 @@ hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipSt
     a.parts = (int32_t)((group + a.group - 1) / a.group);
     a.tq = sh.rows() / a.group;
     a.blocks = sh.grid;
-    a.least = 1;
+    a.unit = sh.keys();
     a.sums = static_cast<float *>(work);
     a.cuts = reinterpret_cast<Cut *>(a.sums + 2 * (int64_t)sh.grid * sh.rows() * (padded(c.head_dim) + 2));
     const bool half = c.dtype == TAM_DTYPE_FP16;
