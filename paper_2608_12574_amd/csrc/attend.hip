@@ -636,28 +636,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                 return (uint64_t)(is ? id : 0) * (uint64_t)a.page_stride + in * (uint64_t)a.token_stride;
         };
         u32x4 k_in[kLoads], v_in[kLoads];
-        // this lane's pieces of a unit's K (or V)
-        auto load = [&](global_u16 *from, uint64_t at, u32x4 (&in)[kLoads]) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if constexpr (kRuns) {
-                    const int j = kApart * i + (kApart > 16 ? wave / 2 * 16 : 0);  // the 16 keys' first
-                    const uint64_t begin = (uint32_t)__builtin_amdgcn_readlane((uint32_t)at, j) |
-                                           (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(at >> 32), j) << 32;
-                    in[i] = *(global_u32x4 *)(from + begin + in_run);
-                } else {
-                    in[i] = *(global_u32x4 *)(from + __shfl(at, kApart * i + key) + (8 * mine < a.dim ? 8 * mine : 0));
-                }
+        // piece i of this lane's share of a unit's K (or V)
+        auto load = [&](global_u16 *from, uint64_t at, int i) -> u32x4 {
+            if constexpr (kRuns) {
+                const int j = kApart * i + (kApart > 16 ? wave / 2 * 16 : 0);  // the 16 keys' first
+                const uint64_t begin = (uint32_t)__builtin_amdgcn_readlane((uint32_t)at, j) |
+                                       (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(at >> 32), j) << 32;
+                return *(global_u32x4 *)(from + begin + in_run);
+            } else {
+                return *(global_u32x4 *)(from + __shfl(at, kApart * i + key) + (8 * mine < a.dim ? 8 * mine : 0));
             }
         };
-        auto store_k = [&](int buf) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4 *>(k_write + buf * kKUnit + i * kApart * kKStride) = k_in[i];
+        auto store_k = [&](int buf, int i) {
+            *reinterpret_cast<u32x4 *>(k_write + buf * kKUnit + i * kApart * kKStride) = k_in[i];
+        };
+        auto store_v = [&](int buf, int i) {
+            *reinterpret_cast<u32x4 *>(v_write + buf * kVUnit + i * kApart * kVStride) = v_in[i];
         };
         // V of keys that no query sees or that lie in no page: zeros (their weights are zero, and what
         // lies there may be anything)
-        auto store_v = [&](int buf, int32_t k0, int32_t id) {
-            if (k0 + kWideKeys > most || clear == 0) {
+        auto clean = [&](int32_t k0, int32_t id) {
+            if (__builtin_expect(k0 + kWideKeys > most || clear == 0, 0)) {
                 asm volatile("");
                 const uint64_t ok = __ballot((uint32_t)id < (uint32_t)a.pages);
 #pragma unroll
@@ -666,8 +665,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                     if (k0 + j >= most || !(ok >> j & 1)) v_in[i] = u32x4{0, 0, 0, 0};
                 }
             }
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) *reinterpret_cast<u32x4 *>(v_write + buf * kVUnit + i * kApart * kVStride) = v_in[i];
         };
         auto read_k = [&](const uint16_t *at, int s) { return *reinterpret_cast<const u32x4 *>(at + 16 * s); };
         auto read_v = [&](const uint16_t *at, int d, int i) -> u32x4 {  // keys 16 i + 4 half + (0..3, 8..11)
@@ -697,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         };
         // scores of the half unit h at key k0, of a unit in pages `id`: those not seen are -inf
         auto settle = [&](int32_t k0, int h, int32_t id, f32x16 (&s)[2]) {
-            if (k0 + 32 > clear) {
+            if (__builtin_expect(k0 + 32 > clear, 0)) {
                 asm volatile("");  // a branch, not selections in every turn
                 const uint32_t ok = (uint32_t)(__ballot((uint32_t)id < (uint32_t)a.pages) >> 32 * h);
 #pragma unroll
@@ -715,7 +712,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         };
         // m follows when it lags too far; the weights w, which are under the old one, go to O first
         auto follow = [&](const uint16_t *at, u32x4 (&w)[2][2]) {
-            if (__any(top[0] > bound[0] || top[1] > bound[1])) {
+            if (__builtin_expect(__any(top[0] > bound[0] || top[1] > bound[1]), 0)) {
                 asm volatile("");
                 gather(at, w);
 #pragma unroll
@@ -735,10 +732,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         };
         // One half unit: its weights from s into w, the next scores into s1, the last weights w0 into O.
         // A step is the two products with one fragment of K or V, the reads of a fragment further on, and
-        // a share of the softmax; the compiler keeps to the steps' order, which feeds the matrix unit.
+        // a share of the softmax and of `more`; the compiler keeps to the steps' order, which feeds the matrix
+        // unit.  The first weights come before the first fragment has been read.
         auto stage = [&](const f32x16 (&s)[2], u32x4 (&w)[2][2], const uint16_t *k, f32x16 (&s1)[2], const uint16_t *v,
-                         const u32x4 (&w0)[2][2]) {
-            constexpr int kFrags = kSteps + 2 * kCols, kAhead = 2, kEach = 32 / kFrags;
+                         const u32x4 (&w0)[2][2], auto more) {
+            constexpr int kFrags = kSteps + 2 * kCols, kAhead = 2, kEach = 32 / kFrags, kFirst = 2 * kEach;
             constexpr int kTop = (16 + kFrags - kSteps - 2) / (kFrags - kSteps - 1);  // scores looked at in a step
             u32x4 frag[kAhead + 1];
             auto fetch = [&](int f) {
@@ -768,14 +766,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
 #pragma unroll
             for (int f = 0; f < kAhead; ++f) fetch(f);
 #pragma unroll
+            for (int e = 0; e < kFirst; ++e) weigh(e);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
             for (int f = 0; f < kFrags; ++f) {
                 if (f + kAhead < kFrags) fetch(f + kAhead);
-#pragma unroll
-                for (int e = 0; e < kEach / 2; ++e) weigh(kEach * f + e);
                 multiply(f, 0);
 #pragma unroll
-                for (int e = kEach / 2; e < kEach; ++e) weigh(kEach * f + e);
+                for (int e = kFirst + kEach * f; e < min(32, kFirst + kEach * (f + 1)); ++e) weigh(e);
                 multiply(f, 1);
+                more(f);
                 if (f > kSteps) {
 #pragma unroll
                     for (int b = 0; b < 2; ++b)
@@ -789,21 +789,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
 
         const int32_t k0 = share.from * kWideKeys, k1 = share.to * kWideKeys;
         if (k0 < most) {
-            // the pages of the unit at hand and of those after it, and where they lie
+            // the pages of the unit at hand and of those after it
             int32_t id0 = page_of(k0), id1 = page_of(k0 + kWideKeys), id2 = page_of(k0 + 2 * kWideKeys), id3 = 0;
-            const uint64_t at = place_of(k0, id0);
-            load(kh, at, k_in);
-            load(vh, at, v_in);
+            const uint64_t at0 = place_of(k0, id0);
             uint64_t at1 = place_of(k0 + kWideKeys, id1);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) k_in[i] = load(kh, at0, i);
             __syncthreads();  // the last tile is done with the buffers
-            store_k(0);
-            store_v(0, k0, id0);
-            load(kh, at1, k_in);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) store_k(0, i);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) k_in[i] = load(kh, at1, i), v_in[i] = load(vh, at0, i);
             // the half unit before the first has weights of zero and a V of zeros
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
                 *reinterpret_cast<u32x4 *>(v_write + kVUnit + i * kApart * kVStride) = u32x4{0, 0, 0, 0};
-            store_k(1);
             __syncthreads();
 #pragma unroll
             for (int f = 0; f < kSteps; ++f) {
@@ -815,23 +815,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
             for (int b = 0; b < 2; ++b) top[b] = highest(sa[b]);
             settle(k0, 0, id0, sa);
             follow(v_half(1, 1), pa);
-            // The unit at key k, whose buffers are number x.  The next one's K is in the others, its V and the K of
-            // the one after it are on their way.
-            int x = 0;
+            int x = 0;  // the unit's buffers
             for (int32_t k = k0; k < k1; k += kWideKeys) {
+                // This unit's V and the next one's K have been loaded, and go to LDS; the next V and the K of
+                // the unit after it set out.
                 const uint64_t at2 = place_of(k + 2 * kWideKeys, id2);
-                load(kh, at2, k_in);
-                load(vh, at1, v_in);
                 id3 = page_of(k + 3 * kWideKeys);
-                stage(sa, pb, k_half(x, 1), sb, v_half(x ^ 1, 1), pa);
+                clean(k, id0);
+                stage(sa, pb, k_half(x, 1), sb, v_half(x ^ 1, 1), pa, [&](int f) {
+                    const int i = f / 4;
+                    if (f % 4 == 0) {
+                        store_k(x ^ 1, i);
+                        k_in[i] = load(kh, at2, i);
+                    } else if (f % 4 == 2) {
+                        store_v(x, i);
+                        v_in[i] = load(vh, at1, i);
+                    }
+                });
                 settle(k + 32, 1, id0, sb);
-                __syncthreads();  // the next unit's K and this one's V are there, the buffers behind them free
+                __syncthreads();
                 follow(v_half(x, 0), pb);
-                stage(sb, pa, k_half(x ^ 1, 0), sa, v_half(x, 0), pb);
+                stage(sb, pa, k_half(x ^ 1, 0), sa, v_half(x, 0), pb, [](int) {});
                 settle(k + 64, 0, id1, sa);
                 if (k + kWideKeys < k1) follow(v_half(x, 1), pa);
-                store_k(x);                          // of the unit at k + 2 kWideKeys
-                store_v(x ^ 1, k + kWideKeys, id1);  // of the one at k + kWideKeys
                 id0 = id1;
                 id1 = id2;
                 id2 = id3;
