@@ -12,7 +12,8 @@
 // A unit is a tile's product with kKeys keys.  The keys that the tiles of a call see, row
 // after row, head after head, tile after tile, are one line, cut into equal pieces for as
 // many blocks as the chip holds: any mix of long and short rows and chunks fills
-// it evenly.  A cut inside a tile moves back to the unit it falls in; the tile's parts
+// it evenly.  A tile begins with `extra` keys that stand for its own cost (queries, first
+// reads, output).  A cut inside a tile moves back to the unit it falls in; the tile's parts
 // leave partial sums in the scratch, which k_join adds up.  The lengths lie on the
 // device: each block finds its piece from them by a prefix sum over the rows.
 #include <hip/hip_runtime.h>
@@ -55,7 +56,7 @@ struct Attend {
     float scale;
     // the cut: tiles of `tq` tokens by `group` heads, `parts` of them per K/V head
     int32_t tq, group, parts, blocks;
-    int32_t unit;   // keys of a unit, a power of two
+    int32_t unit, extra;  // keys of a unit, a power of two; keys that stand for a tile's own cost
     float *sums;    // [2 blocks][tile rows][DP] partial sums, then [2 blocks][tile rows][2] their m and sum of weights
     struct Cut *cuts;  // [blocks] what each block's piece begins with
 };
@@ -110,13 +111,13 @@ __device__ inline Row shared_row(const Attend &a, int64_t i) {
 
 // Keys on the line before tile t of a row and head: tile i < t sees base + (i + 1) tq.
 __device__ inline int64_t keys_before(const Attend &a, const Row &r, int64_t t) {
-    return t * max(r.base, 0) + a.tq * (t * (t + 1) / 2);
+    return t * (max(r.base, 0) + a.extra) + a.tq * (t * (t + 1) / 2);
 }
 
 // Keys on the line of a row and head.  A row of one tile takes whole units, so that a
 // batch of them is cut between units.
 __device__ inline int64_t row_keys(const Attend &a, const Row &r) {
-    const int64_t all = max(r.base, 0) + r.n;
+    const int64_t all = (int64_t)max(r.base, 0) + r.n + a.extra;
     if (r.n <= a.tq) return r.n ? (all + a.unit - 1) & -(int64_t)a.unit : 0;
     return keys_before(a, r, (r.n - 1) / a.tq) + all;
 }
@@ -178,7 +179,7 @@ struct Tile {
     int32_t head, part, tile;     // K/V head and part of its group; number in the row
     int32_t first, n;             // its first token in the chunk, and its tokens
     int32_t heads;                // query heads of the part
-    int64_t rest, keys;           // keys of it before the place, and all that it sees
+    int64_t rest, keys;           // keys of it on the line before the place, and all of them
 };
 
 __device__ inline Tile tile_at(const Attend &a, const Row &r, int64_t rest) {
@@ -199,7 +200,7 @@ __device__ inline Tile tile_at(const Attend &a, const Row &r, int64_t rest) {
     t.n = min(a.tq, r.n - t.first);
     t.heads = min(a.group, a.heads / a.kv_heads - t.part * a.group);
     t.rest = rest - keys_before(a, r, lo);
-    t.keys = r.n <= a.tq ? u : max(r.base, 0) + t.first + t.n;
+    t.keys = r.n <= a.tq ? u : (int64_t)max(r.base, 0) + t.first + t.n + a.extra;
     return t;
 }
 
@@ -209,11 +210,12 @@ struct Share {
 };
 
 template <int kKeys>
-__device__ inline Share share_of(const Tile &t, int64_t left) {
+__device__ inline Share share_of(const Attend &a, const Tile &t, int64_t left) {
+    auto unit = [&](int64_t at) { return (int32_t)(max(at - a.extra, (int64_t)0) / kKeys); };
     Share s;
-    s.all = (int32_t)((t.keys + kKeys - 1) / kKeys);
-    s.from = (int32_t)(t.rest / kKeys);
-    s.to = left >= t.keys - t.rest ? s.all : (int32_t)((t.rest + left) / kKeys);
+    s.all = unit(t.keys + kKeys - 1);
+    s.from = unit(t.rest);
+    s.to = left >= t.keys - t.rest ? s.all : unit(t.rest + left);
     return s;
 }
 
@@ -221,7 +223,7 @@ __device__ inline Share share_of(const Tile &t, int64_t left) {
 template <int kKeys>
 __device__ inline void note(const Attend &a, int64_t block, const Row &r, const Tile &t, int64_t piece) {
     if (threadIdx.x == 0)
-        a.cuts[block] = Cut{t.rest >= kKeys && t.rest - piece < kKeys, (int32_t)((t.keys - t.rest - 1) / piece),
+        a.cuts[block] = Cut{t.rest - a.extra >= kKeys && t.rest - a.extra - piece < kKeys, (int32_t)((t.keys - t.rest - 1) / piece),
                             r.first + t.first, t.n, t.head * (a.heads / a.kv_heads) + t.part * a.group, t.heads};
 }
 
@@ -294,11 +296,11 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
             continue;
         }
         const Tile t = tile_at(a, r, p.rest);
-        const Share share = share_of<kKeys>(t, left);
+        const Share share = share_of<kKeys>(a, t, left);
         if (left == whole_piece) note<kKeys>(a, blockIdx.x, r, t, piece);
         p.rest += t.keys - t.rest;
         left -= t.keys - t.rest;
-        if (share.from == share.to) continue;  // (the piece ends in the tile's first unit)
+        if (share.from == share.to) continue;  // (the piece ends before the next unit)
         // queries, one per lane of 16 and block; rows past the tile's see no key.  Lanes
         // past the last dimension read others of the vector (queries: zero).
         u32x4 q[kBlocks][kSteps];
@@ -580,11 +582,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
             continue;
         }
         const Tile t = tile_at(a, r, p.rest);
-        const Share share = share_of<kWideKeys>(t, left);
+        const Share share = share_of<kWideKeys>(a, t, left);
         if (left == whole_piece) note<kWideKeys>(a, block, r, t, piece);
         p.rest += t.keys - t.rest;
         left -= t.keys - t.rest;
-        if (share.from == share.to) continue;  // (the piece ends in the tile's first unit)
+        if (share.from == share.to) continue;  // (the piece ends before the next unit)
         const int32_t all = max(0, r.base + r.n);
         const int32_t most = max(0, min(r.base + t.first + t.n, all));
         u32x4 q[2][kSteps];
@@ -976,6 +978,7 @@ struct Shape {
     int blocks, row_waves;  // of k_attend_narrow; 256 rows are k_attend_wide's
     int grid;
     int rows() const { return 16 * blocks * row_waves; }
+    int extra() const { return rows() == kWideRows ? 5 * kWideKeys : keys(); }
     int keys() const { return rows() == kWideRows ? kWideKeys : 32 * (4 / row_waves); }
 };
 
@@ -1035,12 +1038,13 @@ hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipSt
              c.head_stride, c.token_stride, q.q_token, q.q_head, q.out_token, q.out_head, c.table, c.length,
              c.offsets, c.slot_ids, c.table_stride, c.slots, c.max_pages, c.rows, c.tokens, (int32_t)c.num_pages,
              __builtin_ctzll((unsigned long long)c.page_tokens), (int32_t)q.heads, (int32_t)c.kv_heads,
-             (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, nullptr, nullptr};
+             (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, 0, nullptr, nullptr};
     a.group = (int32_t)std::min<int64_t>(group, sh.rows());
     a.parts = (int32_t)((group + a.group - 1) / a.group);
     a.tq = sh.rows() / a.group;
     a.blocks = sh.grid;
     a.unit = sh.keys();
+    a.extra = sh.extra();
     a.sums = static_cast<float *>(work);
     a.cuts = reinterpret_cast<Cut *>(a.sums + 2 * (int64_t)sh.grid * sh.rows() * (padded(c.head_dim) + 2));
     const bool half = c.dtype == TAM_DTYPE_FP16;
