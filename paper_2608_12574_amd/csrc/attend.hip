@@ -37,13 +37,10 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kWave = 64;
 constexpr int kThreads = 256;
 
-// Bad page numbers point here: V of zeros.  (Addresses of memory are told from those of LDS
-// here, so that a load does not wait as if it could be of either.)
-__device__ u32x4 kZeros[16];
+// Memory's addresses, told from LDS's, so that a load does not wait as if it could be of either.
 typedef __attribute__((address_space(1))) const uint16_t global_u16;
 typedef __attribute__((address_space(1))) const u32x4 global_u32x4;
 typedef __attribute__((address_space(1))) const u32x2 global_u32x2;
-__device__ inline global_u16 *zeros() { return (global_u16 *)kZeros; }
 
 struct Attend {
     const uint16_t *k, *v, *q;
@@ -259,24 +256,35 @@ __device__ inline uint32_t pack(float x, float y) {  // rounded to nearest, ties
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLag = 8.f;  // m may lag by this much, in powers of two
 
-// A tile of at most 16 kBlocks kRowWaves rows by all its keys, 32 keys per wave and
-// step; kRowWaves waves share the rows and the others the keys of a unit.  The bytes of
+// In both kernels below, kRuns: 16 keys from a multiple of 16 lie side by side in one page (pages of 16
+// tokens or more, strides of 32 bits), so that its number and where they begin are the same for all lanes.
+
+// A tile of at most 16 rows by all its keys, 32 keys per wave and step.  The bytes of
 // K and V bound it, so the fragments come straight from memory into registers, the next
 // step's while this one is computed, and LDS only joins the waves' sums at the end.
 // S^T = K Q^T leaves each lane the weights of one query, for the same eight keys that it
 // then holds as the second factor of O^T = V^T P^T: no weight changes lanes.  V's columns
 // are paired in registers (v_perm).
-template <int DP, int kBlocks, int kRowWaves, bool kHalf>
-__global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narrow(Attend a) {
-    constexpr int kKeyWaves = 4 / kRowWaves, kKeys = 32 * kKeyWaves;
+constexpr int kNarrowKeys = 128;
+
+template <int DP, bool kHalf, bool kRuns>
+__global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
+    constexpr int kKeys = kNarrowKeys;
     constexpr int kSteps = DP / 32;  // products of 32 dimensions
     constexpr int kCols = DP / 16;   // dimensions per lane of 16: adjacent ones
-    constexpr int kRows = 16 * kBlocks * kRowWaves;
+    constexpr int kRows = 16;
     __shared__ float joint[4][16][DP + 4];
-    __shared__ float tops[4][16 * kBlocks], weights[4][16 * kBlocks];
+    __shared__ float tops[4][16], weights[4][16];
     const int lane = threadIdx.x % kWave, wave = uniform((int32_t)threadIdx.x / kWave);
-    const int rw = wave / kKeyWaves, kw = wave % kKeyWaves;
     const int col = lane % 16, grp = lane / 16;
+    const uint32_t place = (1u << a.shift) - 1;
+    // where a lane's parts of K and V lie in their vectors (kRuns: from their run's first); lanes past the
+    // last dimension read others of the vector
+    uint32_t k_in[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+        k_in[s] = (32 * s + 8 * grp < a.dim ? 32 * s + 8 * grp : 0) + (kRuns ? (uint32_t)col * (uint32_t)a.token_stride : 0);
+    const uint32_t v_in = (kCols * col < a.dim ? kCols * col : 0) + (kRuns ? (uint32_t)(4 * grp) * (uint32_t)a.token_stride : 0);
     int64_t piece;
     Place p = find(a, blockIdx.x, &piece);
     if (p.row < 0) {
@@ -301,231 +309,224 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
         p.rest += t.keys - t.rest;
         left -= t.keys - t.rest;
         if (share.from == share.to) continue;  // (the piece ends before the next unit)
-        // queries, one per lane of 16 and block; rows past the tile's see no key.  Lanes
-        // past the last dimension read others of the vector (queries: zero).
-        u32x4 q[kBlocks][kSteps];
-        int32_t seen[kBlocks];  // keys that the query sees
+        // queries, one per lane of 16; rows past the tile's see no key.  Lanes past the last
+        // dimension read others of the vector (queries: zero).
+        u32x4 q[kSteps];
         const int32_t all = max(0, r.base + r.n);  // tokens of the sequence, chunk included
         const int32_t most = max(0, min(r.base + t.first + t.n, all)), least = max(0, min(r.base + t.first + 1, all));
+        const int row = col, tok = row / t.heads, h = row - tok * t.heads;
+        const bool is = tok < t.n;
+        const int32_t seen = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;  // keys that the query sees
+        const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
+                              (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const int row = 16 * (kBlocks * rw + b) + col, tok = row / t.heads, h = row - tok * t.heads;
-            const bool is = tok < t.n;
-            seen[b] = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
-            const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
-                                  (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const int d = 32 * s + 8 * grp;
-                q[b][s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(src + d) : u32x4{0, 0, 0, 0};
-            }
+        for (int s = 0; s < kSteps; ++s) {
+            const int d = 32 * s + 8 * grp;
+            q[s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(src + d) : u32x4{0, 0, 0, 0};
         }
-        f32x4 o[kBlocks][kCols];
-        float m[kBlocks], l[kBlocks];
+        f32x4 o[kCols];
+        float m = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            m[b] = -INFINITY;
-            l[b] = 0.f;
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) o[b][j] = f32x4{0, 0, 0, 0};
-        }
-        global_u16 *kh = (global_u16 *)(a.k + (int64_t)t.head * a.head_stride);
-        global_u16 *vh = (global_u16 *)(a.v + (int64_t)t.head * a.head_stride + (kCols * col < a.dim ? kCols * col : 0));
-        const int32_t *pages = a.table + r.slot * a.table_stride;
-        const int32_t place = (1 << a.shift) - 1;
+        for (int j = 0; j < kCols; ++j) o[j] = f32x4{0, 0, 0, 0};
+        global_u16 *const kh = (global_u16 *)(a.k + (int64_t)t.head * a.head_stride);
+        global_u16 *const vh = (global_u16 *)(a.v + (int64_t)t.head * a.head_stride);
+        const int32_t *const pages = a.table + r.slot * a.table_stride;
+        int32_t clear = least;  // keys that need no look at the mask; 0 once a page number is bad
 
+        // A step's keys, one per lane of 32; those past the last one that the tile sees stand for it.  `id`:
+        // the pages they lie in.
+        auto key_of = [&](int32_t k0) { return min(k0 + lane % 32, most - 1); };
+        auto page_of = [&](int32_t k0) { return pages[(uint32_t)key_of(k0) >> a.shift]; };
+        auto place_of = [&](int32_t k0, int32_t id) -> uint64_t {
+            const bool ok = (uint32_t)id < (uint32_t)a.pages;
+            if (!__all(ok)) clear = 0;
+            const uint32_t in = (uint32_t)key_of(k0) & place;
+            if constexpr (kRuns)
+                return (uint64_t)(ok ? id : 0) * (uint32_t)a.page_stride + (in & ~15u) * (uint32_t)a.token_stride;
+            else
+                return (uint64_t)(ok ? id : 0) * (uint64_t)a.page_stride + in * (uint64_t)a.token_stride;
+        };
         struct Step {
             u32x4 k[2][kSteps];
             u32x4 v[8];  // kCols * 2 bytes of each are used
-            uint32_t bad;  // bit j: key j of the lane's eight lies in no page
         };
-        // The keys of a step; those past the last one that the tile sees stand for it.
-        auto load = [&](int32_t k0, Step &x) {
-            x.bad = 0;
-            global_u16 *src[8];
-            const int32_t first = k0 + 4 * grp;
-            if (k0 + 32 <= most && a.shift >= 2) {  // four keys lie side by side
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int32_t key = first + 16 * i, page = pages[key >> a.shift];
-                    const bool ok = (uint32_t)page < (uint32_t)a.pages;
-                    if (!ok) x.bad |= 15u << 4 * i;
-                    global_u16 *at = ok ? vh + (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride : zeros();
-                    const int64_t step = ok ? a.token_stride : 0;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) src[4 * i + j] = at + j * step;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int32_t key = min(first + 16 * (j / 4) + j % 4, most - 1), page = pages[key >> a.shift];
-                    const bool ok = (uint32_t)page < (uint32_t)a.pages;
-                    if (!ok) x.bad |= 1u << j;
-                    src[j] = ok ? vh + (int64_t)page * a.page_stride + (int64_t)(key & place) * a.token_stride : zeros();
-                }
-            }
+        // the fragments: K of key 16 i + col; V of the keys 16 i + 4 grp + (0..3)
+        auto load = [&](uint64_t at, Step &x) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int32_t key = min(k0 + 16 * i + col, most - 1), page = pages[key >> a.shift];
-                global_u16 *at = kh + (int64_t)((uint32_t)page < (uint32_t)a.pages ? page : 0) * a.page_stride +
-                                     (int64_t)(key & place) * a.token_stride;
+                uint64_t begin;
+                if constexpr (kRuns)
+                    begin = (uint32_t)__builtin_amdgcn_readlane((uint32_t)at, 16 * i) |
+                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(at >> 32), 16 * i) << 32;
+                else
+                    begin = __shfl(at, 16 * i + col);
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    const int d = 32 * s + 8 * grp;
-                    x.k[i][s] = *(global_u32x4 *)(at + (d < a.dim ? d : 0));
-                }
+                for (int s = 0; s < kSteps; ++s) x.k[i][s] = *(global_u32x4 *)(kh + begin + k_in[s]);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                uint64_t begin;
+                if constexpr (kRuns)
+                    begin = (uint32_t)__builtin_amdgcn_readlane((uint32_t)at, 16 * (j / 4)) |
+                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(at >> 32), 16 * (j / 4)) << 32,
+                    begin += (uint32_t)(j % 4) * (uint32_t)a.token_stride;
+                else
+                    begin = __shfl(at, 16 * (j / 4) + 4 * grp + j % 4);
+                global_u16 *src = vh + begin + v_in;
                 if constexpr (kCols == 8) {
-                    x.v[j] = *(global_u32x4 *)src[j];
+                    x.v[j] = *(global_u32x4 *)src;
                 } else {
-                    const u32x2 y = *(global_u32x2 *)src[j];
+                    const u32x2 y = *(global_u32x2 *)src;
                     x.v[j] = u32x4{y[0], y[1], 0, 0};
                 }
             }
         };
-        auto compute = [&](int32_t k0, const Step &x) {
-            u32x4 v[kCols];
-#pragma unroll
-            for (int j = 0; j < kCols; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    v[j][i] = __builtin_amdgcn_perm(x.v[2 * i + 1][j / 2], x.v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-            const bool masked = k0 + 32 > least || __any(x.bad);
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-                f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int d = 0; d < kSteps; ++d) s[i] = mfma16<kHalf>(x.k[i][d], q[b][d], s[i]);
-                if (masked) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (k0 + 16 * (j / 4) + 4 * grp + j % 4 >= seen[b] || (x.bad >> j & 1)) s[j / 4][j % 4] = -INFINITY;
-                }
-                float top = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                if (__any((top - m[b]) * c > kLag)) {  // NaN (both -inf): no
-                    const float now = fmaxf(m[b], top);
-                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
-                    m[b] = now;
-                    l[b] *= keep;
-#pragma unroll
-                    for (int j = 0; j < kCols; ++j) o[b][j] *= keep;
-                }
-                const float mc = m[b] == -INFINITY ? 0.f : m[b] * c;
-                float w[8];
+        auto compute = [&](int32_t k0, int32_t id, Step &x) {
+            uint32_t have = 0xFFFFFFFFu;  // keys of the step that lie in a page
+            if (__builtin_expect(k0 + 32 > clear, 0)) {
+                asm volatile("");
+                have = (uint32_t)__ballot((uint32_t)id < (uint32_t)a.pages);
+                // V of keys that no query sees or that lie in no page: zeros (their weights are zero, and
+                // what lies there may be anything)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j % 4], c, -mc));
-                    l[b] += w[j];
+                    const int key = 16 * (j / 4) + 4 * grp + j % 4;
+                    if (k0 + key >= most || !(have >> key & 1)) x.v[j] = u32x4{0, 0, 0, 0};
                 }
-                u32x4 pw;
+            }
+            f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pw[i] = pack<kHalf>(w[2 * i], w[2 * i + 1]);
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) o[b][j] = mfma16<kHalf>(v[j], pw, o[b][j]);
+                for (int d = 0; d < kSteps; ++d) s[i] = mfma16<kHalf>(x.k[i][d], q[d], s[i]);
+            if (__builtin_expect(k0 + 32 > clear, 0)) {
+                asm volatile("");
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int key = 16 * (j / 4) + 4 * grp + j % 4;
+                    if (k0 + key >= seen || !(have >> key & 1)) s[j / 4][j % 4] = -INFINITY;
+                }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (__any((top - m) * c > kLag)) {  // NaN (both -inf): no
+                const float now = fmaxf(m, top);
+                const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - now) * c);
+                m = now;
+                l *= keep;
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) o[j] *= keep;
+            }
+            const float mc = m == -INFINITY ? 0.f : m * c;
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j / 4][j % 4], c, -mc));
+                l += w[j];
+            }
+            u32x4 pw;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pw[i] = pack<kHalf>(w[2 * i], w[2 * i + 1]);
+            __builtin_amdgcn_sched_barrier(0);  // the columns of V are paired late, into K's registers
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) {
+                u32x4 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][j / 2], x.v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+                o[j] = mfma16<kHalf>(v, pw, o[j]);
             }
         };
         const int32_t k_end = min(share.to * kKeys, most);
-        int32_t k0 = share.from * kKeys + 32 * kw;
+        int32_t k0 = share.from * kKeys + 32 * wave;
         if (k0 < k_end) {
+            // pages two steps ahead, so that no load waits for one that was asked for after the last loads
             Step x, y;
-            load(k0, x);
+            int32_t id0 = page_of(k0), id1 = page_of(k0 + kKeys);
+            load(place_of(k0, id0), x);
             while (true) {
-                int32_t k1 = k0 + kKeys;
-                if (k1 < k_end) load(k1, y);
-                compute(k0, x);
-                if (k1 >= k_end) break;
-                k0 = k1 + kKeys;
-                if (k0 < k_end) load(k0, x);
-                compute(k1, y);
-                if (k0 >= k_end) break;
+                const int32_t id2 = page_of(k0 + 2 * kKeys);
+                if (k0 + kKeys < k_end) load(place_of(k0 + kKeys, id1), y);
+                compute(k0, id0, x);
+                if ((k0 += kKeys) >= k_end) break;
+                id0 = page_of(k0 + 2 * kKeys);
+                if (k0 + kKeys < k_end) load(place_of(k0 + kKeys, id2), x);
+                compute(k0, id1, y);
+                if ((k0 += kKeys) >= k_end) break;
+                id1 = id0;
+                id0 = id2;
             }
         }
-        // join the waves that shared the keys: the largest m, then the sums under it
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            l[b] += __shfl_xor(l[b], 16);
-            l[b] += __shfl_xor(l[b], 32);
-            if (grp == 0) {
-                tops[wave][16 * b + col] = m[b];
-                weights[wave][16 * b + col] = l[b];
-            }
+        // join the waves: the largest m, then the sums under it
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (grp == 0) {
+            tops[wave][col] = m;
+            weights[wave][col] = l;
         }
         __syncthreads();
         const bool whole = share.to - share.from == share.all;
         const int64_t at = 2 * (int64_t)blockIdx.x + (share.from == 0);  // a cut tile's partial sums
+        const float high = fmaxf(fmaxf(tops[0][col], tops[1][col]), fmaxf(tops[2][col], tops[3][col]));
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - high) * c);
+        // o[j][i] is dimension kCols (4 grp + i) + j of query `col`
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            float top = -INFINITY;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int w = 0; w < kKeyWaves; ++w) top = fmaxf(top, tops[rw * kKeyWaves + w][16 * b + col]);
-            const float keep = m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[b] - top) * c);
-            // o[b][j][i] is dimension kCols (4 grp + i) + j of query `col`
+            for (int j = 0; j < kCols; j += 4)
+                *reinterpret_cast<f32x4 *>(&joint[wave][col][kCols * (4 * grp + i) + j]) =
+                    f32x4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]} * keep;
+        __syncthreads();
+        // a thread takes a query and kCols dimensions
+        const int out_row = threadIdx.x / 16, d0 = kCols * (threadIdx.x % 16);
+        const int out_tok = out_row / t.heads, out_h = out_row - out_tok * t.heads;
+        if (out_tok < t.n) {
+            float sum[kCols] = {}, lsum = 0.f, mx = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int w = 0; w < 4; ++w) mx = fmaxf(mx, tops[w][out_row]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float mw = tops[w][out_row];
+                if (mw > -INFINITY) lsum += weights[w][out_row] * __builtin_amdgcn_exp2f((mw - mx) * c);
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) sum[j] += joint[w][out_row][d0 + j];
+            }
+            if (whole) {
+                const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+                const int64_t token = r.first + t.first + out_tok;
+                const int64_t head = t.head * (a.heads / a.kv_heads) + t.part * a.group + out_h;
+                uint16_t *dst = a.out + token * a.out_token + head * a.out_head + d0;
+                if (d0 < a.dim) {
+                    uint32_t y[kCols / 2];
+#pragma unroll
+                    for (int j = 0; j < kCols / 2; ++j) y[j] = pack<kHalf>(sum[2 * j] * inv, sum[2 * j + 1] * inv);
+                    if constexpr (kCols == 8) *reinterpret_cast<u32x4 *>(dst) = u32x4{y[0], y[1], y[2], y[3]};
+                    else *reinterpret_cast<u32x2 *>(dst) = u32x2{y[0], y[1]};
+                }
+                if (a.lse && d0 == 0) a.lse[token * a.heads + head] = lsum > 0.f ? mx * a.scale + logf(lsum) : -INFINITY;
+            } else {
+                float *dst = a.sums + (at * kRows + out_row) * DP + d0;
 #pragma unroll
                 for (int j = 0; j < kCols; j += 4)
-                    *reinterpret_cast<f32x4 *>(&joint[wave][col][kCols * (4 * grp + i) + j]) =
-                        f32x4{o[b][j][i], o[b][j + 1][i], o[b][j + 2][i], o[b][j + 3][i]} * keep;
-            __syncthreads();
-            // a thread takes one query of each wave's rows and kCols dimensions
-            const int qr = threadIdx.x / 16, d0 = kCols * (threadIdx.x % 16);
-#pragma unroll
-            for (int x = 0; x < kRowWaves; ++x) {
-                const int out_row = 16 * (kBlocks * x + b) + qr, tok = out_row / t.heads, h = out_row - tok * t.heads;
-                if (tok >= t.n) continue;
-                float sum[kCols] = {}, lsum = 0.f, mx = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < kKeyWaves; ++w) mx = fmaxf(mx, tops[x * kKeyWaves + w][16 * b + qr]);
-#pragma unroll
-                for (int w = 0; w < kKeyWaves; ++w) {
-                    const int of = x * kKeyWaves + w;
-                    const float mw = tops[of][16 * b + qr];
-                    if (mw > -INFINITY) lsum += weights[of][16 * b + qr] * __builtin_amdgcn_exp2f((mw - mx) * c);
-#pragma unroll
-                    for (int j = 0; j < kCols; ++j) sum[j] += joint[of][qr][d0 + j];
-                }
-                if (whole) {
-                    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-                    const int64_t token = r.first + t.first + tok;
-                    const int64_t head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
-                    uint16_t *dst = a.out + token * a.out_token + head * a.out_head + d0;
-                    if (d0 < a.dim) {
-                        uint32_t y[kCols / 2];
-#pragma unroll
-                        for (int j = 0; j < kCols / 2; ++j) y[j] = pack<kHalf>(sum[2 * j] * inv, sum[2 * j + 1] * inv);
-                        if constexpr (kCols == 8) *reinterpret_cast<u32x4 *>(dst) = u32x4{y[0], y[1], y[2], y[3]};
-                        else *reinterpret_cast<u32x2 *>(dst) = u32x2{y[0], y[1]};
-                    }
-                    if (a.lse && d0 == 0)
-                        a.lse[token * a.heads + head] = lsum > 0.f ? mx * a.scale + logf(lsum) : -INFINITY;
-                } else {
-                    float *dst = a.sums + (at * kRows + out_row) * DP + d0;
-#pragma unroll
-                    for (int j = 0; j < kCols; j += 4)
-                        *reinterpret_cast<f32x4 *>(dst + j) = f32x4{sum[j], sum[j + 1], sum[j + 2], sum[j + 3]};
-                    if (d0 == 0) {
-                        float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP + (at * kRows + out_row) * 2;
-                        ml[0] = mx;
-                        ml[1] = lsum;
-                    }
+                    *reinterpret_cast<f32x4 *>(dst + j) = f32x4{sum[j], sum[j + 1], sum[j + 2], sum[j + 3]};
+                if (d0 == 0) {
+                    float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP + (at * kRows + out_row) * 2;
+                    ml[0] = mx;
+                    ml[1] = lsum;
                 }
             }
-            __syncthreads();
         }
+        __syncthreads();
     }
 }
 
 // -------------------------------------------------------------------- wide ---
 
-// A tile of 256 rows, 64 to a wave, by 64 keys a unit: the matrix products bound it.
+// A tile of 128 kBlocks rows, 32 kBlocks to a wave, by 64 keys a unit: the matrix products bound it
+// (kBlocks 2), or the bytes of K and V (kBlocks 1, for fewer rows).
 // K and V go through LDS, two units of each; the next one's bytes are on their way in
 // registers while this one is computed.  Keys lie apart in LDS by their bytes and 16 (K) or
 // 32 (V) more, which leaves no bank asked twice and every read at a fixed distance from
@@ -535,12 +536,11 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 ? 2 : 1) k_attend_narro
 // matrix unit does not wait for the softmax, a half unit (32 keys) is in three stages at
 // once: the products of the next half's scores and of the last half's weights with V run
 // beside this half's exponentials.
-constexpr int kWideKeys = 64, kWideRows = 256;
+constexpr int kWideKeys = 64;
 
-// kRuns: the 16 keys of a write lie side by side in one page (pages of 16 tokens or more, strides of 32
-// bits), so that its number and where they begin are the same for all lanes.
-template <int DP, bool kHalf, bool kRuns>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
+template <int DP, int kBlocks, bool kHalf, bool kRuns>
+__global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_attend_wide(Attend a) {
+    constexpr int kWaveRows = 32 * kBlocks, kRows = 4 * kWaveRows;
     constexpr int kPieces = DP / 8;            // 16-byte pieces of a key
     constexpr int kSteps = DP / 16;            // products over 16 dimensions
     constexpr int kCols = DP / 32;             // blocks of 32 output dimensions
@@ -589,11 +589,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         if (share.from == share.to) continue;  // (the piece ends before the next unit)
         const int32_t all = max(0, r.base + r.n);
         const int32_t most = max(0, min(r.base + t.first + t.n, all));
-        u32x4 q[2][kSteps];
-        int32_t seen[2];
+        u32x4 q[kBlocks][kSteps];
+        int32_t seen[kBlocks];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int row = 64 * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
+        for (int b = 0; b < kBlocks; ++b) {
+            const int row = kWaveRows * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
             const bool is = tok < t.n;
             seen[b] = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
             const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
@@ -605,14 +605,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
             }
         }
         // keys that every query of the wave's sees
-        const int32_t least = (64 * wave + 63) / t.heads < t.n
-                                  ? max(0, min(r.base + t.first + 64 * wave / t.heads + 1, all)) : 0;
-        f32x16 o[2][kCols], sa[2], sb[2];
-        u32x4 pa[2][2], pb[2][2];
+        const int32_t least = (kWaveRows * (wave + 1) - 1) / t.heads < t.n
+                                  ? max(0, min(r.base + t.first + kWaveRows * wave / t.heads + 1, all)) : 0;
+        f32x16 o[kBlocks][kCols], sa[kBlocks], sb[kBlocks];
+        u32x4 pa[kBlocks][2], pb[kBlocks][2];
         // m and m c; the score above which m follows; sums of weights; the highest of the last scores (this lane's)
-        float m[2] = {-INFINITY, -INFINITY}, mc[2] = {0.f, 0.f}, bound[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, top[2];
+        float m[kBlocks], mc[kBlocks], bound[kBlocks], l[kBlocks], top[kBlocks];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kBlocks; ++b) {
+            m[b] = bound[b] = -INFINITY;
+            mc[b] = l[b] = 0.f;
 #pragma unroll
             for (int d = 0; d < kCols; ++d) o[b][d] = f32x16{};
 #pragma unroll
@@ -684,23 +686,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
             for (int i = 1; i < 15; i += 2) x = fmaxf(fmaxf(x, s[i]), s[i + 1]);
             return fmaxf(x, s[15]);
         };
-        auto gather = [&](const uint16_t *at, const u32x4 (&w)[2][2]) {
+        auto gather = [&](const uint16_t *at, const u32x4 (&w)[kBlocks][2]) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int d = 0; d < kCols; ++d) {
                     const u32x4 v = read_v(at, d, i);
-                    o[0][d] = mfma32<kHalf>(v, w[0][i], o[0][d]);
-                    o[1][d] = mfma32<kHalf>(v, w[1][i], o[1][d]);
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) o[b][d] = mfma32<kHalf>(v, w[b][i], o[b][d]);
                 }
         };
         // scores of the half unit h at key k0, of a unit in pages `id`: those not seen are -inf
-        auto settle = [&](int32_t k0, int h, int32_t id, f32x16 (&s)[2]) {
+        auto settle = [&](int32_t k0, int h, int32_t id, f32x16 (&s)[kBlocks]) {
             if (__builtin_expect(k0 + 32 > clear, 0)) {
                 asm volatile("");  // a branch, not selections in every turn
                 const uint32_t ok = (uint32_t)(__ballot((uint32_t)id < (uint32_t)a.pages) >> 32 * h);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < kBlocks; ++b) {
                     const int32_t rest = seen[b] - k0 - 4 * half;
                     const uint32_t have = ok >> 4 * half;
 #pragma unroll
@@ -713,12 +715,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
             }
         };
         // m follows when it lags too far; the weights w, which are under the old one, go to O first
-        auto follow = [&](const uint16_t *at, u32x4 (&w)[2][2]) {
-            if (__builtin_expect(__any(top[0] > bound[0] || top[1] > bound[1]), 0)) {
+        auto follow = [&](const uint16_t *at, u32x4 (&w)[kBlocks][2]) {
+            if (__builtin_expect(__any(top[0] > bound[0] || top[kBlocks - 1] > bound[kBlocks - 1]), 0)) {
                 asm volatile("");
                 gather(at, w);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
+                for (int b = 0; b < kBlocks; ++b) {
                     const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[b]), __float_as_uint(top[b]), false, false);
                     const float now = fmaxf(m[b], fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
                     const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
@@ -736,9 +738,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         // A step is the two products with one fragment of K or V, the reads of a fragment further on, and
         // a share of the softmax and of `more`; the compiler keeps to the steps' order, which feeds the matrix
         // unit.  The first weights come before the first fragment has been read.
-        auto stage = [&](const f32x16 (&s)[2], u32x4 (&w)[2][2], const uint16_t *k, f32x16 (&s1)[2], const uint16_t *v,
-                         const u32x4 (&w0)[2][2], auto more) {
-            constexpr int kFrags = kSteps + 2 * kCols, kAhead = 2, kEach = 32 / kFrags, kFirst = 2 * kEach;
+        auto stage = [&](const f32x16 (&s)[kBlocks], u32x4 (&w)[kBlocks][2], const uint16_t *k, f32x16 (&s1)[kBlocks], const uint16_t *v,
+                         const u32x4 (&w0)[kBlocks][2], auto more) {
+            constexpr int kFrags = kSteps + 2 * kCols, kAhead = 2, kWeights = 16 * kBlocks, kEach = kWeights / kFrags,
+                          kFirst = 2 * kEach;
             constexpr int kTop = (16 + kFrags - kSteps - 2) / (kFrags - kSteps - 1);  // scores looked at in a step
             u32x4 frag[kAhead + 1];
             auto fetch = [&](int f) {
@@ -775,12 +778,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                 if (f + kAhead < kFrags) fetch(f + kAhead);
                 multiply(f, 0);
 #pragma unroll
-                for (int e = kFirst + kEach * f; e < min(32, kFirst + kEach * (f + 1)); ++e) weigh(e);
-                multiply(f, 1);
+                for (int e = kFirst + kEach * f; e < min(kWeights, kFirst + kEach * (f + 1)); ++e) weigh(e);
+                if constexpr (kBlocks == 2) multiply(f, 1);
                 more(f);
                 if (f > kSteps) {
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
+                    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                         for (int i = kTop * (f - kSteps - 1); i < min(16, kTop * (f - kSteps)); ++i)
                             top[b] = i ? fmaxf(top[b], s1[b][i]) : s1[b][0];
@@ -811,10 +814,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
             for (int f = 0; f < kSteps; ++f) {
                 const u32x4 x = read_k(k_half(0, 0), f);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) sa[b] = mfma32<kHalf>(x, q[b][f], f == 0 ? f32x16{} : sa[b]);
+                for (int b = 0; b < kBlocks; ++b) sa[b] = mfma32<kHalf>(x, q[b][f], f == 0 ? f32x16{} : sa[b]);
             }
 #pragma unroll
-            for (int b = 0; b < 2; ++b) top[b] = highest(sa[b]);
+            for (int b = 0; b < kBlocks; ++b) top[b] = highest(sa[b]);
             settle(k0, 0, id0, sa);
             follow(v_half(1, 1), pa);
             int x = 0;  // the unit's buffers
@@ -852,10 +855,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
         const bool whole = share.to - share.from == share.all;
         const int64_t at = 2 * block + (share.from == 0);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kBlocks; ++b) {
             const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[b]), __float_as_uint(l[b]), false, false);
             const float sum = __uint_as_float(y[0]) + __uint_as_float(y[1]);
-            const int row = 64 * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
+            const int row = kWaveRows * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
             if (tok >= t.n) continue;
             if (whole) {
                 const float inv = sum > 0.f ? 1.f / sum : 0.f;
@@ -874,7 +877,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                 if (a.lse && half == 0)
                     a.lse[token * a.heads + head] = sum > 0.f ? m[b] * a.scale + logf(sum) : -INFINITY;
             } else {
-                float *dst = a.sums + (at * kWideRows + row) * DP;
+                float *dst = a.sums + (at * kRows + row) * DP;
 #pragma unroll
                 for (int d = 0; d < kCols; ++d)
 #pragma unroll
@@ -882,7 +885,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
                         *reinterpret_cast<f32x4 *>(dst + 32 * d + 2 * i + 4 * half) =
                             f32x4{o[b][d][i], o[b][d][i + 1], o[b][d][i + 2], o[b][d][i + 3]};
                 if (half == 0) {
-                    float *ml = a.sums + 2 * (int64_t)a.blocks * kWideRows * DP + (at * kWideRows + row) * 2;
+                    float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP + (at * kRows + row) * 2;
                     ml[0] = m[b];
                     ml[1] = sum;
                 }
@@ -894,10 +897,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_wide(Attend a) {
 // ---------------------------------------------------------------------- join ---
 
 // Partial sums of the tiles that a cut goes through.  blockIdx.x is the cut after
-// block x, and works on the tile it is the first cut of; blockIdx.y takes kJoin rows of it.
+// block x, and works on the tile it is the first cut of; the blocks of one x share its rows.
 // A group of threads takes a row; where the tile is in many pieces, all groups share a
 // row's pieces and their sums meet in LDS.  The partial sums' bytes bound it.
-template <int DP, int kRows, int kJoin, bool kHalf>
+template <int DP, int kRows, bool kHalf>
 __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     constexpr int kLanes = DP / 4, kGroups = kThreads / kLanes;
     __shared__ float part[kGroups][DP];
@@ -905,8 +908,8 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     const int64_t cut = blockIdx.x + 1;
     const Cut t = a.cuts[cut];
     if (!t.is) return;
-    const int row0 = blockIdx.y * kJoin, row1 = min(row0 + kJoin, t.n * t.heads);
-    if (row0 >= row1) return;
+    const int rows = t.n * t.heads, each = (rows + gridDim.y - 1) / gridDim.y;
+    const int row0 = blockIdx.y * each, row1 = min(row0 + each, rows);
     const int64_t last = cut + t.more;  // the block with the tile's end
     const float c = a.scale * kLog2e;
     const float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP;
@@ -975,59 +978,59 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
 // -------------------------------------------------------------------- launch ---
 
 struct Shape {
-    int blocks, row_waves;  // of k_attend_narrow; 256 rows are k_attend_wide's
-    int grid;
-    int rows() const { return 16 * blocks * row_waves; }
-    int extra() const { return rows() == kWideRows ? 5 * kWideKeys : keys(); }
-    int keys() const { return rows() == kWideRows ? kWideKeys : 32 * (4 / row_waves); }
+    int rows, keys;   // of a tile, of a unit
+    int grid, extra;  // blocks of the launch; keys that stand for a tile's own cost
 };
 
 Shape shape_of(const tam_chunk &c, int64_t heads) {
     const int64_t longest = c.longest ? std::min(c.longest, c.tokens) : c.tokens;
     const int64_t rows = longest * (heads / c.kv_heads);
-    if (rows <= 16) return Shape{1, 1, 512};
-    if (rows <= 32) return Shape{2, 1, 256};
-    if (rows <= 64) return Shape{2, 2, 256};
-    if (rows <= 128) return Shape{2, 4, 256};
-    return Shape{4, 4, 256};
+    if (rows <= 16) return Shape{16, kNarrowKeys, 512, kNarrowKeys};
+    if (rows <= 128) return Shape{128, kWideKeys, 512, 2 * kWideKeys};
+    return Shape{256, kWideKeys, 256, 5 * kWideKeys};
 }
 
 int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
 
-template <int DP, int kBlocks, int kRowWaves, bool kHalf>
-hipError_t launch_narrow(const Attend &a, hipStream_t s) {
-    constexpr int kRows = 16 * kBlocks * kRowWaves, kJoin = 4;
-    hipLaunchKernelGGL((k_attend_narrow<DP, kBlocks, kRowWaves, kHalf>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
+template <int DP, int kRows, bool kHalf>
+hipError_t launch_join(const Attend &a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_join<DP, kRows, kJoin, kHalf>), dim3((unsigned)a.blocks - 1, (unsigned)(kRows / kJoin)),
-                       dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_join<DP, kRows, kHalf>), dim3((unsigned)a.blocks - 1, kRows == 16 ? 4 : 16), dim3(kThreads), 0, s, a);
     return hipGetLastError();
+}
+
+// whether kRuns holds
+bool runs(const Attend &a) {
+    return a.shift >= 4 && a.page_stride <= INT32_MAX && a.token_stride <= INT32_MAX >> a.shift;
+}
+
+template <int DP, int kBlocks, bool kHalf>
+hipError_t launch_wide(const Attend &a, hipStream_t s) {
+    constexpr size_t kLds = 2 * kWideKeys * (DP + 8 + DP + 16) * sizeof(uint16_t);
+    if (runs(a))
+        hipLaunchKernelGGL((k_attend_wide<DP, kBlocks, kHalf, true>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
+    else
+        hipLaunchKernelGGL((k_attend_wide<DP, kBlocks, kHalf, false>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
+    return launch_join<DP, 128 * kBlocks, kHalf>(a, s);
 }
 
 template <int DP, bool kHalf>
 hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
-    if (sh.rows() == 16) return launch_narrow<DP, 1, 1, kHalf>(a, s);
-    if (sh.rows() == 32) return launch_narrow<DP, 2, 1, kHalf>(a, s);
-    if (sh.rows() == 64) return launch_narrow<DP, 2, 2, kHalf>(a, s);
-    if (sh.rows() == 128) return launch_narrow<DP, 2, 4, kHalf>(a, s);
-    constexpr size_t kLds = 2 * kWideKeys * (DP + 8 + DP + 16) * sizeof(uint16_t);
-    if (a.shift >= 4 && a.page_stride <= INT32_MAX && (a.token_stride << a.shift) <= INT32_MAX)
-        hipLaunchKernelGGL((k_attend_wide<DP, kHalf, true>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
+    if (sh.rows == 256) return launch_wide<DP, 2, kHalf>(a, s);
+    if (sh.rows == 128) return launch_wide<DP, 1, kHalf>(a, s);
+    if (runs(a))
+        hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, true>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
     else
-        hipLaunchKernelGGL((k_attend_wide<DP, kHalf, false>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_join<DP, kWideRows, 32, kHalf>), dim3((unsigned)a.blocks - 1, kWideRows / 32),
-                       dim3(kThreads), 0, s, a);
-    return hipGetLastError();
+        hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, false>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
+    return launch_join<DP, 16, kHalf>(a, s);
 }
 
 }  // namespace
 
 int64_t attend_work_bytes(const tam_chunk &c, int64_t heads) {
     const Shape sh = shape_of(c, heads);
-    return 2 * (int64_t)sh.grid * sh.rows() * (padded(c.head_dim) + 2) * 4 + sh.grid * (int64_t)sizeof(Cut);
+    return 2 * (int64_t)sh.grid * sh.rows * (padded(c.head_dim) + 2) * 4 + sh.grid * (int64_t)sizeof(Cut);
 }
 
 hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipStream_t s) {
@@ -1039,14 +1042,14 @@ hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipSt
              c.offsets, c.slot_ids, c.table_stride, c.slots, c.max_pages, c.rows, c.tokens, (int32_t)c.num_pages,
              __builtin_ctzll((unsigned long long)c.page_tokens), (int32_t)q.heads, (int32_t)c.kv_heads,
              (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, 0, nullptr, nullptr};
-    a.group = (int32_t)std::min<int64_t>(group, sh.rows());
+    a.group = (int32_t)std::min<int64_t>(group, sh.rows);
     a.parts = (int32_t)((group + a.group - 1) / a.group);
-    a.tq = sh.rows() / a.group;
+    a.tq = sh.rows / a.group;
     a.blocks = sh.grid;
-    a.unit = sh.keys();
-    a.extra = sh.extra();
+    a.unit = sh.keys;
+    a.extra = sh.extra;
     a.sums = static_cast<float *>(work);
-    a.cuts = reinterpret_cast<Cut *>(a.sums + 2 * (int64_t)sh.grid * sh.rows() * (padded(c.head_dim) + 2));
+    a.cuts = reinterpret_cast<Cut *>(a.sums + 2 * (int64_t)sh.grid * sh.rows * (padded(c.head_dim) + 2));
     const bool half = c.dtype == TAM_DTYPE_FP16;
     if (padded(c.head_dim) == 64) return half ? launch<64, true>(a, sh, s) : launch<64, false>(a, sh, s);
     return half ? launch<128, true>(a, sh, s) : launch<128, false>(a, sh, s);
