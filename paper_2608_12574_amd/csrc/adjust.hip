@@ -1,9 +1,10 @@
 // Penalties, biases and the grammar's mask on [B, V] logits, in place.
 //
-// A block takes one span of one row's vocabulary.  It counts the row's text in a
-// table in LDS with one word per token of the span (an integer sum, so the order of
-// the atomics does not matter), and then goes through the span's logits in 16-byte
-// chunks: a chunk without a valid token is stored as -inf and not read, one
+// A block takes one span of one row's vocabulary.  A span without a valid token (most of
+// a constrained row's) is -inf, and nothing else is looked at.  Else the block counts
+// the row's text in a table in LDS with one word per token of the span (an integer sum,
+// so the order of the atomics does not matter), and then goes through the span's logits
+// in 16-byte chunks: a chunk without a valid token is stored as -inf and not read, one
 // whose valid tokens are not named is left alone or merged, and only the named
 // tokens are computed.  So a logit is read and written at most once, and the text
 // is all that is read beside the mask; each block of a row reads that again, from L2.
@@ -25,8 +26,12 @@ constexpr uint32_t kSeen = 1u << 19, kCount = kSeen - 1;
 constexpr int kEntry = 20;
 static_assert(TAM_MAX_HISTORY == kCount && TAM_MAX_BIASES == (1 << (32 - kEntry)) - 1, "fields of a table word");
 
-constexpr int kThreads = 256;
-constexpr int kSpan = 4096;  // tokens of a block
+// Threads and tokens of a block, with a mask and without.  The text is read again by each block of a row,
+// but more threads hold more of the chip back while one waits: us per call of 256 bf16 rows over
+// V = 262,144 (texts of 2,048, a mask) with 256 threads and 4,096 tokens 47, 512 and 8,192 50, 512 and
+// 4,096 68, 1,024 and 8,192 78, 128 and 2,048 56; of 64 fp32 rows over V = 128,255 (texts of 8,192, no
+// mask) 21, 18, 21, 20, 26.
+constexpr int kMaskThreads = 256, kMaskSpan = 4096, kFreeThreads = 512, kFreeSpan = 8192;
 
 template <typename T>
 struct Lane;
@@ -71,7 +76,7 @@ __device__ float edited(float x, uint32_t w, const Edits &e) {
     return x;
 }
 
-template <typename T>
+template <typename T, int kThreads, int kSpan>
 __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict__ rows, int64_t num_rows,
                                                      int64_t rows_stride, const int32_t *__restrict__ ids, tam_edits e,
                                                      int64_t V, T *__restrict__ logits, int64_t row_stride) {
@@ -87,12 +92,26 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
     if (v0 >= V) return;
     const int span = (int)min((int64_t)kSpan, V - v0);  // elements of the span, those before 0 among them
 
+    // What needs no other answer sets out first: the row's numbers and its first ids, kBatch per thread.
+    constexpr int kBatch = 8;
+    const int32_t *text = e.tokens + b * e.tokens_stride;
+    const int history = e.tokens ? (int)e.history : 0;
+    int32_t ids0[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+        const int i = threadIdx.x + j * kThreads;
+        ids0[j] = i < history ? text[i] : -1;
+    }
+    const int len = e.length ? min(max(e.length[b], 0), history) : history;
+    const int prompt = e.prompt ? e.prompt[b] : 0;
+    const Edits ed{e.repetition ? e.repetition[b] : 1.f, e.frequency ? e.frequency[b] : 0.f,
+                   e.presence ? e.presence[b] : 0.f, e.bias ? e.bias + b * e.bias_stride : nullptr};
     for (int i = threadIdx.x * 4; i < kSpan; i += kThreads * 4) *reinterpret_cast<u32x4 *>(&tab[i]) = u32x4{0, 0, 0, 0};
-    bool dead = false;
+    bool any = true;  // some token of the span is valid
     if (rows) {
         const int64_t r = ids[b];
-        dead = r < 0 || r >= num_rows;
-        if (!dead) {  // the span's bits, shifted so that bit 0 is element v0
+        uint32_t mine = 0;
+        if (r >= 0 && r < num_rows) {  // the span's bits, shifted so that bit 0 is element v0
             const uint32_t *src = reinterpret_cast<const uint32_t *>(rows + r * rows_stride);
             const int64_t words = (V + 31) / 32;
             const int sh = (int)(v0 & 31);
@@ -101,101 +120,121 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
                 const int64_t w = w0 + i;
                 const uint32_t lo = w >= 0 && w < words ? src[w] : 0u, hi = w + 1 < words ? src[w + 1] : 0u;
                 bits[i] = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
+                mine |= bits[i];
+            }
+        }
+        any = __syncthreads_or(mine);
+    } else {
+        __syncthreads();
+    }
+    // The span's chunks, kChunks per thread: without a valid token -inf at once; those that hold both
+    // kinds are read while the text is counted.
+    constexpr uint32_t kAll = (1u << N) - 1;
+    constexpr int kChunks = kSpan / (N * kThreads);
+    uint32_t valid[kChunks], inside[kChunks];
+    u32x4 x[kChunks];
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+        const int o = (threadIdx.x + k * kThreads) * N;
+        inside[k] = o < span ? kAll : 0u;  // elements of the chunk that the row has
+        if (v0 + o < 0) inside[k] &= kAll << (int)-(v0 + o);
+        if (o < span && o + N > span) inside[k] &= kAll >> (o + N - span);
+        valid[k] = !rows ? kAll : any ? (bits[o >> 5] >> (o & 31)) & kAll : 0u;
+        u32x4 *at = reinterpret_cast<u32x4 *>(row + (v0 + o));
+        if (inside[k] == kAll) {
+            if (!valid[k]) {
+                constexpr uint32_t m = Lane<T>::kMinusInf;
+                __builtin_nontemporal_store(u32x4{m, m, m, m}, at);
+            } else if (valid[k] != kAll) {
+                x[k] = *at;
             }
         }
     }
-    __syncthreads();
-    if (!dead) {
+    if (any) {
         if (e.bias_ids) {
             const int32_t *named = e.bias_ids + b * e.bias_stride;
             for (int i = threadIdx.x; i < (int)e.biases; i += kThreads) {
-                const int64_t v = named[i], o = v - v0;
-                if (v >= 0 && o >= 0 && o < span) atomicMax(&tab[o], (uint32_t)(i + 1) << kEntry);
+                const int32_t v = named[i];
+                const uint32_t o = (uint32_t)v - (uint32_t)v0;
+                if (v >= 0 && o < (uint32_t)span) atomicMax(&tab[o], (uint32_t)(i + 1) << kEntry);
             }
             __syncthreads();  // the entry's field is final before the counts are added below it
         }
-        if (e.tokens) {
-            const int32_t *text = e.tokens + b * e.tokens_stride;
-            const int len = e.length ? min(max(e.length[b], 0), (int)e.history) : (int)e.history;
-            const int prompt = e.prompt ? e.prompt[b] : 0;
-            for (int i = threadIdx.x; i < len; i += kThreads) {
-                const int64_t v = text[i], o = v - v0;
-                if (v >= 0 && o >= 0 && o < span) {
-                    if (i < prompt)
-                        atomicOr(&tab[o], kSeen);
-                    else
-                        atomicAdd(&tab[o], 1u);
-                }
+        auto count = [&](int32_t v, int i) {
+            const uint32_t o = (uint32_t)v - (uint32_t)v0;
+            if (i < len && v >= 0 && o < (uint32_t)span) {
+                if (i < prompt)
+                    atomicOr(&tab[o], kSeen);
+                else
+                    atomicAdd(&tab[o], 1u);
             }
-            __syncthreads();
+        };
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) count(ids0[j], threadIdx.x + j * kThreads);
+        for (int i0 = threadIdx.x + kThreads * kBatch; i0 < len; i0 += kThreads * kBatch) {
+            int32_t v[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) v[j] = i0 + j * kThreads < len ? text[i0 + j * kThreads] : -1;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) count(v[j], i0 + j * kThreads);
         }
+        __syncthreads();
     }
-    const Edits ed{e.repetition ? e.repetition[b] : 1.f, e.frequency ? e.frequency[b] : 0.f,
-                   e.presence ? e.presence[b] : 0.f, e.bias ? e.bias + b * e.bias_stride : nullptr};
-    constexpr uint32_t kAll = (1u << N) - 1;
-    for (int o = threadIdx.x * N; o < span; o += kThreads * N) {
-        uint32_t inside = kAll;  // elements of the chunk that the row has
-        if (v0 + o < 0) inside &= kAll << (int)-(v0 + o);
-        if (o + N > span) inside &= kAll >> (o + N - span);
-        uint32_t valid = kAll;
-        if (rows) valid = dead ? 0u : (bits[o >> 5] >> (o & 31)) & kAll;
-        u32x4 *at = reinterpret_cast<u32x4 *>(row + (v0 + o));
-        if (!(valid & inside)) {
-            if (inside == kAll) {
-                constexpr uint32_t m = Lane<T>::kMinusInf;
-                __builtin_nontemporal_store(u32x4{m, m, m, m}, at);
-                continue;
-            }
-        }
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+        const int o = (threadIdx.x + k * kThreads) * N;
+        const bool whole = inside[k] == kAll;
+        if (!inside[k] || (whole && !valid[k])) continue;
         uint32_t named = 0;
-        if (valid) {
+        if (valid[k]) {
 #pragma unroll
             for (int i = 0; i < N; i += 4) {
                 const u32x4 w = *reinterpret_cast<const u32x4 *>(&tab[o + i]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) named |= (w[j] != 0u) << (i + j);
             }
-            named &= valid;
+            named &= valid[k];
         }
-        const uint32_t edit = (named | ~valid) & inside;
+        const uint32_t edit = (named | ~valid[k]) & inside[k];
         if (!edit) continue;
-        if (inside == kAll) {
-            u32x4 x = *at;
+        if (whole) {
+            u32x4 *at = reinterpret_cast<u32x4 *>(row + (v0 + o));
+            u32x4 y = valid[k] == kAll ? *at : x[k];
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                if (!(valid >> i & 1)) Lane<T>::minus_inf(x, i);
-                else if (named >> i & 1) Lane<T>::put(x, i, edited(Lane<T>::get(x, i), tab[o + i], ed));
+                if (!(valid[k] >> i & 1)) Lane<T>::minus_inf(y, i);
+                else if (named >> i & 1) Lane<T>::put(y, i, edited(Lane<T>::get(y, i), tab[o + i], ed));
             }
-            __builtin_nontemporal_store(x, at);
+            __builtin_nontemporal_store(y, at);
         } else {  // the row's ends: element by element
             for (int i = 0; i < N; ++i) {
                 if (!(edit >> i & 1)) continue;
-                u32x4 x{0, 0, 0, 0};
+                u32x4 y{0, 0, 0, 0};
                 T *p = row + (v0 + o + i);
-                if (!(valid >> i & 1)) {
-                    Lane<T>::minus_inf(x, 0);
+                if (!(valid[k] >> i & 1)) {
+                    Lane<T>::minus_inf(y, 0);
                 } else {
                     uint32_t raw = 0;
                     __builtin_memcpy(&raw, p, sizeof(T));
-                    x[0] = raw;
-                    Lane<T>::put(x, 0, edited(Lane<T>::get(x, 0), tab[o + i], ed));
+                    y[0] = raw;
+                    Lane<T>::put(y, 0, edited(Lane<T>::get(y, 0), tab[o + i], ed));
                 }
-                const uint32_t raw = x[0];
+                const uint32_t raw = y[0];
                 __builtin_memcpy(p, &raw, sizeof(T));
             }
         }
     }
 }
 
-template <typename T>
+template <typename T, int kThreads, int kSpan>
 hipError_t launch(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, const int32_t *ids, tam_edits e,
                   int64_t B, int64_t V, T *logits, int64_t row_stride, hipStream_t s) {
     // a row may start up to 15 bytes into a chunk, which moves its end as far
     const unsigned gx = (unsigned)((V + Lane<T>::n - 1 + kSpan - 1) / kSpan);
     for (int64_t r0 = 0; r0 < B; r0 += 65535) {
         const int64_t n = std::min<int64_t>(B - r0, 65535);
-        hipLaunchKernelGGL((k_adjust<T>), dim3(gx, (unsigned)n), dim3(kThreads), 0, s, rows, num_rows, rows_stride,
-                           ids ? ids + r0 : nullptr, e, V, logits + r0 * row_stride, row_stride);
+        hipLaunchKernelGGL((k_adjust<T, kThreads, kSpan>), dim3(gx, (unsigned)n), dim3(kThreads), 0, s, rows, num_rows,
+                           rows_stride, ids ? ids + r0 : nullptr, e, V, logits + r0 * row_stride, row_stride);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
         if (e.tokens) e.tokens += n * e.tokens_stride;
@@ -208,14 +247,22 @@ hipError_t launch(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, c
     return hipSuccess;
 }
 
+template <typename T>
+hipError_t launch_type(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, const int32_t *ids,
+                       const tam_edits &e, int64_t B, int64_t V, void *logits, int64_t row_stride, hipStream_t s) {
+    T *p = static_cast<T *>(logits);
+    return rows ? launch<T, kMaskThreads, kMaskSpan>(rows, num_rows, rows_stride, ids, e, B, V, p, row_stride, s)
+                : launch<T, kFreeThreads, kFreeSpan>(rows, num_rows, rows_stride, ids, e, B, V, p, row_stride, s);
+}
+
 }  // namespace
 
 hipError_t launch_adjust(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, const int32_t *ids,
                          const tam_edits &e, int64_t B, int64_t V, void *logits, int dtype, int64_t row_stride,
                          hipStream_t s) {
     if (dtype == TAM_DTYPE_BF16)
-        return launch(rows, num_rows, rows_stride, ids, e, B, V, static_cast<uint16_t *>(logits), row_stride, s);
-    return launch(rows, num_rows, rows_stride, ids, e, B, V, static_cast<float *>(logits), row_stride, s);
+        return launch_type<uint16_t>(rows, num_rows, rows_stride, ids, e, B, V, logits, row_stride, s);
+    return launch_type<float>(rows, num_rows, rows_stride, ids, e, B, V, logits, row_stride, s);
 }
 
 }  // namespace tam

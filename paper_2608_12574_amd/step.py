@@ -16,70 +16,80 @@ def _bad(where, what):
     return TamError(-1, where, what)
 
 
-def _stream(c, stream):
-    return c.stream() if stream is None else stream.cuda_stream
-
-
-def _int32(where, name, t, shape=None, null=True):
-    """The pointer of a contiguous device int32 tensor (None: null)."""
-    if t is None:
-        if null:
-            return None
-        raise _bad(where, f"{name} is missing")
-    if t.dtype is not _calls().int32 or not t.is_cuda or not t.is_contiguous():
-        raise _bad(where, f"{name} must be a contiguous int32 tensor on the GPU")
-    if shape is not None and tuple(t.shape) != shape:
-        raise _bad(where, f"{name} has shape {tuple(t.shape)}, not {shape}")
+def _int32(where, name, t, n):
+    """The pointer of a contiguous device int32 tensor of n elements."""
+    if t.dtype is not _int or not t.is_cuda or t.numel() != n or not t.is_contiguous():
+        raise _bad(where, f"{name} must be a contiguous int32 tensor of {n} elements on the GPU")
     return t.data_ptr()
 
 
 def _rows_of(where, name, t, B, dtype):
     """(pointer, row stride, columns) of a device [B, n] tensor whose rows are contiguous."""
-    if t is None:
-        return None, 0, 0
-    if t.dtype is not dtype or not t.is_cuda or t.dim() != 2 or t.shape[0] != B or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dtype is not dtype or not t.is_cuda or t.dim() != 2:
+        raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on the GPU")
+    rows, n = t.shape
+    stride, step = t.stride()
+    if rows != B or (n > 1 and step != 1):
         raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on the GPU with contiguous rows")
-    return t.data_ptr(), max(t.stride(0), t.shape[1]) if B == 1 else t.stride(0), t.shape[1]
+    return t.data_ptr(), stride if B > 1 else max(stride, n), n
+
+
+_int = _float = _long = None  # torch's types, once torch is there
+
+
+def _ready():
+    global _int, _float, _long
+    import torch
+    c = _calls()
+    c.adjust = _tam.lib().tam_adjust_logits
+    _int, _float, _long = torch.int32, torch.float32, torch.int64
+    return c
 
 
 def _adjust(logits, stream, handle=None, rows=None, ids=None, tokens=None, length=None, prompt=None, repetition=None,
             frequency=None, presence=None, bias_ids=None, bias=None):
-    import torch
     where = "tam_adjust_logits"
-    c = _tam._calls_made or _calls()
-    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in c.dtypes or (
-            logits.shape[1] > 1 and logits.stride(1) != 1):
-        raise _bad(where, "logits must be a [B, V] fp32 or bf16 tensor on the GPU with contiguous rows")
+    c = _tam._calls_made if _int is not None else _ready()
+    dtype = c.dtypes.get(logits.dtype)
+    if dtype is None or not logits.is_cuda or logits.dim() != 2:
+        raise _bad(where, "logits must be a [B, V] fp32 or bf16 tensor on the GPU")
     B, V = logits.shape
+    row_stride, step = logits.stride()
+    if V > 1 and step != 1:
+        raise _bad(where, "logits must have contiguous rows")
+    row_stride = row_stride if B > 1 else max(row_stride, V)
+    raw = rows_p = ids_p = None
+    num_rows = stride = 0
     if handle is not None:
         if V < handle.vocab_size:
             raise _bad(where, f"logits have {V} columns, the vocabulary {handle.vocab_size} tokens")
-        V = handle.vocab_size
-    masked = handle is not None or rows is not None
-    ids_p = _int32(where, "node_ids" if handle is not None else "row_ids", ids, (B,), null=not masked)
-    num_rows = stride = 0
-    rows_p = None
-    if rows is not None:
-        if rows.dtype is not torch.int64 or not rows.is_cuda or rows.dim() != 2 or rows.shape[1] < (V + 63) // 64 or (
-                rows.shape[1] > 1 and rows.stride(1) != 1):
-            raise _bad(where, f"rows must be an [R, {(V + 63) // 64}] int64 tensor on the GPU with contiguous rows")
-        rows_p, num_rows, stride = rows.data_ptr(), rows.shape[0], max(rows.stride(0), rows.shape[1])
-    e = Edits()
-    e.tokens, e.tokens_stride, e.history = _rows_of(where, "tokens", tokens, B, c.int32)
-    e.length = _int32(where, "length", length, (B,))
-    e.prompt = _int32(where, "prompt", prompt, (B,))
-    for name, t in (("repetition", repetition), ("frequency", frequency), ("presence", presence)):
-        if t is not None:
-            if t.dtype is not torch.float32 or not t.is_cuda or tuple(t.shape) != (B,) or not t.is_contiguous():
-                raise _bad(where, f"{name} must be a contiguous [{B}] fp32 tensor on the GPU")
-            setattr(e, name, t.data_ptr())
-    e.bias_ids, e.bias_stride, e.biases = _rows_of(where, "bias_ids", bias_ids, B, c.int32)
-    e.bias, other, n = _rows_of(where, "bias", bias, B, torch.float32)
-    if (e.bias_stride, e.biases) != (other, n):
+        V, raw = handle.vocab_size, handle._raw
+        ids_p = _int32(where, "node_ids", ids, B)
+    elif rows is not None:
+        if ids is None:
+            raise _bad(where, "rows without row_ids")
+        rows_p, stride, width = _rows_of(where, "rows", rows, rows.shape[0], _long)
+        num_rows = rows.shape[0]
+        if width < (V + 63) // 64:
+            raise _bad(where, f"rows must have {(V + 63) // 64} words")
+        ids_p = _int32(where, "row_ids", ids, B)
+    text_p, text_stride, history = (None, 0, 0) if tokens is None else _rows_of(where, "tokens", tokens, B, _int)
+    floats = []
+    for t in (repetition, frequency, presence):
+        if t is None:
+            floats.append(None)
+            continue
+        if t.dtype is not _float or not t.is_cuda or t.numel() != B or not t.is_contiguous():
+            raise _bad(where, f"repetition, frequency and presence must be contiguous [{B}] fp32 tensors on the GPU")
+        floats.append(t.data_ptr())
+    named_p, named_stride, named = (None, 0, 0) if bias_ids is None else _rows_of(where, "bias_ids", bias_ids, B, _int)
+    bias_p, other, n = (None, 0, 0) if bias is None else _rows_of(where, "bias", bias, B, _float)
+    if named_stride != other or named != n:
         raise _bad(where, "bias_ids and bias must have the same shape and strides")
-    rc = _tam.lib().tam_adjust_logits(handle._raw if handle is not None else None, rows_p, num_rows, stride, ids_p,
-                                      ctypes.byref(e), B, V, logits.data_ptr(), c.dtypes[logits.dtype],
-                                      logits.stride(0) if B > 1 else max(logits.stride(0), V), _stream(c, stream))
+    e = Edits(text_p, text_stride, history, None if length is None else _int32(where, "length", length, B),
+              None if prompt is None else _int32(where, "prompt", prompt, B), *floats, named_p, bias_p, named_stride, named)
+    rc = c.adjust(raw, rows_p, num_rows, stride, ids_p, ctypes.byref(e), B, V, logits.data_ptr(), dtype, row_stride,
+                  c.stream() if stream is None else stream.cuda_stream)
     if rc != TAM_OK:
         _check(rc, where)
     return logits
@@ -127,8 +137,9 @@ class PageCache:
             raise _bad(where, "table must be a [slots, max_pages] int32 tensor on the GPU with contiguous rows")
         slots, width = table.shape
         stride = max(table.stride(0), width)
-        length_p = _int32(where, "length", length, (slots,), null=False)
-        refs_p = _int32(where, "refs", refs, (pages,), null=False)
+        self._calls = _tam._calls_made if _int is not None else _ready()
+        length_p = _int32(where, "length", length, slots)
+        refs_p = _int32(where, "refs", refs, pages)
         self.data, self.table, self.length, self.refs = data, table, length, refs
         self.layers, self.kv_heads, self.page_tokens, self.head_dim = planes // 2, kv, page, dim
         self._torch = torch
@@ -139,8 +150,9 @@ class PageCache:
         dtype = DTYPE_FP16 if data.dtype is torch.float16 else DTYPE_BF16
         self._chunk = Chunk(None, None, data.stride(1), data.stride(2), data.stride(3), pages, page, kv, dim, dtype,
                             table.data_ptr(), slots, width, stride, length_p)
-        self._chunk_ref = ctypes.byref(self._chunk)
-        if _tam.lib().tam_pages_work(self._pages_ref, 0) < 0:
+        self._lib = _tam.lib()
+        self._work_bytes = self._lib.tam_pages_work(self._pages_ref, slots)  # enough for any call
+        if self._work_bytes < 0:
             _check(-1, where)
 
     @classmethod
@@ -163,14 +175,11 @@ class PageCache:
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self.data.device)
 
-    def _work(self, n, stream):
-        size = _tam.lib().tam_pages_work(self._pages_ref, n)
-        if size < 0:
-            _check(-1, "tam_pages_work")
-        return self._empty(size, self._torch.uint8, stream)
+    def _work(self, stream):
+        return self._empty(self._work_bytes, self._torch.uint8, stream)
 
     def _on(self, stream):
-        return _stream(_tam._calls_made or _calls(), stream)
+        return self._calls.stream() if stream is None else stream.cuda_stream
 
     def fork(self, slots, parents, lengths=None, stream=None):
         """Slot ``slots[i]`` becomes a copy of the first ``lengths[i]`` tokens (all of them without
@@ -178,10 +187,10 @@ class PageCache:
         slots (-1) frees the slot.  Pages are shared, not copied."""
         where = "tam_pages_fork"
         n = slots.numel()
-        s, p = _int32(where, "slots", slots, (n,)), _int32(where, "parents", parents, (n,))
-        work = self._work(n, stream)
-        rc = _tam.lib().tam_pages_fork(self._pages_ref, s, p, _int32(where, "lengths", lengths, (n,)), n,
-                                       work.data_ptr(), self._on(stream))
+        s, p = _int32(where, "slots", slots, n), _int32(where, "parents", parents, n)
+        keep = None if lengths is None else _int32(where, "lengths", lengths, n)
+        work = self._work(stream)
+        rc = self._lib.tam_pages_fork(self._pages_ref, s, p, keep, n, work.data_ptr(), self._on(stream))
         if rc != TAM_OK:
             _check(rc, where)
 
@@ -202,10 +211,10 @@ class PageCache:
         ``max_pages`` is too small for."""
         where = "tam_pages_extend"
         n = slots.numel()
-        s, c = _int32(where, "slots", slots, (n,)), _int32(where, "counts", counts, (n,))
-        work = self._work(n, stream)
+        s, c = _int32(where, "slots", slots, n), _int32(where, "counts", counts, n)
+        work = self._work(stream)
         info = self._empty(4, self._torch.int32, stream)
-        rc = _tam.lib().tam_pages_extend(self._pages_ref, s, c, n, info.data_ptr(), work.data_ptr(), self._on(stream))
+        rc = self._lib.tam_pages_extend(self._pages_ref, s, c, n, info.data_ptr(), work.data_ptr(), self._on(stream))
         if rc != TAM_OK:
             _check(rc, where)
         return info
@@ -213,10 +222,10 @@ class PageCache:
     def compact(self, stream=None):
         """The pages in use move to the front of the pool.  Returns int32 [2] (pages in use,
         pages moved) and int32 [pages] (each page's new number, -1 of a free one), both on the GPU."""
-        work = self._work(0, stream)
+        work = self._work(stream)
         info = self._empty(2, self._torch.int32, stream)
         moved = self._empty(self.refs.shape, self._torch.int32, stream)
-        rc = _tam.lib().tam_pages_compact(self._pages_ref, info.data_ptr(), moved.data_ptr(), work.data_ptr(),
+        rc = self._lib.tam_pages_compact(self._pages_ref, info.data_ptr(), moved.data_ptr(), work.data_ptr(),
                                           self._on(stream))
         if rc != TAM_OK:
             _check(rc, "tam_pages_compact")
@@ -226,20 +235,20 @@ class PageCache:
     def _new(self, where, layer, tokens, offsets, slots, longest):
         if not 0 <= layer < self.layers:
             raise _bad(where, f"layer {layer} of {self.layers}")
-        c = self._chunk
-        c.offsets = _int32(where, "offsets", offsets)
+        c = Chunk.from_buffer_copy(self._chunk)  # a call's own: threads may share the cache
         if offsets is not None:
-            if offsets.dim() != 1 or offsets.numel() < 1:
-                raise _bad(where, "offsets must be [rows + 1]")
             rows = offsets.numel() - 1
+            if rows < 0:
+                raise _bad(where, "offsets must be [rows + 1]")
+            c.offsets = _int32(where, "offsets", offsets, rows + 1)
         else:
-            rows = tokens
-        c.slot_ids = _int32(where, "slots", slots, (rows,))
+            rows, c.offsets = tokens, None
+        c.slot_ids = None if slots is None else _int32(where, "slots", slots, rows)
         plane = self._pages.plane_stride
         c.k = self._pages.data + 2 * layer * plane
         c.v = c.k + plane
         c.rows, c.tokens, c.longest = rows, tokens, (1 if offsets is None else 0) if longest is None else longest
-        return self._chunk_ref
+        return ctypes.byref(c)
 
     def _vectors(self, where, name, t, heads=None):
         """(pointer, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
@@ -257,7 +266,7 @@ class PageCache:
         kp, vp = self._vectors(where, "k", k, self.kv_heads), self._vectors(where, "v", v, self.kv_heads)
         if k.shape[0] != v.shape[0]:
             raise _bad(where, "k and v have different numbers of tokens")
-        rc = _tam.lib().tam_pages_store(self._new(where, layer, k.shape[0], offsets, slots, longest), *kp, *vp,
+        rc = self._lib.tam_pages_store(self._new(where, layer, k.shape[0], offsets, slots, longest), *kp, *vp,
                                         self._on(stream))
         if rc != TAM_OK:
             _check(rc, where)
@@ -279,7 +288,7 @@ class PageCache:
         op = self._vectors(where, "out", out)
         lse = self._empty((T, heads), self._torch.float32, stream) if return_lse else None
         chunk = self._new(where, layer, T, offsets, slots, longest)
-        lib = _tam.lib()
+        lib = self._lib
         size = lib.tam_attend_work(chunk, heads)
         if size < 0:
             _check(-1, where)
