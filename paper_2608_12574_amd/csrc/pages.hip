@@ -213,26 +213,40 @@ __global__ void __launch_bounds__(kPlan) k_extend(Tables t, const int32_t *__res
         for (int64_t i = threadIdx.x; i < n; i += kPlan) w.src[i] = -1;
         return;
     }
-    // a wave per row hands its pages out
+    // The pages are handed out: a thread takes a row, and the rows that get many pages go to the whole wave.
+    constexpr int kAlone = 4;
     const int lane = threadIdx.x % kWave;
-    for (int64_t i = threadIdx.x / kWave; i < n; i += kPlan / kWave) {
-        const int64_t slot = slots[i];
-        if (!t.slot_ok(slot) || counts[i] <= 0) continue;
-        const int32_t src = w.src[i];
-        const int64_t len = t.tokens(slot), total = t.held(len + counts[i]);
-        const int64_t first = t.held(len) - (src >= 0);
-        const int32_t *mine = w.got + w.start[i];
-        for (int64_t j = first + lane; j < total; j += kWave) {
-            const int32_t page = mine[j - first];
-            t.table[slot * t.stride + j] = page;
-            t.refs[page] = 1;
-        }
-        if (lane == 0) {
+    for (int64_t i0 = 0; i0 < n; i0 += kPlan) {
+        const int64_t i = i0 + threadIdx.x;
+        int64_t slot = -1, first = 0, total = 0;
+        int32_t start = 0;
+        if (i < n && t.slot_ok(slots[i]) && counts[i] > 0) {
+            slot = slots[i];
+            start = w.start[i];
+            const int32_t src = w.src[i];
+            const int64_t len = t.tokens(slot);
+            total = t.held(len + counts[i]);
+            first = t.held(len) - (src >= 0);
             if (src >= 0) {
-                w.dst[i] = mine[0];
+                w.dst[i] = w.got[start];
                 atomicSub(&t.refs[src], 1);
             }
             t.length[slot] = (int32_t)(len + counts[i]);
+            for (int64_t j = first; j < min(total, first + kAlone); ++j) {
+                const int32_t page = w.got[start + (j - first)];
+                t.table[slot * t.stride + j] = page;
+                t.refs[page] = 1;
+            }
+        }
+        for (uint64_t rest = __ballot(total - first > kAlone); rest; rest &= rest - 1) {
+            const int of = __ffsll((unsigned long long)rest) - 1;
+            const int64_t s = __shfl(slot, of), f = __shfl(first, of), m = __shfl(total, of);
+            const int32_t at = __shfl(start, of);
+            for (int64_t j = f + kAlone + lane; j < m; j += kWave) {
+                const int32_t page = w.got[at + (j - f)];
+                t.table[s * t.stride + j] = page;
+                t.refs[page] = 1;
+            }
         }
     }
 }
@@ -375,7 +389,9 @@ __global__ void __launch_bounds__(kBlock) k_store(Store a) {
     }
 }
 
-constexpr int64_t kFew = 16384;  // table entries that one block forks
+// Rows that one block forks: a row's trips to memory follow one another, so a wave takes one row (us per
+// call, one launch and two: 4 rows 2.3 and 5.2, 256 rows 38 and 6.1).
+constexpr int64_t kFew = kPlan / kWave;
 
 }  // namespace
 
@@ -389,7 +405,7 @@ hipError_t launch_pages_fork(const tam_pages &c, const int32_t *slots, const int
                              int64_t n, void *work, hipStream_t s) {
     const Tables t = tables_of(c);
     int32_t *rows = static_cast<int32_t *>(work), *lens = rows + n * c.max_pages;
-    if (n * c.max_pages <= kFew) {
+    if (n <= kFew) {
         hipLaunchKernelGGL(k_fork_few, dim3(1), dim3(kPlan), 0, s, t, slots, parents, lengths, n, rows, lens);
         return hipGetLastError();
     }
