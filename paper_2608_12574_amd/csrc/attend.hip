@@ -38,7 +38,7 @@ constexpr int kWave = 64;
 constexpr int kThreads = 256;
 
 // Memory's addresses, told from LDS's, so that a load does not wait as if it could be of either.
-typedef __attribute__((address_space(1))) const uint16_t global_u16;
+typedef __attribute__((address_space(1))) const uint8_t global_u8;
 typedef __attribute__((address_space(1))) const u32x4 global_u32x4;
 typedef __attribute__((address_space(1))) const u32x2 global_u32x2;
 
@@ -259,6 +259,21 @@ constexpr float kLag = 8.f;  // m may lag by this much, in powers of two
 // In both kernels below, kRuns: 16 keys from a multiple of 16 lie side by side in one page (pages of 16
 // tokens or more, strides of 32 bits), so that its number and where they begin are the same for all lanes.
 
+// Where place `in` of a page (kRuns: its run of 16) begins, in bytes.
+template <bool kRuns>
+__device__ inline uint64_t place_in(const Attend &a, uint32_t page, uint32_t in) {
+    if constexpr (kRuns)
+        return (uint64_t)page * (uint32_t)(2 * a.page_stride) + (in & ~15u) * (uint32_t)(2 * a.token_stride);
+    else
+        return (uint64_t)page * (uint64_t)(2 * a.page_stride) + in * (uint64_t)(2 * a.token_stride);
+}
+
+// What lane `of` holds of x, for all lanes.
+__device__ inline uint64_t lane_of(uint64_t x, int of) {
+    return (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, of) |
+           (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), of) << 32;
+}
+
 // A tile of at most 16 rows by all its keys, 32 keys per wave and step.  The bytes of
 // K and V bound it, so the fragments come straight from memory into registers, the next
 // step's while this one is computed, and LDS only joins the waves' sums at the end.
@@ -278,13 +293,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
     const int lane = threadIdx.x % kWave, wave = uniform((int32_t)threadIdx.x / kWave);
     const int col = lane % 16, grp = lane / 16;
     const uint32_t place = (1u << a.shift) - 1;
-    // where a lane's parts of K and V lie in their vectors (kRuns: from their run's first); lanes past the
+    // where a lane's parts of K and V lie in their vectors, in bytes (kRuns: from their run's first); lanes past the
     // last dimension read others of the vector
     uint32_t k_in[kSteps];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
-        k_in[s] = (32 * s + 8 * grp < a.dim ? 32 * s + 8 * grp : 0) + (kRuns ? (uint32_t)col * (uint32_t)a.token_stride : 0);
-    const uint32_t v_in = (kCols * col < a.dim ? kCols * col : 0) + (kRuns ? (uint32_t)(4 * grp) * (uint32_t)a.token_stride : 0);
+        k_in[s] = 2 * ((32 * s + 8 * grp < a.dim ? 32 * s + 8 * grp : 0) + (kRuns ? (uint32_t)col * (uint32_t)a.token_stride : 0));
+    const uint32_t v_in = 2 * ((kCols * col < a.dim ? kCols * col : 0) + (kRuns ? (uint32_t)(4 * grp) * (uint32_t)a.token_stride : 0));
     int64_t piece;
     Place p = find(a, blockIdx.x, &piece);
     if (p.row < 0) {
@@ -328,8 +343,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
         float m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int j = 0; j < kCols; ++j) o[j] = f32x4{0, 0, 0, 0};
-        global_u16 *const kh = (global_u16 *)(a.k + (int64_t)t.head * a.head_stride);
-        global_u16 *const vh = (global_u16 *)(a.v + (int64_t)t.head * a.head_stride);
+        global_u8 *const kh = (global_u8 *)(a.k + (int64_t)t.head * a.head_stride);
+        global_u8 *const vh = (global_u8 *)(a.v + (int64_t)t.head * a.head_stride);
         const int32_t *const pages = a.table + r.slot * a.table_stride;
         int32_t clear = least;  // keys that need no look at the mask; 0 once a page number is bad
 
@@ -341,10 +356,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
             const bool ok = (uint32_t)id < (uint32_t)a.pages;
             if (!__all(ok)) clear = 0;
             const uint32_t in = (uint32_t)key_of(k0) & place;
-            if constexpr (kRuns)
-                return (uint64_t)(ok ? id : 0) * (uint32_t)a.page_stride + (in & ~15u) * (uint32_t)a.token_stride;
-            else
-                return (uint64_t)(ok ? id : 0) * (uint64_t)a.page_stride + in * (uint64_t)a.token_stride;
+            return place_in<kRuns>(a, ok ? id : 0, in);
         };
         struct Step {
             u32x4 k[2][kSteps];
@@ -354,25 +366,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
         auto load = [&](uint64_t at, Step &x) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                uint64_t begin;
-                if constexpr (kRuns)
-                    begin = (uint32_t)__builtin_amdgcn_readlane((uint32_t)at, 16 * i) |
-                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(at >> 32), 16 * i) << 32;
-                else
-                    begin = __shfl(at, 16 * i + col);
+                const uint64_t begin = kRuns ? lane_of(at, 16 * i) : __shfl(at, 16 * i + col);
 #pragma unroll
                 for (int s = 0; s < kSteps; ++s) x.k[i][s] = *(global_u32x4 *)(kh + begin + k_in[s]);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint64_t begin;
-                if constexpr (kRuns)
-                    begin = (uint32_t)__builtin_amdgcn_readlane((uint32_t)at, 16 * (j / 4)) |
-                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(at >> 32), 16 * (j / 4)) << 32,
-                    begin += (uint32_t)(j % 4) * (uint32_t)a.token_stride;
-                else
-                    begin = __shfl(at, 16 * (j / 4) + 4 * grp + j % 4);
-                global_u16 *src = vh + begin + v_in;
+                const uint64_t begin = kRuns ? lane_of(at, 16 * (j / 4)) + (uint32_t)(j % 4) * (uint32_t)(2 * a.token_stride)
+                                             : __shfl(at, 16 * (j / 4) + 4 * grp + j % 4);
+                global_u8 *src = vh + begin + v_in;
                 if constexpr (kCols == 8) {
                     x.v[j] = *(global_u32x4 *)src;
                 } else {
@@ -571,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
     constexpr int kApart = kThreads / kPieces;
     const int key = threadIdx.x / kPieces, mine = threadIdx.x % kPieces;
     uint16_t *const k_write = kbuf + key * kKStride + 8 * mine, *const v_write = vbuf + key * kVStride + 8 * mine;
-    const uint32_t in_run = (uint32_t)(key % 16) * (uint32_t)a.token_stride + (8 * mine < a.dim ? 8 * mine : 0);
+    const uint32_t in_run = 2 * ((kRuns ? (uint32_t)(key % 16) * (uint32_t)a.token_stride : 0) + (8 * mine < a.dim ? 8 * mine : 0));
 
     while (left > 0) {
         const Row r = shared_row(a, p.row);
@@ -620,8 +622,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
 #pragma unroll
             for (int i = 0; i < 2; ++i) pa[b][i] = u32x4{0, 0, 0, 0};
         }
-        global_u16 *const kh = (global_u16 *)(a.k + (int64_t)t.head * a.head_stride);
-        global_u16 *const vh = (global_u16 *)(a.v + (int64_t)t.head * a.head_stride);
+        global_u8 *const kh = (global_u8 *)(a.k + (int64_t)t.head * a.head_stride);
+        global_u8 *const vh = (global_u8 *)(a.v + (int64_t)t.head * a.head_stride);
         const int32_t *const pages = a.table + r.slot * a.table_stride;
         int32_t clear = least;  // keys that need no look at the mask; 0 once a page number is bad
 
@@ -629,27 +631,18 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         // pages they lie in.
         auto key_of = [&](int32_t k0) { return min(k0 + lane, most - 1); };
         auto page_of = [&](int32_t k0) { return pages[(uint32_t)key_of(k0) >> a.shift]; };
-        // where the keys lie, in elements
+        // where the keys lie
         auto place_of = [&](int32_t k0, int32_t id) -> uint64_t {
             const bool is = (uint32_t)id < (uint32_t)a.pages;
             if (!__all(is)) clear = 0;
             const uint32_t in = (uint32_t)key_of(k0) & place;
-            if constexpr (kRuns)
-                return (uint64_t)(is ? id : 0) * (uint32_t)a.page_stride + (in & ~15u) * (uint32_t)a.token_stride;
-            else
-                return (uint64_t)(is ? id : 0) * (uint64_t)a.page_stride + in * (uint64_t)a.token_stride;
+            return place_in<kRuns>(a, is ? id : 0, in);
         };
         u32x4 k_in[kLoads], v_in[kLoads];
         // piece i of this lane's share of a unit's K (or V)
-        auto load = [&](global_u16 *from, uint64_t at, int i) -> u32x4 {
-            if constexpr (kRuns) {
-                const int j = kApart * i + (kApart > 16 ? wave / 2 * 16 : 0);  // the 16 keys' first
-                const uint64_t begin = (uint32_t)__builtin_amdgcn_readlane((uint32_t)at, j) |
-                                       (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(at >> 32), j) << 32;
-                return *(global_u32x4 *)(from + begin + in_run);
-            } else {
-                return *(global_u32x4 *)(from + __shfl(at, kApart * i + key) + (8 * mine < a.dim ? 8 * mine : 0));
-            }
+        auto load = [&](global_u8 *from, uint64_t at, int i) -> u32x4 {
+            const int j = kApart * i + (kApart > 16 ? wave / 2 * 16 : 0);  // the 16 keys' first
+            return *(global_u32x4 *)(from + (kRuns ? lane_of(at, j) : __shfl(at, kApart * i + key)) + in_run);
         };
         auto store_k = [&](int buf, int i) {
             *reinterpret_cast<u32x4 *>(k_write + buf * kKUnit + i * kApart * kKStride) = k_in[i];
@@ -737,11 +730,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         // One half unit: its weights from s into w, the next scores into s1, the last weights w0 into O.
         // A step is the two products with one fragment of K or V, the reads of a fragment further on, and
         // a share of the softmax and of `more`; the compiler keeps to the steps' order, which feeds the matrix
-        // unit.  The first weights come before the first fragment has been read.
+        // unit.
         auto stage = [&](const f32x16 (&s)[kBlocks], u32x4 (&w)[kBlocks][2], const uint16_t *k, f32x16 (&s1)[kBlocks], const uint16_t *v,
                          const u32x4 (&w0)[kBlocks][2], auto more) {
-            constexpr int kFrags = kSteps + 2 * kCols, kAhead = 2, kWeights = 16 * kBlocks, kEach = kWeights / kFrags,
-                          kFirst = 2 * kEach;
+            constexpr int kFrags = kSteps + 2 * kCols, kAhead = 2, kWeights = 16 * kBlocks, kEach = kWeights / kFrags;
             constexpr int kTop = (16 + kFrags - kSteps - 2) / (kFrags - kSteps - 1);  // scores looked at in a step
             u32x4 frag[kAhead + 1];
             auto fetch = [&](int f) {
@@ -764,21 +756,18 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                 if (i % 2 == 0) odd = x;
                 else {
                     uint32_t y = pack<kHalf>(odd, x);
-                    asm volatile("" : "+v"(y));  // here, not where it is first used
+                    asm volatile("" : "+v"(y), "+v"(l[b]));  // here, not where they are first used
                     w[b][i / 8][i % 8 / 2] = y;
                 }
             };
 #pragma unroll
             for (int f = 0; f < kAhead; ++f) fetch(f);
 #pragma unroll
-            for (int e = 0; e < kFirst; ++e) weigh(e);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
             for (int f = 0; f < kFrags; ++f) {
                 if (f + kAhead < kFrags) fetch(f + kAhead);
                 multiply(f, 0);
 #pragma unroll
-                for (int e = kFirst + kEach * f; e < min(kWeights, kFirst + kEach * (f + 1)); ++e) weigh(e);
+                for (int e = 0; e < kEach; ++e) weigh(kEach * f + e);
                 if constexpr (kBlocks == 2) multiply(f, 1);
                 more(f);
                 if (f > kSteps) {
@@ -1002,7 +991,7 @@ hipError_t launch_join(const Attend &a, hipStream_t s) {
 
 // whether kRuns holds
 bool runs(const Attend &a) {
-    return a.shift >= 4 && a.page_stride <= INT32_MAX && a.token_stride <= INT32_MAX >> a.shift;
+    return a.shift >= 4 && a.page_stride <= INT32_MAX && a.token_stride <= (INT32_MAX / 2) >> a.shift;
 }
 
 template <int DP, int kBlocks, bool kHalf>

@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kBlock) k_store(Store a) {
 }
 
 // Rows that one block forks: a row's trips to memory follow one another, so a wave takes one row (us per
-// call, one launch and two: 4 rows 2.3 and 5.2, 256 rows 38 and 6.1).
+// call, one launch and two: 4 rows 2.6 and 4.6, 256 rows 38 and 8.7).
 constexpr int64_t kFew = kPlan / kWave;
 
 }  // namespace
