@@ -31,7 +31,7 @@ def _rows_of(where, name, t, B, dtype):
     stride, step = t.stride()
     if rows != B or (n > 1 and step != 1):
         raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on the GPU with contiguous rows")
-    return t.data_ptr(), stride if B > 1 else max(stride, n), n
+    return t.data_ptr(), stride if rows > 1 else max(stride, n), n
 
 
 _int = _float = _long = None  # torch's types, once torch is there
@@ -61,18 +61,23 @@ def _adjust(logits, stream, handle=None, rows=None, ids=None, tokens=None, lengt
     raw = rows_p = ids_p = None
     num_rows = stride = 0
     if handle is not None:
+        if rows is not None or handle._raw is None:
+            raise _bad(where, "a handle and mask rows" if handle._raw else "the handle is closed")
         if V < handle.vocab_size:
             raise _bad(where, f"logits have {V} columns, the vocabulary {handle.vocab_size} tokens")
         V, raw = handle.vocab_size, handle._raw
         ids_p = _int32(where, "node_ids", ids, B)
     elif rows is not None:
-        if ids is None:
-            raise _bad(where, "rows without row_ids")
+        if ids is None or rows.dim() != 2:
+            raise _bad(where, "rows must be [R, words] and come with row_ids")
         rows_p, stride, width = _rows_of(where, "rows", rows, rows.shape[0], _long)
         num_rows = rows.shape[0]
         if width < (V + 63) // 64:
             raise _bad(where, f"rows must have {(V + 63) // 64} words")
         ids_p = _int32(where, "row_ids", ids, B)
+        rows_p = rows_p or ids_p and ids_p & -8  # no rows at all have no memory, and none of it is read: nothing is valid
+    elif ids is not None:
+        raise _bad(where, "row_ids without rows")
     text_p, text_stride, history = (None, 0, 0) if tokens is None else _rows_of(where, "tokens", tokens, B, _int)
     floats = []
     for t in (repetition, frequency, presence):
@@ -130,13 +135,13 @@ class PageCache:
             raise _bad(where, "data must be a [2 * layers, pages, kv_heads, page_tokens, head_dim] bf16 or fp16 "
                               "tensor on the GPU")
         planes, pages, kv, page, dim = data.shape
-        if planes < 2 or planes % 2 or not data[0, 0].is_contiguous():
+        if planes < 2 or planes % 2 or pages < 1 or not data[0, 0].is_contiguous():
             raise _bad(where, "data needs a K and a V plane per layer and contiguous pages")
         if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_cuda or (
                 table.shape[1] > 1 and table.stride(1) != 1):
             raise _bad(where, "table must be a [slots, max_pages] int32 tensor on the GPU with contiguous rows")
         slots, width = table.shape
-        stride = max(table.stride(0), width)
+        stride = table.stride(0) if slots > 1 else width
         self._calls = _tam._calls_made if _int is not None else _ready()
         length_p = _int32(where, "length", length, slots)
         refs_p = _int32(where, "refs", refs, pages)
@@ -256,7 +261,8 @@ class PageCache:
                 or t.stride(2) != 1 or (heads is not None and t.shape[1] != heads)):
             raise _bad(where, f"{name} must be a [tokens, {heads or 'heads'}, {self.head_dim}] {self.data.dtype} tensor "
                               "on the GPU with contiguous vectors")
-        return t.data_ptr(), t.stride(0), t.stride(1)
+        # of a single token or head any stride will do
+        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
 
     def store(self, layer, k, v, offsets=None, slots=None, longest=None, stream=None):
         """K and V [tokens, kv_heads, head_dim] of the new tokens into their pages.  Row i's tokens are

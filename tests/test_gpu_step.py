@@ -196,6 +196,25 @@ def test_adjust_refusals(P):
     assert (x == 0).all()
 
 
+def test_adjust_mask_arguments(P):
+    """No mask rows at all: nothing is valid.  A mask given twice or by half, or of a closed handle, is refused."""
+    x = torch.zeros((2, 100), device="cuda")
+    rows = torch.full((3, 2), -1, dtype=torch.int64, device="cuda")
+    P.adjust_logits(x, rows=rows[:0].clone(), row_ids=ints([0, 1]))
+    assert (x == -math.inf).all()
+    x.zero_()
+    h = P.compile([b"ab", b"c"], [b"a", b"b", b"c", b'"'], device="cuda:0")
+    for call in (lambda: P.adjust_logits(x, row_ids=ints([0, 1])),
+                 lambda: P.adjust_logits(x, rows=rows[0], row_ids=ints([0, 1])),
+                 lambda: h.adjust_logits(ints([0, 1]), x, rows=rows)):
+        with pytest.raises(P.TamError):
+            call()
+    h.close()
+    with pytest.raises(P.TamError):
+        h.adjust_logits(ints([0, 1]), x, tokens=ints([[1], [2]]))
+    assert (x == 0).all()
+
+
 @pytest.mark.parametrize("flags", ["0", "FLAG_TAIL_LISTS", "FLAG_NO_TABLE", "FLAG_LAZY_ROWS"])
 def test_adjust_on_a_handle_is_edits_then_mask(P, flags):
     w = W.config(1)
@@ -429,6 +448,16 @@ def test_pages_refusals(P):
         P.PageCache(c.data, c.table, c.length[:2], c.refs)
     rc = P.lib().tam_pages_extend(ctypes.byref(c._pages), None, None, 1, None, None, None)
     assert rc == -1 and P.lib().tam_last_error()
+
+
+def test_pages_overlapping_tables(P):
+    c = page_cache(P, 6, 3, 8)
+    for table in (c.table[:1].expand(3, 8), c.table.view(-1).as_strided((3, 8), (4, 1))):
+        with pytest.raises(P.TamError):
+            P.PageCache(c.data, table, c.length, c.refs)
+    with pytest.raises(P.TamError):
+        P.PageCache(c.data[:, :0], c.table, c.length, c.refs[:0])
+    P.PageCache(c.data, c.table[:1], c.length[:1], c.refs)
 
 
 # ------------------------------------------------------- store and attention ----
@@ -724,3 +753,12 @@ def test_chunk_refusals(P):
     big = P.PageCache.empty(1, 1, 136, 4, 1, 4)
     with pytest.raises(P.TamError):
         big.attend(0, torch.zeros((1, 1, 136), dtype=torch.bfloat16, device="cuda"))
+
+
+def test_attend_one_token_of_any_stride(P):
+    """The strides of an axis of one element say nothing."""
+    s = Sequences(P, [50], [1], 8, 2, 64, 16, torch.bfloat16, seed=15)
+    out, lse = s.check()
+    q = s.q.contiguous().as_strided((1, 8, 64), (1, 64, 1))
+    got = s.cache.attend(1, q, offsets=s.offsets, return_lse=True)
+    assert torch.equal(got[0], out) and torch.equal(got[1], lse)
