@@ -3,8 +3,8 @@
 // Mathematics.  For a query q, o = sum_j w_j v_j / sum_j w_j with w_j = exp(scale (q k_j - m)),
 // for any m; in one pass over the keys m is the running maximum, and what was summed
 // under an older m is scaled when m grows.  Parts of the keys summed apart join the
-// same way.  m is let lag by up to 2^8 in w before it is moved, which the fp32 sums
-// and the 16-bit weights hold, so that the sums are scaled a few times per row and
+// same way.  m is let lag by up to 2^8 in w before it is moved (Range), which the fp32
+// sums and the 16-bit weights hold, so that the sums are scaled a few times per row and
 // not in each step.
 //
 // A tile is `tq` tokens of one row, times the heads that share a K/V head (their
@@ -254,7 +254,18 @@ __device__ inline uint32_t pack(float x, float y) {  // rounded to nearest, ties
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLag = 8.f;  // m may lag by this much, in powers of two
+
+// Where the weights lie, in powers of two: m is put kRaise under the highest score, and may lag until a
+// weight passes 2^kMost.  bf16 has fp32's range.  In fp16 what lies under 2^-24 is lost, and a long row of small
+// weights with it, so the highest weight is kept as high as the type allows, 2^7 to 2^15.
+template <bool kHalf>
+struct Range {
+    static constexpr float kRaise = kHalf ? 7.f : 0.f, kMost = kRaise + 8.f;
+    // where m goes for a highest score x
+    static __device__ float follow(float m, float x, float c) {
+        return fmaxf(m, kHalf ? x - fminf(kRaise / c, 1e38f) : x);  // (a tiny scale: no infinite step)
+    }
+};
 
 // In both kernels below, kRuns: 16 keys from a multiple of 16 lie side by side in one page (pages of 16
 // tokens or more, strides of 32 bits), so that its number and where they begin are the same for all lanes.
@@ -414,8 +425,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
             for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            if (__any((top - m) * c > kLag)) {  // NaN (both -inf): no
-                const float now = fmaxf(m, top);
+            if (__any((top - m) * c > Range<kHalf>::kMost)) {  // NaN (both -inf): no
+                const float now = Range<kHalf>::follow(m, top, c);
                 const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - now) * c);
                 m = now;
                 l *= keep;
@@ -715,10 +726,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
                     const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[b]), __float_as_uint(top[b]), false, false);
-                    const float now = fmaxf(m[b], fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+                    const float now = Range<kHalf>::follow(m[b], fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])), c);
                     const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
                     m[b] = now;
-                    bound[b] = now + kLag / c;
+                    bound[b] = now + Range<kHalf>::kMost / c;
                     mc[b] = now == -INFINITY ? 0.f : now * c;
                     l[b] *= keep;
 #pragma unroll

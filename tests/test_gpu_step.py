@@ -762,3 +762,25 @@ def test_attend_one_token_of_any_stride(P):
     q = s.q.contiguous().as_strided((1, 8, 64), (1, 64, 1))
     got = s.cache.attend(1, q, offsets=s.offsets, return_lse=True)
     assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+
+
+@pytest.mark.parametrize("x", [1, 70])
+def test_attend_small_fp16_weights(P, x):
+    """One key far above many: weights of 2^-27 are under fp16's range, and their sum is not."""
+    n, dim, scale = 60000, 64, 64 ** -0.5
+    s = Sequences(P, [n], [x], 4, 2, dim, 16, torch.float16, seed=16)
+    k, v = s.k[0], s.v[0]
+    s.q.fill_(1)
+    k.zero_()
+    k[77] = 27 * math.log(2) * 8 / 64  # its score
+    v.fill_(1)
+    v[77] = 0
+    pos = torch.arange(n, device="cuda")
+    to = s.cache.table[0, pos // 16].long()
+    s.cache.data[2][to, :, pos % 16] = k
+    s.cache.data[3][to, :, pos % 16] = v
+    out, lse = s.cache.attend(1, s.q, offsets=s.offsets, scale=scale, return_lse=True)
+    want, wl, _, ltol = s.reference(scale)
+    # the highest weight is 2^7 or more and all are held to 2^-25: n 2^-32 in the sum, beside what weights and output round
+    assert ((out.double() - want).abs() <= 2.0 ** -10 * want + n * 2.0 ** -32).all()
+    assert ((lse.double() - wl).abs() <= ltol).all()
