@@ -784,3 +784,34 @@ def test_attend_small_fp16_weights(P, x):
     # the highest weight is 2^7 or more and all are held to 2^-25: n 2^-32 in the sum, beside what weights and output round
     assert ((out.double() - want).abs() <= 2.0 ** -10 * want + n * 2.0 ** -32).all()
     assert ((lse.double() - wl).abs() <= ltol).all()
+
+
+def test_beams_example(P):
+    """The example's beams, found step by step, have the scores that whole sequences get in one chunk."""
+    import examples.beams as E
+    vocab = E.vocabulary()
+    h = P.compile(E.STRINGS, vocab, device="cuda:0")
+    ends = torch.tensor([t.endswith(b'"') for t in vocab], device="cuda")
+    model = E.Decoder(len(vocab))
+    prompts = [list(b"a prompt"), list(b"and one that is longer than a page of the cache")]
+    found, cache = E.search(model, h, ends, prompts, width=4)
+    assert (cache.refs == 0).all() and (cache.length == 0).all()
+    for prompt, beams in zip(prompts, found):
+        assert beams and beams == sorted(beams, key=lambda x: -x[0])
+        for score, tokens in beams:
+            assert b"".join(vocab[t] for t in tokens)[:-1] in E.STRINGS
+            T, n = len(prompt) + len(tokens) - 1, len(tokens)
+            whole = ints(prompt + tokens)
+            one = P.PageCache.empty(len(model.layers), 2, 64, 8, 1, 8)
+            one.extend(ints([0]), ints([T]))
+            logits = model(whole[:T], one, ints([0]), ints([0, T]), T)[len(prompt) - 1:]
+            nodes = [ints([0])]
+            for t in tokens[:-1]:
+                nodes.append(h.advance(nodes[-1], ints([t])))
+            at = ints(range(len(prompt), len(prompt) + n))
+            h.adjust_logits(torch.cat(nodes), logits, tokens=whole.expand(n, -1).contiguous(), length=at,
+                            prompt=torch.full_like(at, len(prompt)), presence=torch.full((n,), 0.3, device="cuda"))
+            want = torch.log_softmax(logits.float(), 1)[torch.arange(n), tokens].sum()
+            # logits of size 1 from bf16 layers, a few roundings of 2^-8 each
+            assert abs(float(want) - score) <= 0.03 * n
+    h.close()
