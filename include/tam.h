@@ -500,7 +500,7 @@ enum { TAM_MAX_HISTORY = (1 << 19) - 1, TAM_MAX_BIASES = (1 << 12) - 1 };
 
 /*
  * tam_adjust_logits -- penalties for repeated tokens, biases and the grammar's
- * mask on logits, in place, each logit read and written at most once.  With x
+ * mask on logits, in place.  With x
  * the logit of row b and token v, n the occurrences of v in tokens[b] after the
  * prompt, and "seen" if v occurs anywhere in the row's text:
  *     x = x > 0 ? x / repetition[b] : x * repetition[b]     if seen
@@ -517,8 +517,8 @@ enum { TAM_MAX_HISTORY = (1 << 19) - 1, TAM_MAX_BIASES = (1 << 12) - 1 };
  *              >= ceil(V/64), 8-byte aligned; bits >= V are not looked at): row b
  *              has the mask row ids[b], or nothing valid when ids[b] is outside [0, num_rows);
  *   neither    (both null; ids is not read) every token is valid.
- * A full table (and `rows`) is masked and edited in one pass; the other
- * representations of a handle are edited first and then masked.
+ * A full table (and `rows`) is masked and edited in one pass or, for large batches,
+ * as the other representations of a handle always are, edited first and then masked.
  *
  *   ids         device int32[B] with a mask.
  *   edits       NULL = none.

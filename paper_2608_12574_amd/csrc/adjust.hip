@@ -1,6 +1,6 @@
 // Penalties, biases and the grammar's mask on [B, V] logits, in place.
 //
-// A block takes one span of one row's vocabulary.  A span without a valid token (most of
+// k_adjust: a block takes one span of one row's vocabulary.  A span without a valid token (most of
 // a constrained row's) is -inf, and nothing else is looked at.  Else the block counts
 // the row's text in a table in LDS with one word per token of the span (an integer sum,
 // so the order of the atomics does not matter), and then goes through the span's logits
@@ -8,12 +8,15 @@
 // whose valid tokens are not named is left alone or merged, and only the named
 // tokens are computed.  So a logit is read and written at most once, and the text
 // is all that is read beside the mask; each block of a row reads that again, from L2.
+//
+// k_edit: without a mask, or before it, only the named tokens are gone to.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <climits>
 
 #include "step.hpp"
+#include "tam_internal.hpp"
 
 namespace tam {
 namespace {
@@ -28,7 +31,7 @@ static_assert(TAM_MAX_HISTORY == kCount && TAM_MAX_BIASES == (1 << (32 - kEntry)
 
 // Threads and tokens of a block, with a mask and without.  The text is read again by each block of a row,
 // but more threads hold more of the chip back while one waits: us per call of 256 bf16 rows over
-// V = 262,144 (texts of 2,048, a mask) with 256 threads and 4,096 tokens 47, 512 and 8,192 50, 512 and
+// V = 262,144 (texts of 2,048, a mask) with 256 threads and 4,096 tokens 47 (45 since), 512 and 8,192 50, 512 and
 // 4,096 68, 1,024 and 8,192 78, 128 and 2,048 56; of 64 fp32 rows over V = 128,255 (texts of 8,192, no
 // mask) 21, 18, 21, 20, 26.
 constexpr int kMaskThreads = 256, kMaskSpan = 4096, kFreeThreads = 512, kFreeSpan = 8192;
@@ -82,7 +85,7 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
                                                      int64_t V, T *__restrict__ logits, int64_t row_stride) {
     constexpr int N = Lane<T>::n;
     __shared__ __align__(16) uint32_t tab[kSpan];
-    __shared__ uint32_t bits[kSpan / 32 + 2];
+    __shared__ uint32_t bits[kSpan / 32 + 2], named_bits[kSpan / 32];
     const int64_t b = blockIdx.y;
     T *row = logits + b * row_stride;
     // chunk k of the row covers elements [k N - a, (k + 1) N - a), a being the row's
@@ -107,6 +110,7 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
     const Edits ed{e.repetition ? e.repetition[b] : 1.f, e.frequency ? e.frequency[b] : 0.f,
                    e.presence ? e.presence[b] : 0.f, e.bias ? e.bias + b * e.bias_stride : nullptr};
     for (int i = threadIdx.x * 4; i < kSpan; i += kThreads * 4) *reinterpret_cast<u32x4 *>(&tab[i]) = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < kSpan / 32; i += kThreads) named_bits[i] = 0;
     bool any = true;  // some token of the span is valid
     if (rows) {
         const int64_t r = ids[b];
@@ -133,12 +137,16 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
     constexpr int kChunks = kSpan / (N * kThreads);
     uint32_t valid[kChunks], inside[kChunks];
     u32x4 x[kChunks];
+    const bool inner = v0 >= 0 && span == kSpan;
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
         const int o = (threadIdx.x + k * kThreads) * N;
-        inside[k] = o < span ? kAll : 0u;  // elements of the chunk that the row has
-        if (v0 + o < 0) inside[k] &= kAll << (int)-(v0 + o);
-        if (o < span && o + N > span) inside[k] &= kAll >> (o + N - span);
+        inside[k] = kAll;  // elements of the chunk that the row has
+        if (!inner) {
+            if (o >= span) inside[k] = 0;
+            if (v0 + o < 0) inside[k] &= kAll << (int)-(v0 + o);
+            if (o < span && o + N > span) inside[k] &= kAll >> (o + N - span);
+        }
         valid[k] = !rows ? kAll : any ? (bits[o >> 5] >> (o & 31)) & kAll : 0u;
         u32x4 *at = reinterpret_cast<u32x4 *>(row + (v0 + o));
         if (inside[k] == kAll) {
@@ -156,17 +164,22 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
             for (int i = threadIdx.x; i < (int)e.biases; i += kThreads) {
                 const int32_t v = named[i];
                 const uint32_t o = (uint32_t)v - (uint32_t)v0;
-                if (v >= 0 && o < (uint32_t)span) atomicMax(&tab[o], (uint32_t)(i + 1) << kEntry);
+                if (o < (uint32_t)span) {
+                    atomicMax(&tab[o], (uint32_t)(i + 1) << kEntry);
+                    atomicOr(&named_bits[o >> 5], 1u << (o & 31));
+                }
             }
             __syncthreads();  // the entry's field is final before the counts are added below it
         }
         auto count = [&](int32_t v, int i) {
+            // (an id below 0 falls outside, or before the row's first element, where nothing is edited)
             const uint32_t o = (uint32_t)v - (uint32_t)v0;
-            if (i < len && v >= 0 && o < (uint32_t)span) {
+            if (o < (uint32_t)span && i < len) {
                 if (i < prompt)
                     atomicOr(&tab[o], kSeen);
                 else
                     atomicAdd(&tab[o], 1u);
+                atomicOr(&named_bits[o >> 5], 1u << (o & 31));
             }
         };
 #pragma unroll
@@ -185,16 +198,7 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
         const int o = (threadIdx.x + k * kThreads) * N;
         const bool whole = inside[k] == kAll;
         if (!inside[k] || (whole && !valid[k])) continue;
-        uint32_t named = 0;
-        if (valid[k]) {
-#pragma unroll
-            for (int i = 0; i < N; i += 4) {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(&tab[o + i]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) named |= (w[j] != 0u) << (i + j);
-            }
-            named &= valid[k];
-        }
+        const uint32_t named = (named_bits[o >> 5] >> (o & 31)) & valid[k];
         const uint32_t edit = (named | ~valid[k]) & inside[k];
         if (!edit) continue;
         if (whole) {
@@ -226,6 +230,133 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
     }
 }
 
+// The edits alone.  A block gathers a row's text and list of biases in a hash table in LDS (a token's word is
+// as above), then goes through the table's tokens: only their logits are read and written, and their mask words
+// before, where there is a mask.  Those scattered lines bound it.  us per call without a mask, against k_adjust: 64 fp32
+// rows over V = 128,256 with texts of 1,024 5.7 and 10.7; 256 bf16 rows over V = 262,144 with texts of 256 6.5 and 35, of
+// 2,048 15 and 52, of 8,192 49 and 84.  Where texts name a large part of the vocabulary, going through all
+// of it is faster: 64 fp32 rows over V = 128,255 with texts of 8,192 24 and 17.
+constexpr int kEditThreads = 1024;
+constexpr int kEditMost = 12288;  // entries of text and biases: three quarters of the largest table
+constexpr int kEditShare = 16;    // and no more than the vocabulary's 16th part
+constexpr int kEditLine = 64;     // neighbouring tokens, a line or two of logits, that go to one block of the row's
+// Up to eight blocks share a row while there are no more of them than this (us per call with 1 and 8 blocks a row:
+// 16 rows 5.4 and 5.0, 64 rows 5.7 and 6.3).
+constexpr int kEditBlocks = 128;
+// With a mask, from this many bytes of logits on: the edits of the valid tokens first, then the mask's own pass, whose
+// blocks then wait for no text (us per call, in one pass and in two: 256 bf16 rows over V = 262,144 with texts of 2,048
+// 45 and 38, over 128,256 with texts of 256 24 and 21; 64 fp32 rows over 128,256 14 and 17).
+constexpr int64_t kApartBytes = 48ll << 20;
+
+template <typename T, int kEach>
+__global__ void __launch_bounds__(kEditThreads) k_edit(const uint64_t *__restrict__ rows, int64_t num_rows, int64_t rows_stride,
+                                                       const int32_t *__restrict__ ids, tam_edits e, int64_t V,
+                                                       T *__restrict__ logits, int64_t row_stride) {
+    constexpr int kSlots = kEach * kEditThreads, kLog = __builtin_ctz(kSlots);
+    extern __shared__ __align__(16) uint32_t table[];  // ids, then words
+    uint32_t *const id_of = table, *const word_of = table + kSlots;
+    const int64_t b = blockIdx.y;
+    const uint64_t *mask = nullptr;  // with a mask: the row's, to leave out tokens that become -inf
+    if (rows) {
+        const int64_t r = ids[b];
+        if (r < 0 || r >= num_rows) return;
+        mask = rows + r * rows_stride;
+    }
+    const uint32_t parts = gridDim.x - 1, part = blockIdx.x;  // (a power of two) - 1; this block's
+    T *row = logits + b * row_stride;
+    constexpr int kBatch = 4;
+    constexpr uint32_t kNone = 0xFFFFFFFFu;  // no token
+    const int32_t *text = e.tokens + b * e.tokens_stride;
+    const int history = e.tokens ? (int)e.history : 0;
+    int32_t ids0[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+        const int i = threadIdx.x + j * kEditThreads;
+        ids0[j] = i < history ? text[i] : -1;
+    }
+    const int len = e.length ? min(max(e.length[b], 0), history) : history;
+    const int prompt = e.prompt ? e.prompt[b] : 0;
+    const Edits ed{e.repetition ? e.repetition[b] : 1.f, e.frequency ? e.frequency[b] : 0.f,
+                   e.presence ? e.presence[b] : 0.f, e.bias ? e.bias + b * e.bias_stride : nullptr};
+#pragma unroll
+    for (int i = threadIdx.x * 4; i < kSlots; i += kEditThreads * 4) {
+        *reinterpret_cast<u32x4 *>(&id_of[i]) = u32x4{kNone, kNone, kNone, kNone};
+        *reinterpret_cast<u32x4 *>(&word_of[i]) = u32x4{0, 0, 0, 0};
+    }
+    __syncthreads();
+    auto ours = [&](int32_t v) { return v >= 0 && v < V && ((uint32_t)v / kEditLine & parts) == part; };
+    // a token's place: there are more places than entries, so a free one is found
+    auto place = [&](int32_t v) {
+        uint32_t at = ((uint32_t)v * 0x9E3779B1u) >> (32 - kLog);
+        while (true) {
+            const uint32_t was = atomicCAS(&id_of[at], kNone, (uint32_t)v);
+            if (was == kNone || was == (uint32_t)v) return at;
+            at = (at + 1) & (uint32_t)(kSlots - 1);
+        }
+    };
+    if (e.bias_ids) {
+        const int32_t *named = e.bias_ids + b * e.bias_stride;
+        for (int i = threadIdx.x; i < (int)e.biases; i += kEditThreads) {
+            const int32_t v = named[i];
+            if (ours(v)) atomicMax(&word_of[place(v)], (uint32_t)(i + 1) << kEntry);
+        }
+        __syncthreads();  // the entry's field is final before the counts are added below it
+    }
+    auto count = [&](int32_t v, int i) {
+        if (i < len && ours(v)) {
+            uint32_t *const w = &word_of[place(v)];
+            if (i < prompt)
+                atomicOr(w, kSeen);
+            else
+                atomicAdd(w, 1u);
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) count(ids0[j], threadIdx.x + j * kEditThreads);
+    for (int i0 = threadIdx.x + kEditThreads * kBatch; i0 < len; i0 += kEditThreads * kBatch) {
+        int32_t v[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) v[j] = i0 + j * kEditThreads < len ? text[i0 + j * kEditThreads] : -1;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) count(v[j], i0 + j * kEditThreads);
+    }
+    __syncthreads();
+    uint32_t v[kEach];
+    uint64_t word[kEach];
+    T x[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        v[j] = id_of[threadIdx.x + j * kEditThreads];
+        if (mask) word[j] = v[j] != kNone ? mask[v[j] / 64] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        if (mask && !(word[j] >> (v[j] % 64) & 1)) v[j] = kNone;
+        if (v[j] != kNone) x[j] = row[v[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        if (v[j] == kNone) continue;
+        u32x4 y{0, 0, 0, 0};
+        uint32_t raw = 0;
+        __builtin_memcpy(&raw, &x[j], sizeof(T));
+        y[0] = raw;
+        Lane<T>::put(y, 0, edited(Lane<T>::get(y, 0), word_of[threadIdx.x + j * kEditThreads], ed));
+        raw = y[0];
+        __builtin_memcpy(&row[v[j]], &raw, sizeof(T));
+    }
+}
+
+// the edits of the rows after the first n
+void next_rows(tam_edits &e, int64_t n) {
+    if (e.tokens) e.tokens += n * e.tokens_stride;
+    if (e.bias_ids) e.bias_ids += n * e.bias_stride, e.bias += n * e.bias_stride;
+    for (const int32_t **p : {&e.length, &e.prompt})
+        if (*p) *p += n;
+    for (const float **p : {&e.repetition, &e.frequency, &e.presence})
+        if (*p) *p += n;
+}
+
 template <typename T, int kThreads, int kSpan>
 hipError_t launch(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, const int32_t *ids, tam_edits e,
                   int64_t B, int64_t V, T *logits, int64_t row_stride, hipStream_t s) {
@@ -237,20 +368,54 @@ hipError_t launch(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, c
                            rows_stride, ids ? ids + r0 : nullptr, e, V, logits + r0 * row_stride, row_stride);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
-        if (e.tokens) e.tokens += n * e.tokens_stride;
-        if (e.bias_ids) e.bias_ids += n * e.bias_stride, e.bias += n * e.bias_stride;
-        for (const int32_t **p : {&e.length, &e.prompt})
-            if (*p) *p += n;
-        for (const float **p : {&e.repetition, &e.frequency, &e.presence})
-            if (*p) *p += n;
+        next_rows(e, n);
     }
     return hipSuccess;
+}
+
+template <typename T, int kEach>
+hipError_t launch_edit(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, const int32_t *ids, tam_edits e,
+                       int64_t B, int64_t V, T *logits, int64_t row_stride, hipStream_t s) {
+    unsigned parts = 1;
+    while (parts < 8 && B * parts * 2 <= kEditBlocks) parts *= 2;
+    for (int64_t r0 = 0; r0 < B; r0 += 65535) {
+        const int64_t n = std::min<int64_t>(B - r0, 65535);
+        hipLaunchKernelGGL((k_edit<T, kEach>), dim3(parts, (unsigned)n), dim3(kEditThreads), 8 * kEach * kEditThreads, s, rows,
+                           num_rows, rows_stride, ids ? ids + r0 : nullptr, e, V, logits + r0 * row_stride, row_stride);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+        next_rows(e, n);
+    }
+    return hipSuccess;
+}
+
+// Whether a masked call edits first and masks then.  (Mask rows of a wider stride have words that are not there
+// behind the last one; the mask pass looks at its neighbour only where logits are not 16-byte aligned.)
+template <typename T>
+bool apart(int64_t rows_stride, int64_t B, int64_t V, const T *logits, int64_t row_stride) {
+    const bool aligned = (reinterpret_cast<uintptr_t>(logits) | (uint64_t)(row_stride * sizeof(T))) % 16 == 0;
+    return B * V * (int64_t)sizeof(T) >= kApartBytes && (aligned || rows_stride == (V + 63) / 64);
 }
 
 template <typename T>
 hipError_t launch_type(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, const int32_t *ids,
                        const tam_edits &e, int64_t B, int64_t V, void *logits, int64_t row_stride, hipStream_t s) {
     T *p = static_cast<T *>(logits);
+    const int64_t entries = e.history + (e.bias_ids ? e.biases : 0);
+    if (entries <= kEditMost && entries <= V / kEditShare && (!rows || apart(rows_stride, B, V, p, row_stride))) {
+        // tables of 4,096, 8,192 or 16,384 places, at most three quarters of them taken
+        const auto edit = entries <= 3 * kEditThreads   ? launch_edit<T, 4>
+                          : entries <= 6 * kEditThreads ? launch_edit<T, 8>
+                                                        : launch_edit<T, 16>;
+        const hipError_t err = edit(rows, num_rows, rows_stride, ids, e, B, V, p, row_stride, s);
+        if (err != hipSuccess || !rows) return err;
+        DevTables t{};
+        t.table = const_cast<uint64_t *>(rows);
+        t.Wp = rows_stride;
+        t.N = num_rows;
+        t.V = V;
+        return launch_apply(t, ids, B, logits, sizeof(T) == 2 ? TAM_DTYPE_BF16 : TAM_DTYPE_FP32, row_stride, s);
+    }
     return rows ? launch<T, kMaskThreads, kMaskSpan>(rows, num_rows, rows_stride, ids, e, B, V, p, row_stride, s)
                 : launch<T, kFreeThreads, kFreeSpan>(rows, num_rows, rows_stride, ids, e, B, V, p, row_stride, s);
 }

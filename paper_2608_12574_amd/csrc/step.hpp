@@ -14,7 +14,7 @@ namespace tam {
 void api_begin();                                           // clears the thread's message
 tam_status api_fail(tam_status st, const std::string &msg);  // sets it
 
-// edits and mask rows in one pass; rows null: every token valid
+// edits and mask rows; rows null: every token valid
 hipError_t launch_adjust(const uint64_t *rows, int64_t num_rows, int64_t rows_stride, const int32_t *ids,
                          const tam_edits &e, int64_t B, int64_t V, void *logits, int dtype, int64_t row_stride,
                          hipStream_t s);

@@ -103,7 +103,7 @@ def _adjust(logits, stream, handle=None, rows=None, ids=None, tokens=None, lengt
 def adjust_logits(logits, tokens=None, length=None, prompt=None, repetition=None, frequency=None, presence=None,
                   bias_ids=None, bias=None, rows=None, row_ids=None, stream=None):
     """Penalties for repeated tokens, biases and a mask on ``logits`` [B, V] (fp32 or
-    bf16), in place and in one pass.  A token ``v`` of row ``b`` that occurs in
+    bf16), in place.  A token ``v`` of row ``b`` that occurs in
     ``tokens[b, :length[b]]`` has its logit divided (multiplied where it is not
     positive) by ``repetition[b]``; ``frequency[b]`` is subtracted for each time it occurs
     after the first ``prompt[b]`` tokens, ``presence[b]`` once if it does; then the

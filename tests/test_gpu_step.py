@@ -156,6 +156,21 @@ def test_adjust_lists(P, history, biases):
     check_adjusted(P, 2, 5003, torch.float32, 4, history=history, biases=biases, masked=False)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,V,history,biases", [(3, 150000, 3000, 100), (2, 262144, 12000, 200), (20, 50001, 900, 30),
+                                                (200, 20000, 64, 5), (9, 16 * 45, 40, 5), (1, 400000, 6100, 0),
+                                                (2, 262144, 12200, 90)])
+def test_adjust_few_of_many(P, dtype, B, V, history, biases):
+    """Texts that name a small part of the vocabulary, no mask."""
+    check_adjusted(P, B, V, dtype, V, pad=3, offset=1, history=history, biases=biases, masked=False)
+
+
+@pytest.mark.parametrize("B,V,pad,offset,dtype", [(50, 262144, 0, 0, torch.float32), (97, 262143, 1, 0, torch.bfloat16),
+                                                  (97, 262143, 2, 3, torch.bfloat16)])
+def test_adjust_large_batches(P, B, V, pad, offset, dtype):
+    check_adjusted(P, B, V, dtype, 5, pad=pad, offset=offset, history=300, biases=20)
+
+
 @pytest.mark.parametrize("name", ["length", "prompt", "repetition", "frequency", "presence"])
 def test_adjust_parts_left_out(P, name):
     check_adjusted(P, 4, 1000, torch.float32, 8, **{name: None})
@@ -579,6 +594,21 @@ def test_attend_long_rows(P, heads, kv, dim, page):
     Sequences(P, [20011, 3, 4097], [1, 1, 1], heads, kv, dim, page, torch.bfloat16, seed=2).check(longest=1)
     Sequences(P, [9000, 50, 1023], [9, 2, 17], heads, kv, dim, page, torch.float16, seed=3).check()
     Sequences(P, [2000, 700], [700, 700], heads, kv, dim, page, torch.bfloat16, seed=4).check()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads,kv,dim", HEADS)
+def test_attend_long_chunks(P, dtype, heads, kv, dim):
+    """Tiles of 256 rows, the last ones of a row partly filled; and of 128 for mostly short rows."""
+    for page, lens, chunks in ((16, [700, 333, 64], [610, 300, 64]), (4, [300], [290]), (32, [500, 9, 40, 90, 0, 3], [310, 1, 1, 1, 0, 3])):
+        Sequences(P, lens, chunks, heads, kv, dim, page, dtype, seed=page + 1).check()
+
+
+@pytest.mark.parametrize("chunk", [5, 17])
+def test_attend_join_of_many_pieces(P, chunk):
+    """A few rows over keys enough for every block: each tile's parts lie in many of them."""
+    Sequences(P, [50000, 33000], [chunk, 3], 16, 2, 128, 16, torch.bfloat16, seed=17).check()
+    Sequences(P, [40001], [chunk], 6, 2, 64, 16, torch.float16, seed=18).check()
 
 
 def test_attend_rows_without_keys(P):
