@@ -59,9 +59,9 @@ struct Attend {
 };
 
 // The tile in whose middle a block's piece begins.
-struct Cut {
-    int32_t is;       // this is the first cut of a tile
-    int32_t more;     // the blocks after this one that have parts of the tile
+struct alignas(16) Cut {
+    int32_t is;       // a tile is cut here, behind its first unit
+    int32_t back, more;  // the cuts of the tile before this one, and after it
     int32_t token, n, head, heads;  // the tile's first token and query head, and how many
 };
 
@@ -219,9 +219,12 @@ __device__ inline Share share_of(const Attend &a, const Tile &t, int64_t left) {
 // What the block's piece begins with, for k_join.
 template <int kKeys>
 __device__ inline void note(const Attend &a, int64_t block, const Row &r, const Tile &t, int64_t piece) {
-    if (threadIdx.x == 0)
-        a.cuts[block] = Cut{t.rest - a.extra >= kKeys && t.rest - a.extra - piece < kKeys, (int32_t)((t.keys - t.rest - 1) / piece),
-                            r.first + t.first, t.n, t.head * (a.heads / a.kv_heads) + t.part * a.group, t.heads};
+    if (threadIdx.x != 0) return;
+    // (a tile has fewer than 2^31 keys)
+    const uint32_t keys = (uint32_t)min(piece, (int64_t)INT32_MAX), rest = (uint32_t)(t.keys - t.rest - 1);
+    const int32_t behind = (int32_t)(t.rest - a.extra - kKeys);
+    a.cuts[block] = Cut{behind >= 0, behind >= 0 ? (int32_t)((uint32_t)behind / keys) : 0, (int32_t)(rest / keys),
+                        r.first + t.first, t.n, t.head * (a.heads / a.kv_heads) + t.part * a.group, t.heads};
 }
 
 // ------------------------------------------------------------------ products ---
@@ -617,9 +620,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                 q[b][s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(src + d) : u32x4{0, 0, 0, 0};
             }
         }
-        // keys that every query of the wave's sees
-        const int32_t least = (kWaveRows * (wave + 1) - 1) / t.heads < t.n
-                                  ? max(0, min(r.base + t.first + kWaveRows * wave / t.heads + 1, all)) : 0;
+        // keys that every query of the wave's sees (what rows past the tile's come to is written nowhere)
+        const int32_t least = kWaveRows * wave / t.heads < t.n
+                                  ? max(0, min(r.base + t.first + kWaveRows * wave / t.heads + 1, all)) : INT_MAX;
         f32x16 o[kBlocks][kCols], sa[kBlocks], sb[kBlocks];
         u32x4 pa[kBlocks][2], pb[kBlocks][2];
         // m and m c; the score above which m follows; sums of weights; the highest of the last scores (this lane's)
@@ -897,20 +900,22 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
 // ---------------------------------------------------------------------- join ---
 
 // Partial sums of the tiles that a cut goes through.  blockIdx.x is the cut after
-// block x, and works on the tile it is the first cut of; the blocks of one x share its rows.
-// A group of threads takes a row; where the tile is in many pieces, all groups share a
-// row's pieces and their sums meet in LDS.  The partial sums' bytes bound it.
+// block x; the blocks of a tile's first cut share its rows, a group of threads to a row.
+// Where the tile is in many pieces the blocks of all its cuts do, and the groups of one share
+// a row's pieces, whose sums meet in LDS.  Where there are few tiles the chain of reads bounds it, else the partial sums' bytes.
 template <int DP, int kRows, bool kHalf>
 __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     constexpr int kLanes = DP / 4, kGroups = kThreads / kLanes;
     __shared__ float part[kGroups][DP];
     __shared__ float part_l[kGroups];
-    const int64_t cut = blockIdx.x + 1;
-    const Cut t = a.cuts[cut];
-    if (!t.is) return;
-    const int rows = t.n * t.heads, each = (rows + gridDim.y - 1) / gridDim.y;
-    const int row0 = blockIdx.y * each, row1 = min(row0 + each, rows);
-    const int64_t last = cut + t.more;  // the block with the tile's end
+    const Cut t = a.cuts[blockIdx.x + 1];
+    const bool many = t.back + t.more >= 4;  // six pieces or more
+    if (!t.is || (!many && t.back)) return;
+    const int64_t cut = blockIdx.x + 1 - t.back, last = blockIdx.x + 1 + t.more;  // the tile's first cut, and its last
+    const int rows = t.n * t.heads, shares = (many ? t.back + t.more + 1 : 1) * gridDim.y;
+    const int each = rows <= shares ? 1 : (rows + shares - 1) / shares;
+    const int row0 = min((t.back * (int)gridDim.y + (int)blockIdx.y) * each, rows), row1 = min(row0 + each, rows);
+    if (row0 == row1) return;
     const float c = a.scale * kLog2e;
     const float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP;
     const int lane = threadIdx.x % kLanes, g = threadIdx.x / kLanes;
@@ -925,7 +930,7 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
                 u32x2{pack<kHalf>(x[0] * inv, x[1] * inv), pack<kHalf>(x[2] * inv, x[3] * inv)};
         if (a.lse && lane == 0) a.lse[token * a.heads + head] = l > 0.f ? mx * a.scale + logf(l) : -INFINITY;
     };
-    if (last - cut < 4) {
+    if (!many) {
         for (int row = row0 + g; row < row1; row += kGroups) {
             float mx = -INFINITY;
             for (int64_t i = cut - 1; i <= last; ++i) mx = fmaxf(mx, ml[(slot_of(i) * kRows + row) * 2]);
@@ -986,7 +991,9 @@ Shape shape_of(const tam_chunk &c, int64_t heads) {
     const int64_t longest = c.longest ? std::min(c.longest, c.tokens) : c.tokens;
     const int64_t rows = longest * (heads / c.kv_heads);
     if (rows <= 16) return Shape{16, kNarrowKeys, 512, kNarrowKeys};
-    if (rows <= 128) return Shape{128, kWideKeys, 512, 2 * kWideKeys};
+    // a batch of mostly short rows fills tiles of 128 rows better (us per call with 128 and 256: 40 chunks of up to
+    // 200 tokens, 74 rows on average, 50 and 63; 24 of 265 rows on average, heads of 64, 46 and 41)
+    if (rows <= 128 || c.tokens * (heads / c.kv_heads) <= 128 * c.rows) return Shape{128, kWideKeys, 512, 2 * kWideKeys};
     return Shape{256, kWideKeys, 256, 5 * kWideKeys};
 }
 
