@@ -4,9 +4,11 @@
 // tables that lie there, so a decode step needs no answer from the host.  A page
 // is free when its count is 0; there is no list of free pages to keep in step.  A
 // call that takes pages finds the lowest free ones by a pass over the counts
-// (4 bytes per page).  The decisions are one block's work (k_extend, k_plan: a few
-// dependent trips to memory and prefix sums over the rows or the pages); the page
-// contents are moved by a launch of their own over the whole chip.
+// (4 bytes per page).  The decisions are one block's work (k_extend, 6.0 us for 4 rows and
+// 7.4 for 256; k_plan, 6.7 us for 2,048 pages): a few dependent trips to memory and
+// prefix sums over the rows or the pages bound them.  The page contents are moved by a
+// launch of their own over the whole chip, which its bytes bound (k_copy: 134 MB read and
+// written in 27 us, 537 MB in 113 us, 4.8 to 4.9 TB/s; a large copy reaches 5.1).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -123,7 +125,7 @@ __global__ void __launch_bounds__(kPlan) k_fork_few(Tables t, const int32_t *slo
 // page what the rows say of it; the free pages taken.
 struct ExtendWork {
     int32_t *start;   // [n] pages needed by the rows before
-    int32_t *last;    // [n] the partly filled last page, or -1
+    int32_t *last;    // [n] the partly filled last page, or -1; then the row's tokens
     int32_t *src;     // [n] the page copied, or -1
     int32_t *dst;     // [n] to where
     int32_t *sharers; // [pages] rows that write on in the page
@@ -131,74 +133,125 @@ struct ExtendWork {
     int32_t *got;     // [pages] free pages, ascending
 };
 
+// kOne: a row per thread (at most kPlan of them), which keeps it in registers, and the rows of a page are
+// found in a hash table in LDS instead of the scratch (us of a step of 4 and of 256 beams: 12.3 and 41.6, with
+// !kOne 14.2 and 44).
+template <bool kOne>
 __global__ void __launch_bounds__(kPlan) k_extend(Tables t, const int32_t *__restrict__ slots,
                                                   const int32_t *__restrict__ counts, int64_t n, int32_t *info,
                                                   ExtendWork w) {
     const int64_t mask = ((int64_t)1 << t.shift) - 1;
+    constexpr int kPlaces = kOne ? 2 * kPlan : 1;
+    __shared__ int32_t page_of[kPlaces], sharers_of[kPlaces], final_of[kPlaces];
+    // A row, and the pages it needs.
+    struct Row {
+        int64_t slot, len, count;  // slot < 0: nothing to do
+        int32_t page, start, copy;  // the partly filled last page or -1; pages needed by the rows before; copied
+    };
+    auto row_at = [&](int64_t i) {
+        Row r{-1, 0, 0, -1, 0, 0};
+        if (i >= n) return r;
+        const int64_t slot = slots[i], count = counts[i];
+        if (!t.slot_ok(slot) || count <= 0) return r;
+        r.slot = slot;
+        r.count = count;
+        r.len = t.tokens(slot);
+        if (r.len & mask) r.page = t.table[slot * t.stride + (r.len >> t.shift)];
+        if (!t.page_ok(r.page)) r.page = -1;
+        return r;
+    };
+    // the first counts of the search for free pages, which wait for nothing
+    int32_t refs0[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t p = 4 * (int64_t)threadIdx.x + j;
+        refs0[j] = p < t.pages ? t.refs[p] : 1;
+    }
     // rows that write on in a page
-    for (int64_t i = threadIdx.x; i < n; i += kPlan) {
-        const int64_t slot = slots[i];
-        int32_t page = -1;
-        if (t.slot_ok(slot) && counts[i] > 0) {
-            const int64_t len = t.tokens(slot);
-            if (len & mask) page = t.table[slot * t.stride + (len >> t.shift)];
-            if (!t.page_ok(page)) page = -1;
+    Row mine{-1, 0, 0, -1, 0, 0};
+    if (kOne) mine = row_at(threadIdx.x);
+    int32_t holders = 0, at_place = 0;
+    if constexpr (kOne) {
+        if (mine.page >= 0) holders = t.refs[mine.page];
+        for (int i = threadIdx.x; i < kPlaces; i += kPlan) page_of[i] = final_of[i] = -1, sharers_of[i] = 0;
+        __syncthreads();
+        if (mine.page >= 0) {
+            uint32_t at = ((uint32_t)mine.page * 0x9E3779B1u) >> 21;  // (there are twice as many places as rows)
+            while (true) {
+                const int32_t was = atomicCAS(&page_of[at], -1, mine.page);
+                if (was == -1 || was == mine.page) break;
+                at = (at + 1) % kPlaces;
+            }
+            atomicAdd(&sharers_of[at], 1);
+            atomicMax(&final_of[at], (int32_t)threadIdx.x);
+            at_place = (int32_t)at;
         }
-        w.last[i] = page;
-        if (page >= 0) w.sharers[page] = 0, w.final_[page] = -1;
-    }
-    __syncthreads();
-    for (int64_t i = threadIdx.x; i < n; i += kPlan) {
-        const int32_t page = w.last[i];
-        if (page >= 0) {
-            atomicAdd(&w.sharers[page], 1);
-            atomicMax(&w.final_[page], (int32_t)i);
+        __syncthreads();
+    } else {
+        for (int64_t i = threadIdx.x; i < n; i += kPlan) {
+            const int32_t page = row_at(i).page;
+            w.last[i] = page;
+            if (page >= 0) w.sharers[page] = 0, w.final_[page] = -1;
         }
+        __syncthreads();
+        for (int64_t i = threadIdx.x; i < n; i += kPlan) {
+            const int32_t page = w.last[i];
+            if (page >= 0) {
+                atomicAdd(&w.sharers[page], 1);
+                atomicMax(&w.final_[page], (int32_t)i);
+            }
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    // pages needed, row after row
+    // pages needed, row after row; rows too long for the table in the sum's upper bits
+    constexpr int kWide = 48;
     int64_t need = 0, narrow = 0;
     for (int64_t i0 = 0; i0 < n; i0 += kPlan) {
         const int64_t i = i0 + threadIdx.x;
-        int64_t mine = 0;
+        Row r = kOne ? mine : row_at(i);
+        int64_t pages = 0;
         bool wide = false;
-        if (i < n) {
-            const int64_t slot = slots[i];
-            const int32_t page = w.last[i];
-            bool copy = false;
-            if (t.slot_ok(slot) && counts[i] > 0) {
-                // device-scope reads: the block's own atomics wrote these words
-                if (page >= 0)
-                    copy = t.refs[page] != __hip_atomic_load(&w.sharers[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ||
-                           __hip_atomic_load(&w.final_[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (int32_t)i;
-                const int64_t len = t.tokens(slot), total = t.held(len + counts[i]);
-                wide = total > t.max_pages;
-                mine = (int64_t)copy + total - t.held(len);
-            }
-            w.src[i] = copy ? page : -1;
+        if (r.slot >= 0) {
+            if (kOne && r.page >= 0)
+                r.copy = holders != sharers_of[at_place] || final_of[at_place] != (int32_t)i;
+            if (!kOne && r.page >= 0)  // device-scope reads: the block's own atomics wrote these words
+                r.copy = t.refs[r.page] != __hip_atomic_load(&w.sharers[r.page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ||
+                         __hip_atomic_load(&w.final_[r.page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (int32_t)i;
+            const int64_t total = t.held(r.len + r.count);
+            wide = total > t.max_pages;
+            pages = r.copy + total - t.held(r.len);
         }
         int64_t sum;
-        const int64_t at = need + scan(mine, &sum);
-        if (i < n) w.start[i] = (int32_t)min(at, (int64_t)INT_MAX);
-        need += sum;
-        scan(wide ? 1 : 0, &sum);
-        narrow += sum;
+        const int64_t before = scan(pages | (int64_t)wide << kWide, &sum) & ((1ll << kWide) - 1);
+        r.start = (int32_t)min(need + before, (int64_t)INT_MAX);
+        need += sum & ((1ll << kWide) - 1);
+        narrow += sum >> kWide;
+        if (kOne) {
+            mine = r;
+        } else if (i < n) {
+            w.start[i] = r.start;
+            w.src[i] = r.copy ? r.page : -1;
+            w.last[i] = (int32_t)r.len;
+        }
     }
     // the free pages, in order
     int64_t nfree = 0;
     for (int64_t p0 = 0; p0 < t.pages; p0 += 4 * kPlan) {
         const int64_t p = p0 + 4 * (int64_t)threadIdx.x;
         bool is[4];
-        int64_t mine = 0, sum;
+        int64_t own = 0, sum;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            is[j] = p + j < t.pages && t.refs[p + j] <= 0;
-            mine += is[j];
+            is[j] = p + j < t.pages && (p0 ? t.refs[p + j] : refs0[j]) <= 0;
+            own += is[j];
         }
-        int64_t at = nfree + scan(mine, &sum);
+        int64_t at = nfree + scan(own, &sum);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (is[j]) w.got[at++] = (int32_t)(p + j);
+            if (is[j]) {
+                if (at < need) w.got[at] = (int32_t)(p + j);
+                ++at;
+            }
         nfree += sum;
     }
     const bool done = need <= nfree && narrow == 0;
@@ -218,30 +271,32 @@ __global__ void __launch_bounds__(kPlan) k_extend(Tables t, const int32_t *__res
     const int lane = threadIdx.x % kWave;
     for (int64_t i0 = 0; i0 < n; i0 += kPlan) {
         const int64_t i = i0 + threadIdx.x;
-        int64_t slot = -1, first = 0, total = 0;
-        int32_t start = 0;
-        if (i < n && t.slot_ok(slots[i]) && counts[i] > 0) {
-            slot = slots[i];
-            start = w.start[i];
-            const int32_t src = w.src[i];
-            const int64_t len = t.tokens(slot);
-            total = t.held(len + counts[i]);
-            first = t.held(len) - (src >= 0);
-            if (src >= 0) {
-                w.dst[i] = w.got[start];
-                atomicSub(&t.refs[src], 1);
+        Row r = mine;
+        if (kOne && i < n) w.src[i] = r.copy ? r.page : -1;
+        if (!kOne) {  // as it was counted above
+            r = Row{-1, 0, 0, -1, 0, 0};
+            if (i < n && t.slot_ok(slots[i]) && counts[i] > 0)
+                r = Row{slots[i], w.last[i], counts[i], w.src[i], w.start[i], w.src[i] >= 0};
+        }
+        int64_t first = 0, total = 0;
+        if (r.slot >= 0) {
+            total = t.held(r.len + r.count);
+            first = t.held(r.len) - r.copy;
+            if (r.copy) {
+                w.dst[i] = w.got[r.start];
+                atomicSub(&t.refs[r.page], 1);
             }
-            t.length[slot] = (int32_t)(len + counts[i]);
+            t.length[r.slot] = (int32_t)(r.len + r.count);
             for (int64_t j = first; j < min(total, first + kAlone); ++j) {
-                const int32_t page = w.got[start + (j - first)];
-                t.table[slot * t.stride + j] = page;
+                const int32_t page = w.got[r.start + (j - first)];
+                t.table[r.slot * t.stride + j] = page;
                 t.refs[page] = 1;
             }
         }
         for (uint64_t rest = __ballot(total - first > kAlone); rest; rest &= rest - 1) {
             const int of = __ffsll((unsigned long long)rest) - 1;
-            const int64_t s = __shfl(slot, of), f = __shfl(first, of), m = __shfl(total, of);
-            const int32_t at = __shfl(start, of);
+            const int64_t s = __shfl(r.slot, of), f = __shfl(first, of), m = __shfl(total, of);
+            const int32_t at = __shfl(r.start, of);
             for (int64_t j = f + kAlone + lane; j < m; j += kWave) {
                 const int32_t page = w.got[at + (j - f)];
                 t.table[s * t.stride + j] = page;
@@ -420,7 +475,8 @@ hipError_t launch_pages_extend(const tam_pages &c, const int32_t *slots, const i
                                int32_t *info, void *work, hipStream_t s) {
     int32_t *p = static_cast<int32_t *>(work);
     const ExtendWork w{p, p + n, p + 2 * n, p + 3 * n, p + 4 * n, p + 4 * n + c.num_pages, p + 4 * n + 2 * c.num_pages};
-    hipLaunchKernelGGL(k_extend, dim3(1), dim3(kPlan), 0, s, tables_of(c), slots, counts, n, info, w);
+    hipLaunchKernelGGL(n <= kPlan ? k_extend<true> : k_extend<false>, dim3(1), dim3(kPlan), 0, s, tables_of(c), slots, counts,
+                       n, info, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.page_tokens == 1) return e;  // pages of one token are never partly filled
     return launch_copy(c, w.src, w.dst, n, nullptr, s);
