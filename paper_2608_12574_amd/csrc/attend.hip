@@ -96,9 +96,8 @@ __device__ inline Row row_at(const Attend &a, int64_t i) {
     return r;
 }
 
-// the same for a row number that all lanes share
-__device__ inline Row shared_row(const Attend &a, int64_t i) {
-    Row r = row_at(a, i);
+// a row that is the same in all lanes, to the compiler too
+__device__ inline Row uniform(Row r) {
     r.n = uniform(r.n);
     r.base = uniform(r.base);
     r.first = uniform(r.first);
@@ -123,6 +122,7 @@ __device__ inline int64_t row_keys(const Attend &a, const Row &r) {
 struct Place {
     int64_t row, total;   // the row; keys on the whole line
     int64_t rest;         // keys of the row before this place
+    Row r;                // what the row is
 };
 
 // Where piece number `share` (this block's) begins, and the keys of a piece.  All threads of
@@ -130,11 +130,16 @@ struct Place {
 __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
     __shared__ int64_t sums[kThreads / kWave];
     __shared__ int64_t found[2];
+    __shared__ Row found_row;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int64_t per = (a.rows + kThreads - 1) / kThreads, lo = threadIdx.x * per, hi = min(lo + per, a.rows);
     const int64_t heads = (int64_t)a.kv_heads * a.parts;
     int64_t mine = 0;
-    for (int64_t i = lo; i < hi; ++i) mine += heads * row_keys(a, row_at(a, i));
+    Row r{};
+    for (int64_t i = lo; i < hi; ++i) {
+        r = row_at(a, i);
+        mine += heads * row_keys(a, r);
+    }
     int64_t upto = mine;
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) {
@@ -152,22 +157,28 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
         p.total += sums[w];
     }
     p.total = uniform(p.total);
-    *piece = max((int64_t)1, (p.total + (int64_t)a.blocks * a.unit - 1) / ((int64_t)a.blocks * a.unit)) * a.unit;
+    const int shift = __builtin_ctz((uint32_t)a.blocks * (uint32_t)a.unit);  // (both are powers of two)
+    *piece = max((int64_t)1, (p.total + (1ll << shift) - 1) >> shift) * a.unit;
     const int64_t at = share * *piece;
     if (at >= upto - mine && at < upto) {  // one thread: walk its rows
         int64_t rest = at - (upto - mine);
         int64_t i = lo;
-        for (; i < hi; ++i) {
-            const int64_t u = heads * row_keys(a, row_at(a, i));
-            if (rest < u) break;
-            rest -= u;
+        if (per > 1) {
+            for (; i < hi; ++i) {
+                r = row_at(a, i);
+                const int64_t u = heads * row_keys(a, r);
+                if (rest < u) break;
+                rest -= u;
+            }
         }
         found[0] = i;
         found[1] = rest;
+        found_row = r;
     }
     __syncthreads();
     p.row = uniform(found[0]);
     p.rest = uniform(found[1]);
+    p.r = uniform(found_row);
     return p;
 }
 
@@ -293,7 +304,9 @@ __device__ inline uint64_t lane_of(uint64_t x, int of) {
 // step's while this one is computed, and LDS only joins the waves' sums at the end.
 // S^T = K Q^T leaves each lane the weights of one query, for the same eight keys that it
 // then holds as the second factor of O^T = V^T P^T: no weight changes lanes.  V's columns
-// are paired in registers (v_perm).
+// are paired in registers (v_perm).  64 rows of up to 8,192 tokens, 8 K/V heads of 128: 226 us,
+// 5.7 TB/s of K and V.  One row of 700 tokens: 7 us, of which 2 find the cut and 3 more pass
+// until the first keys are there.
 constexpr int kNarrowKeys = 128;
 
 template <int DP, bool kHalf, bool kRuns>
@@ -325,10 +338,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
     int64_t left = whole_piece;
     const float c = a.scale * kLog2e;
     while (left > 0) {
-        const Row r = shared_row(a, p.row);
-        const int64_t in_row = row_keys(a, r) * a.kv_heads * a.parts;
-        if (p.rest >= in_row) {
-            ++p.row;
+        const Row r = p.r;
+        if (p.rest >= row_keys(a, r) * a.kv_heads * a.parts) {
+            p.r = uniform(row_at(a, ++p.row));
             p.rest = 0;
             continue;
         }
@@ -551,7 +563,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 // since with 32 the reads of K and V from LDS take as long as the products.  So that the
 // matrix unit does not wait for the softmax, a half unit (32 keys) is in three stages at
 // once: the products of the next half's scores and of the last half's weights with V run
-// beside this half's exponentials.
+// beside this half's exponentials.  4,096 tokens over 16,384 keys, 32 heads of 128: 910 us, 1.06
+// PFLOP/s (a bf16 product of 8,192^3 by the library: 1.23), the matrix units busy in 48 cycles of
+// 100 at the 2.1 GHz that the power leaves.  Where K and V's bytes bound it a unit takes 2.1
+// us, 4 TB/s.
 constexpr int kWideKeys = 64;
 
 template <int DP, int kBlocks, bool kHalf, bool kRuns>
@@ -590,10 +605,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
     const uint32_t in_run = 2 * ((kRuns ? (uint32_t)(key % 16) * (uint32_t)a.token_stride : 0) + (8 * mine < a.dim ? 8 * mine : 0));
 
     while (left > 0) {
-        const Row r = shared_row(a, p.row);
-        const int64_t in_row = row_keys(a, r) * a.kv_heads * a.parts;
-        if (p.rest >= in_row) {
-            ++p.row;
+        const Row r = p.r;
+        if (p.rest >= row_keys(a, r) * a.kv_heads * a.parts) {
+            p.r = uniform(row_at(a, ++p.row));
             p.rest = 0;
             continue;
         }
@@ -902,7 +916,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
 // Partial sums of the tiles that a cut goes through.  blockIdx.x is the cut after
 // block x; the blocks of a tile's first cut share its rows, a group of threads to a row.
 // Where the tile is in many pieces the blocks of all its cuts do, and the groups of one share
-// a row's pieces, whose sums meet in LDS.  Where there are few tiles the chain of reads bounds it, else the partial sums' bytes.
+// a row's pieces, whose sums meet in LDS.  Where there are few tiles the chain of reads bounds
+// it, else the partial sums' bytes.
+// us per call: 3.9 for one row of 700 tokens, 7.7 for 4 tiles in 512 pieces (12 with the first
+// cut's blocks alone), 15.5 for 255 cuts of 256 rows of 128 (70 MB).
 template <int DP, int kRows, bool kHalf>
 __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     constexpr int kLanes = DP / 4, kGroups = kThreads / kLanes;
