@@ -389,12 +389,12 @@ hipError_t launch_edit(const uint64_t *rows, int64_t num_rows, int64_t rows_stri
     return hipSuccess;
 }
 
-// Whether a masked call edits first and masks then.  (Mask rows of a wider stride have words that are not there
-// behind the last one; the mask pass looks at its neighbour only where logits are not 16-byte aligned.)
+// Whether the mask can have a pass of its own.  (That looks at the neighbour of a row's last mask word where logits
+// are not 16-byte aligned, and rows of a wider stride may have nothing there.)
 template <typename T>
-bool apart(int64_t rows_stride, int64_t B, int64_t V, const T *logits, int64_t row_stride) {
+bool own_pass(int64_t rows_stride, int64_t V, const T *logits, int64_t row_stride) {
     const bool aligned = (reinterpret_cast<uintptr_t>(logits) | (uint64_t)(row_stride * sizeof(T))) % 16 == 0;
-    return B * V * (int64_t)sizeof(T) >= kApartBytes && (aligned || rows_stride == (V + 63) / 64);
+    return aligned || rows_stride == (V + 63) / 64;
 }
 
 template <typename T>
@@ -402,13 +402,16 @@ hipError_t launch_type(const uint64_t *rows, int64_t num_rows, int64_t rows_stri
                        const tam_edits &e, int64_t B, int64_t V, void *logits, int64_t row_stride, hipStream_t s) {
     T *p = static_cast<T *>(logits);
     const int64_t entries = e.history + (e.bias_ids ? e.biases : 0);
-    if (entries <= kEditMost && entries <= V / kEditShare && (!rows || apart(rows_stride, B, V, p, row_stride))) {
-        // tables of 4,096, 8,192 or 16,384 places, at most three quarters of them taken
-        const auto edit = entries <= 3 * kEditThreads   ? launch_edit<T, 4>
-                          : entries <= 6 * kEditThreads ? launch_edit<T, 8>
-                                                        : launch_edit<T, 16>;
-        const hipError_t err = edit(rows, num_rows, rows_stride, ids, e, B, V, p, row_stride, s);
-        if (err != hipSuccess || !rows) return err;
+    const bool few = entries <= kEditMost && entries <= V / kEditShare, large = B * V * (int64_t)sizeof(T) >= kApartBytes;
+    if (rows ? (!entries || (few && large)) && own_pass(rows_stride, V, p, row_stride) : few) {
+        if (entries) {
+            // tables of 4,096, 8,192 or 16,384 places, at most three quarters of them taken
+            const auto edit = entries <= 3 * kEditThreads   ? launch_edit<T, 4>
+                              : entries <= 6 * kEditThreads ? launch_edit<T, 8>
+                                                            : launch_edit<T, 16>;
+            const hipError_t err = edit(rows, num_rows, rows_stride, ids, e, B, V, p, row_stride, s);
+            if (err != hipSuccess || !rows) return err;
+        }
         DevTables t{};
         t.table = const_cast<uint64_t *>(rows);
         t.Wp = rows_stride;

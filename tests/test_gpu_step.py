@@ -171,6 +171,13 @@ def test_adjust_large_batches(P, B, V, pad, offset, dtype):
     check_adjusted(P, B, V, dtype, 5, pad=pad, offset=offset, history=300, biases=20)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,V,pad,offset", [(9, 4096, 0, 0), (5, 4101, 3, 0), (4, 8191, 2, 5), (6, 200, 0, 1)])
+def test_adjust_mask_alone(P, dtype, B, V, pad, offset):
+    for seed in range(2):
+        check_adjusted(P, B, V, dtype, seed, pad=pad, offset=offset, history=None, biases=0)
+
+
 @pytest.mark.parametrize("name", ["length", "prompt", "repetition", "frequency", "presence"])
 def test_adjust_parts_left_out(P, name):
     check_adjusted(P, 4, 1000, torch.float32, 8, **{name: None})
