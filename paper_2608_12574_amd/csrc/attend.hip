@@ -518,12 +518,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const float mw = tops[w][out_row];
-                if (mw > -INFINITY) lsum += weights[w][out_row] * __builtin_amdgcn_exp2f((mw - mx) * c);
+                lsum += weights[w][out_row] * (mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - mx) * c));  // (NaN stays)
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) sum[j] += joint[w][out_row][d0 + j];
             }
             if (whole) {
-                const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+                const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
                 const int64_t token = r.first + t.first + out_tok;
                 const int64_t head = t.head * (a.heads / a.kv_heads) + t.part * a.group + out_h;
                 uint16_t *dst = a.out + token * a.out_token + head * a.out_head + d0;
@@ -534,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
                     if constexpr (kCols == 8) *reinterpret_cast<u32x4 *>(dst) = u32x4{y[0], y[1], y[2], y[3]};
                     else *reinterpret_cast<u32x2 *>(dst) = u32x2{y[0], y[1]};
                 }
-                if (a.lse && d0 == 0) a.lse[token * a.heads + head] = lsum > 0.f ? mx * a.scale + logf(lsum) : -INFINITY;
+                if (a.lse && d0 == 0) a.lse[token * a.heads + head] = lsum == 0.f ? -INFINITY : mx * a.scale + logf(lsum);
             } else {
                 float *dst = a.sums + (at * kRows + out_row) * DP + d0;
 #pragma unroll
@@ -878,7 +878,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
             const int row = kWaveRows * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
             if (tok >= t.n) continue;
             if (whole) {
-                const float inv = sum > 0.f ? 1.f / sum : 0.f;
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
                 const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
                 uint16_t *dst = a.out + token * a.out_token + head * a.out_head;
 #pragma unroll
@@ -892,7 +892,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                                       pack<kHalf>(o[b][d][i + 2] * inv, o[b][d][i + 3] * inv)};
                     }
                 if (a.lse && half == 0)
-                    a.lse[token * a.heads + head] = sum > 0.f ? m[b] * a.scale + logf(sum) : -INFINITY;
+                    a.lse[token * a.heads + head] = sum == 0.f ? -INFINITY : m[b] * a.scale + logf(sum);
             } else {
                 float *dst = a.sums + (at * kRows + row) * DP;
 #pragma unroll
@@ -939,13 +939,13 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     // the first piece begins the tile, the others go on with it
     auto slot_of = [&](int64_t i) { return i < cut ? 2 * i + 1 : 2 * i; };
     auto write = [&](int row, f32x4 x, float l, float mx) {
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         const int tok = row / t.heads, h = row - tok * t.heads;
         const int64_t token = t.token + tok, head = t.head + h;
         if (4 * lane < a.dim)
             *reinterpret_cast<u32x2 *>(a.out + token * a.out_token + head * a.out_head + 4 * lane) =
                 u32x2{pack<kHalf>(x[0] * inv, x[1] * inv), pack<kHalf>(x[2] * inv, x[3] * inv)};
-        if (a.lse && lane == 0) a.lse[token * a.heads + head] = l > 0.f ? mx * a.scale + logf(l) : -INFINITY;
+        if (a.lse && lane == 0) a.lse[token * a.heads + head] = l == 0.f ? -INFINITY : mx * a.scale + logf(l);
     };
     if (!many) {
         for (int row = row0 + g; row < row1; row += kGroups) {

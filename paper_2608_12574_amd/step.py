@@ -147,7 +147,7 @@ class PageCache:
         refs_p = _int32(where, "refs", refs, pages)
         self.data, self.table, self.length, self.refs = data, table, length, refs
         self.layers, self.kv_heads, self.page_tokens, self.head_dim = planes // 2, kv, page, dim
-        self._torch = torch
+        self._torch, self._device = torch, data.device
         size = data.element_size()
         self._pages = Pages(data.data_ptr(), planes, data.stride(0) * size, data.stride(1) * size, kv * page * dim * size,
                             pages, page, table.data_ptr(), slots, width, stride, length_p, refs_p)
@@ -176,9 +176,9 @@ class PageCache:
         nothing still running on another stream holds it."""
         torch = self._torch
         if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.data.device)
+            return torch.empty(shape, dtype=dtype, device=self._device)
         with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=dtype, device=self.data.device)
+            return torch.empty(shape, dtype=dtype, device=self._device)
 
     def _work(self, stream):
         return self._empty(self._work_bytes, self._torch.uint8, stream)

@@ -636,6 +636,21 @@ def test_attend_rows_without_keys(P):
     cut.compare(out[keep], lse[keep], 64 ** -0.5)
 
 
+@pytest.mark.parametrize("chunks", [[1, 1], [40, 3], [200, 90]])
+def test_attend_nan_stays_in_its_row(P, chunks):
+    """A query or a key that is not a number: its rows say so, the others do not change."""
+    s = Sequences(P, [700, 3000], chunks, 8, 2, 128, 16, torch.bfloat16, seed=19)
+    out, lse = s.check()
+    s.q[0, 3, 5] = float("nan")
+    s.cache.data[2][int(s.cache.table[1, 20]), 1, 3] = float("nan")  # K of the second sequence, heads 4 to 7
+    got, glse = s.cache.attend(1, s.q, offsets=s.offsets, return_lse=True)
+    bad = torch.zeros(lse.shape, dtype=torch.bool, device="cuda")
+    bad[0, 3] = True
+    bad[chunks[0]:, 4:] = True
+    assert torch.isnan(glse[bad]).all() and torch.isnan(got[bad]).all()
+    assert torch.equal(glse[~bad], lse[~bad]) and torch.equal(got[~bad], out[~bad])
+
+
 def test_attend_slots_and_page_ids(P):
     s = Sequences(P, [33, 70, 5], [4, 9, 1], 8, 2, 64, 16, torch.bfloat16, seed=6, slots=[7, 0, 3])
     out, lse = s.check()
