@@ -313,14 +313,14 @@ struct Pool {
     int64_t planes, plane_stride, page_stride, page_bytes;
 };
 
-// Item k is plane k % planes of pair k / planes; a block per item, grid-stride.  The
+// Item k is plane k % planes of pair k / planes; a block per item, `blocks` of them, grid-stride.  The
 // number of pairs is n, or *count where that is smaller.
 template <typename V>
-__global__ void __launch_bounds__(kBlock) k_copy(Pool p, const int32_t *__restrict__ src,
-                                                 const int32_t *__restrict__ dst, int64_t n, const int32_t *count) {
+__device__ void copy_pages(const Pool &p, const int32_t *__restrict__ src, const int32_t *__restrict__ dst, int64_t n,
+                           const int32_t *count, int64_t block, int64_t blocks) {
     if (count) n = min(n, (int64_t)*count);
     const int64_t items = n * p.planes, words = p.page_bytes / (int64_t)sizeof(V);
-    for (int64_t k = blockIdx.x; k < items; k += gridDim.x) {
+    for (int64_t k = block; k < items; k += blocks) {
         const int64_t pair = k / p.planes, plane = k - pair * p.planes;
         if (src[pair] < 0) continue;
         const V *from = reinterpret_cast<const V *>(p.data + plane * p.plane_stride + src[pair] * p.page_stride);
@@ -329,19 +329,34 @@ __global__ void __launch_bounds__(kBlock) k_copy(Pool p, const int32_t *__restri
     }
 }
 
+template <typename V>
+__global__ void __launch_bounds__(kBlock) k_copy(Pool p, const int32_t *__restrict__ src, const int32_t *__restrict__ dst,
+                                                 int64_t n) {
+    copy_pages<V>(p, src, dst, n, nullptr, blockIdx.x, gridDim.x);
+}
+
 constexpr int64_t kCopyBlocks = 256 * 16;
 
-hipError_t launch_copy(const tam_pages &c, const int32_t *src, const int32_t *dst, int64_t n, const int32_t *count,
-                       hipStream_t s) {
-    if (c.planes == 0 || c.page_bytes == 0 || n == 0) return hipSuccess;
-    const Pool p{static_cast<uint8_t *>(c.data), c.planes, c.plane_stride, c.page_stride, c.page_bytes};
-    const uint64_t any = reinterpret_cast<uintptr_t>(c.data) | (uint64_t)c.plane_stride | (uint64_t)c.page_stride |
-                         (uint64_t)c.page_bytes;
-    const dim3 grid((unsigned)std::min<int64_t>(n > kCopyBlocks ? kCopyBlocks : n * c.planes, kCopyBlocks));
-    if (any % 16 == 0)
-        hipLaunchKernelGGL((k_copy<u32x4>), grid, dim3(kBlock), 0, s, p, src, dst, n, count);
-    else
-        hipLaunchKernelGGL((k_copy<uint8_t>), grid, dim3(kBlock), 0, s, p, src, dst, n, count);
+Pool pool_of(const tam_pages &c) {
+    return Pool{static_cast<uint8_t *>(c.data), c.planes, c.plane_stride, c.page_stride, c.page_bytes};
+}
+
+// whether pages can be moved in pieces of 16 bytes
+bool in_pieces(const tam_pages &c) {
+    return (reinterpret_cast<uintptr_t>(c.data) | (uint64_t)c.plane_stride | (uint64_t)c.page_stride | (uint64_t)c.page_bytes) % 16 == 0;
+}
+
+// blocks for up to n pages
+int64_t copy_blocks(const tam_pages &c, int64_t n) {
+    if (c.planes == 0 || c.page_bytes == 0) return 0;
+    return n > kCopyBlocks ? kCopyBlocks : std::min(n * c.planes, kCopyBlocks);
+}
+
+hipError_t launch_copy(const tam_pages &c, const int32_t *src, const int32_t *dst, int64_t n, hipStream_t s) {
+    const int64_t blocks = copy_blocks(c, n);
+    if (!blocks) return hipSuccess;
+    hipLaunchKernelGGL(in_pieces(c) ? k_copy<u32x4> : k_copy<uint8_t>, dim3((unsigned)blocks), dim3(kBlock), 0, s, pool_of(c), src,
+                       dst, n);
     return hipGetLastError();
 }
 
@@ -383,8 +398,13 @@ __global__ void __launch_bounds__(kPlan) k_plan(Tables t, int32_t *info, int32_t
     }
 }
 
-__global__ void __launch_bounds__(kBlock) k_renumber(Tables t, const int32_t *__restrict__ moved) {
+// The tables' new numbers, a block per slot, and beside them the pages' contents (one launch: 2 us less than two).
+template <typename V>
+__global__ void __launch_bounds__(kBlock) k_move(Tables t, const int32_t *__restrict__ moved, Pool p,
+                                                 const int32_t *__restrict__ src, const int32_t *__restrict__ dst, int64_t n,
+                                                 const int32_t *count) {
     const int64_t slot = blockIdx.x;
+    if (slot >= t.slots) return copy_pages<V>(p, src, dst, n, count, slot - t.slots, gridDim.x - t.slots);
     const int64_t held = t.held(t.tokens(slot));
     for (int64_t j = threadIdx.x; j < t.max_pages; j += kBlock) {
         int32_t *at = t.table + slot * t.stride + j;
@@ -480,19 +500,19 @@ hipError_t launch_pages_extend(const tam_pages &c, const int32_t *slots, const i
                        n, info, w);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.page_tokens == 1) return e;  // pages of one token are never partly filled
-    return launch_copy(c, w.src, w.dst, n, nullptr, s);
+    return launch_copy(c, w.src, w.dst, n, s);
 }
 
 hipError_t launch_pages_compact(const tam_pages &c, int32_t *info, int32_t *moved, void *work, hipStream_t s) {
     int32_t *src = static_cast<int32_t *>(work), *dst = src + c.num_pages;
     hipLaunchKernelGGL(k_plan, dim3(1), dim3(kPlan), 0, s, tables_of(c), info, moved, src, dst);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (c.slots > 0 && c.max_pages > 0) {
-        hipLaunchKernelGGL(k_renumber, dim3((unsigned)c.slots), dim3(kBlock), 0, s, tables_of(c), moved);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    return launch_copy(c, src, dst, c.num_pages / 2, info + 1, s);
+    const int64_t blocks = c.slots + copy_blocks(c, c.num_pages / 2);
+    if (!blocks) return hipSuccess;
+    hipLaunchKernelGGL(in_pieces(c) ? k_move<u32x4> : k_move<uint8_t>, dim3((unsigned)blocks), dim3(kBlock), 0, s, tables_of(c), moved,
+                       pool_of(c), src, dst, c.num_pages / 2, info + 1);
+    return hipGetLastError();
 }
 
 hipError_t launch_pages_store(const tam_chunk &c, const void *k_new, int64_t k_token, int64_t k_head,
