@@ -563,8 +563,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 // since with 32 the reads of K and V from LDS take as long as the products.  So that the
 // matrix unit does not wait for the softmax, a half unit (32 keys) is in three stages at
 // once: the products of the next half's scores and of the last half's weights with V run
-// beside this half's exponentials.  4,096 tokens over 16,384 keys, 32 heads of 128: 910 us, 1.06
-// PFLOP/s (a bf16 product of 8,192^3 by the library: 1.23), the matrix units busy in 48 cycles of
+// beside this half's exponentials.  4,096 tokens over 16,384 keys, 32 heads of 128: 905 to 955 us
+// by the card, 1.01 to 1.06 PFLOP/s (a bf16 product of 8,192^3 by the library: 1.23), the matrix units busy in 48 cycles of
 // 100 at the 2.1 GHz that the power leaves.  Where K and V's bytes bound it a unit takes 2.1
 // us, 4 TB/s.
 constexpr int kWideKeys = 64;

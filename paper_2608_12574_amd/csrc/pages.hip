@@ -7,8 +7,8 @@
 // (4 bytes per page).  The decisions are one block's work (k_extend, 6.0 us for 4 rows and
 // 7.4 for 256; k_plan, 6.7 us for 2,048 pages): a few dependent trips to memory and
 // prefix sums over the rows or the pages bound them.  The page contents are moved by a
-// launch of their own over the whole chip, which its bytes bound (k_copy: 134 MB read and
-// written in 27 us, 537 MB in 113 us, 4.8 to 4.9 TB/s; a large copy reaches 5.1).
+// launch of their own over the whole chip, which its bytes bound (k_copy: 126 MB read and
+// written in 27 us, k_move: 537 MB in 113 us, 4.7 TB/s; a large copy reaches 5.1).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
