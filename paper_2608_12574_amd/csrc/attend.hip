@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 // (kBlocks 2), or the bytes of K and V (kBlocks 1, for fewer rows).
 // K and V go through LDS, two units of each; the next one's bytes are on their way in
 // registers while this one is computed.  Keys lie apart in LDS by their bytes and 16 (K) or
-// 32 (V) more, which leaves no bank asked twice and every read at a fixed distance from
+// 32 (V) more, which leaves few banks asked twice (6 cycles of 100) and every read at a fixed distance from
 // one address.  As above S^T = K Q^T, O^T = V^T P^T (V read from LDS by columns),
 // so the weights stay in their lanes.  A wave has its matrix unit to itself, and 64 rows,
 // since with 32 the reads of K and V from LDS take as long as the products.  So that the
