@@ -293,6 +293,45 @@ __device__ inline uint64_t place_in(const Attend &a, uint32_t page, uint32_t in)
         return (uint64_t)page * (uint64_t)(2 * a.page_stride) + in * (uint64_t)(2 * a.token_stride);
 }
 
+// V of a key that some of a tile's queries see and others do not must be finite in the products, where what a query does not see
+// has the weight 0.  So what is not finite there becomes 0 (`only_finite`), and is added to the queries that see it
+// when the tile's sums are done (`not_finite`); a tile looks at its last tokens' keys for such, and hardly ever finds one.
+
+// Bits 15 and 31 of it, over all words of `of`: some half is not finite.
+template <bool kHalf>
+__device__ inline uint32_t exponents(uint32_t of, uint32_t before) {
+    constexpr uint32_t kAll = kHalf ? 0x7C007C00u : 0x7F807F80u, kOne = kHalf ? 0x04000400u : 0x00800080u;
+    return before | ((of & kAll) + kOne);
+}
+
+template <bool kHalf>
+__device__ inline uint32_t only_finite(uint32_t x) {
+    constexpr uint32_t kAll = kHalf ? 0x7C00u : 0x7F80u;
+    if ((x & kAll) == kAll) x &= 0xFFFF0000u;
+    if ((x >> 16 & kAll) == kAll) x &= 0xFFFFu;
+    return x;
+}
+
+template <bool kHalf>
+__device__ inline float to_float(uint16_t x) {
+    if constexpr (kHalf) return (float)__builtin_bit_cast(_Float16, x);
+    else return __uint_as_float((uint32_t)x << 16);
+}
+
+// x if that is not finite, else 0
+template <bool kHalf>
+__device__ inline float not_finite(uint16_t x) {
+    constexpr uint32_t kAll = kHalf ? 0x7C00u : 0x7F80u;
+    return (x & kAll) == kAll ? to_float<kHalf>(x) : 0.f;
+}
+
+// V of a key, of a head of which `v` is the first element, or null where the key lies in no page.
+__device__ inline const uint16_t *v_of(const Attend &a, const uint16_t *v, const int32_t *pages, int32_t key) {
+    const int32_t id = pages[(uint32_t)key >> a.shift];
+    if ((uint32_t)id >= (uint32_t)a.pages) return nullptr;
+    return v + id * a.page_stride + (key & ((1 << a.shift) - 1)) * a.token_stride;
+}
+
 // What lane `of` holds of x, for all lanes.
 __device__ inline uint64_t lane_of(uint64_t x, int of) {
     return (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, of) |
@@ -317,6 +356,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
     constexpr int kRows = 16;
     __shared__ float joint[4][16][DP + 4];
     __shared__ float tops[4][16], weights[4][16];
+    __shared__ int32_t odd[4];  // the wave has put zeros in the place of values that are not finite
     const int lane = threadIdx.x % kWave, wave = uniform((int32_t)threadIdx.x / kWave);
     const int col = lane % 16, grp = lane / 16;
     const uint32_t place = (1u << a.shift) - 1;
@@ -373,6 +413,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
         global_u8 *const vh = (global_u8 *)(a.v + (int64_t)t.head * a.head_stride);
         const int32_t *const pages = a.table + r.slot * a.table_stride;
         int32_t clear = least;  // keys that need no look at the mask; 0 once a page number is bad
+        int32_t zeros = 0;
 
         // A step's keys, one per lane of 32; those past the last one that the tile sees stand for it.  `id`:
         // the pages they lie in.
@@ -420,6 +461,21 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
                 for (int j = 0; j < 8; ++j) {
                     const int key = 16 * (j / 4) + 4 * grp + j % 4;
                     if (k0 + key >= most || !(have >> key & 1)) x.v[j] = u32x4{0, 0, 0, 0};
+                }
+                if (least < most) {
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int i = 0; i < kCols / 2; ++i) top = exponents<kHalf>(x.v[j][i], top);
+                    if (__any((top & 0x80008000u) != 0)) {
+                        zeros = 1;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (k0 + 16 * (j / 4) + 4 * grp + j % 4 >= least)
+#pragma unroll
+                                for (int i = 0; i < kCols / 2; ++i) x.v[j][i] = only_finite<kHalf>(x.v[j][i]);
+                    }
                 }
             }
             f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -495,6 +551,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
             tops[wave][col] = m;
             weights[wave][col] = l;
         }
+        if (lane == 0) odd[wave] = zeros;
         __syncthreads();
         const bool whole = share.to - share.from == share.all;
         const int64_t at = 2 * (int64_t)blockIdx.x + (share.from == 0);  // a cut tile's partial sums
@@ -521,6 +578,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
                 lsum += weights[w][out_row] * (mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - mx) * c));  // (NaN stays)
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) sum[j] += joint[w][out_row][d0 + j];
+            }
+            if (least < most && __builtin_expect(odd[0] | odd[1] | odd[2] | odd[3], 0) && d0 < a.dim) {
+                const int32_t end = min(min(r.base + t.first + out_tok + 1, most), share.to * kKeys);
+                for (int32_t k = max(least, share.from * kKeys); k < end; ++k) {
+                    const uint16_t *v = v_of(a, a.v + (int64_t)t.head * a.head_stride + d0, pages, k);
+                    if (!v) continue;
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) sum[j] += not_finite<kHalf>(v[j]);
+                }
             }
             if (whole) {
                 const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
@@ -569,6 +635,37 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 // us, 4 TB/s.
 constexpr int kWideKeys = 64;
 
+// What is not finite in V of the keys from .. to - 1, added to the sums or outputs that this lane has written (lanes and rows as
+// below).  Apart from these, and from the thread's number on, so that it takes none of their registers.
+template <int DP, int kBlocks, bool kHalf>
+__device__ inline void add_values(const Attend &a, const Row &r, const Tile &t, int32_t from, int32_t to, bool whole, int64_t at) {
+    constexpr int kWaveRows = 32 * kBlocks, kRows = 4 * kWaveRows;
+    int32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int32_t *const pages = a.table + r.slot * a.table_stride;
+#pragma unroll 1
+    for (int b = 0; b < kBlocks; ++b) {
+        const int row = thread / kWave * kWaveRows + 32 * b + thread % 32, tok = row / t.heads, h = row - tok * t.heads;
+        if (tok >= t.n) return;
+        const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
+        uint16_t *const out = a.out + token * a.out_token + head * a.out_head;
+        float *const sum = a.sums + (at * kRows + row) * DP;
+        const int32_t end = min(to, r.base + t.first + tok + 1);
+#pragma unroll 1
+        for (int32_t key = from; key < end; ++key) {
+            const uint16_t *const v = v_of(a, a.v + (int64_t)t.head * a.head_stride, pages, key);
+            if (!v) continue;
+#pragma unroll 1
+            for (int d = thread / 8 & 4; d < a.dim; d = d % 4 == 3 ? d + 5 : d + 1) {
+                const float x = not_finite<kHalf>(v[d]);
+                if (x == 0.f) continue;
+                if (whole) out[d] = (uint16_t)pack<kHalf>(to_float<kHalf>(out[d]) + x, 0.f);
+                else sum[d] += x;
+            }
+        }
+    }
+}
+
 template <int DP, int kBlocks, bool kHalf, bool kRuns>
 __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_attend_wide(Attend a) {
     constexpr int kWaveRows = 32 * kBlocks, kRows = 4 * kWaveRows;
@@ -584,6 +681,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
     const int col = lane % 32, half = lane / 32;
     // blocks go to the eight dies in turn: neighbouring pieces, which share K and V, to one die
     const int64_t block = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    // the number, among the block's, of the last tile in which zeros were put in the place of values that are not finite
+    __shared__ int32_t odd;
+    int32_t number = 0;
+    if (threadIdx.x == 0) odd = 0;
     int64_t piece;
     Place p = find(a, block, &piece);
     if (p.row < 0) {
@@ -619,6 +720,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         if (share.from == share.to) continue;  // (the piece ends before the next unit)
         const int32_t all = max(0, r.base + r.n);
         const int32_t most = max(0, min(r.base + t.first + t.n, all));
+        const int32_t shared_keys = max(0, min(r.base + t.first + 1, all));  // that every query of the tile's sees
+        ++number;
         u32x4 q[kBlocks][kSteps];
         int32_t seen[kBlocks];
 #pragma unroll
@@ -681,13 +784,28 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         // V of keys that no query sees or that lie in no page: zeros (their weights are zero, and what
         // lies there may be anything)
         auto clean = [&](int32_t k0, int32_t id) {
-            if (__builtin_expect(k0 + kWideKeys > most || clear == 0, 0)) {
+            if (__builtin_expect(k0 + kWideKeys > shared_keys || clear == 0, 0)) {
                 asm volatile("");
                 const uint64_t ok = __ballot((uint32_t)id < (uint32_t)a.pages);
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const int j = kApart * i + key;
                     if (k0 + j >= most || !(ok >> j & 1)) v_in[i] = u32x4{0, 0, 0, 0};
+                }
+                if (shared_keys < most) {
+                    uint32_t high = 0;
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) high = exponents<kHalf>(v_in[i][j], high);
+                    if (__any((high & 0x80008000u) != 0)) {
+                        odd = number;
+#pragma unroll
+                        for (int i = 0; i < kLoads; ++i)
+                            if (k0 + kApart * i + key >= shared_keys)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) v_in[i][j] = only_finite<kHalf>(v_in[i][j]);
+                    }
                 }
             }
         };
@@ -908,6 +1026,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                 }
             }
         }
+        // (`odd` was written before the last barrier, and the next tile writes it after one)
+        if (__builtin_expect(k1 > shared_keys && shared_keys < most && odd == number, 0))
+            add_values<DP, kBlocks, kHalf>(a, r, t, max(k0, shared_keys), min(k1, most), whole, at);
     }
 }
 

@@ -651,6 +651,38 @@ def test_attend_nan_stays_in_its_row(P, chunks):
     assert torch.equal(glse[~bad], lse[~bad]) and torch.equal(got[~bad], out[~bad])
 
 
+# chunks of tiles of 16, 128 and 256 rows with four heads to a K/V head
+TILES = [[4, 2], [20, 30], [200, 90]]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads,kv,dim,page", [(8, 2, 128, 16), (8, 2, 64, 4), (4, 1, 40, 16), (16, 4, 120, 1)])
+@pytest.mark.parametrize("chunks", TILES)
+@pytest.mark.parametrize("lens", [[700, 3000], [20011, 203]])
+def test_attend_hidden_values(P, dtype, heads, kv, dim, page, chunks, lens):
+    """V of a chunk's tokens that is not finite: the queries before them do not change, those that see it say so."""
+    s = Sequences(P, lens, chunks, heads, kv, dim, page, dtype, seed=20)
+    out, lse = s.check(longest=max(chunks))
+    inf, nan, group = math.inf, math.nan, heads // kv
+    extra = torch.zeros(out.shape, device="cuda")
+    t0 = 0
+    for row, (n, x) in enumerate(zip(lens, chunks)):
+        hits = {}  # the last one of a place stands
+        for j, head, d, value in ((x - 1, 0, 5, nan), (x - 1, kv - 1, dim - 1, inf), (x // 2, 0, 0, -inf), (x // 2, 0, 9, inf),
+                                  (x - 1, 0, 9, -inf), (1, kv - 1, 17, nan)):
+            hits[j, head, d] = value
+        for (j, head, d), value in hits.items():
+            pos = n - x + j
+            s.cache.data[3][int(s.cache.table[row, pos // page]), head, pos % page, d] = value
+            extra[t0 + j:t0 + x, head * group:(head + 1) * group, d] += value
+        t0 += x
+    got, glse = s.cache.attend(1, s.q, offsets=s.offsets, longest=max(chunks), return_lse=True)
+    want = torch.where(extra == 0, out.float(), extra)
+    assert torch.equal(glse, lse)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got.float().nan_to_num(0), want.nan_to_num(0))
+
+
 def test_attend_slots_and_page_ids(P):
     s = Sequences(P, [33, 70, 5], [4, 9, 1], 8, 2, 64, 16, torch.bfloat16, seed=6, slots=[7, 0, 3])
     out, lse = s.check()
