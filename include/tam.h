@@ -640,7 +640,8 @@ tam_status tam_pages_store(const tam_chunk *c, const void *k_new, int64_t k_toke
  * with the sums and the softmax in fp32 and out rounded once to `dtype`; the
  * weights are rounded to `dtype` before they meet V.  A query without keys
  * (position < 0) gets out = 0 and lse = -inf.  Keys after a query's position do not
- * reach it, whatever their K and V hold.
+ * reach it, whatever their K and V hold; an infinity in V of a key that it sees is one in
+ * out, or NaN where the key's weight is too small for `dtype`.
  *   q     device, element (t, h, d) at q[t * q_token + h * q_head + d]; strides
  *         multiples of 8, 16-byte aligned.
  *   out   device, like q with out_token and out_head; tokens of no row are not written.

@@ -853,23 +853,39 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                 }
             }
         };
-        // m follows when it lags too far; the weights w, which are under the old one, go to O first
-        auto follow = [&](const uint16_t *at, u32x4 (&w)[kBlocks][2]) {
+        // m follows when it lags too far; sums, and the weights w on their way to V, go along.  After the first time it moves
+        // by whole powers of two in the weights, so that these, in 16 bits, keep their digits.
+        auto follow = [&](u32x4 (&w)[kBlocks][2]) {
             if (__builtin_expect(__any(top[0] > bound[0] || top[kBlocks - 1] > bound[kBlocks - 1]), 0)) {
                 asm volatile("");
-                gather(at, w);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
                     const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[b]), __float_as_uint(top[b]), false, false);
                     const float now = Range<kHalf>::follow(m[b], fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])), c);
-                    const float keep = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[b] - now) * c);
-                    m[b] = now;
-                    bound[b] = now + Range<kHalf>::kMost / c;
-                    mc[b] = now == -INFINITY ? 0.f : now * c;
+                    float keep = 1.f;
+                    if (m[b] == -INFINITY) {  // nothing has a weight yet
+                        if (now != -INFINITY) {
+                            keep = 0.f;
+                            m[b] = now;
+                            mc[b] = now * c;
+                        }
+                    } else {
+                        const float by = ceilf((m[b] - now) * c);
+                        keep = ldexpf(1.f, (int)fmaxf(by, -512.f));
+                        mc[b] -= by;
+                        m[b] = mc[b] / c;
+                    }
+                    bound[b] = m[b] + Range<kHalf>::kMost / c;
                     l[b] *= keep;
 #pragma unroll
                     for (int d = 0; d < kCols; ++d) o[b][d] *= keep;
-                    w[b][0] = w[b][1] = u32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t x = w[b][i][j];
+                            w[b][i][j] = pack<kHalf>(to_float<kHalf>((uint16_t)x) * keep, to_float<kHalf>((uint16_t)(x >> 16)) * keep);
+                        }
                 }
             }
         };
@@ -954,7 +970,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) top[b] = highest(sa[b]);
             settle(k0, 0, id0, sa);
-            follow(v_half(1, 1), pa);
+            follow(pa);
             int x = 0;  // the unit's buffers
             for (int32_t k = k0; k < k1; k += kWideKeys) {
                 // This unit's V and the next one's K have been loaded, and go to LDS; the next V and the K of
@@ -974,10 +990,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                 });
                 settle(k + 32, 1, id0, sb);
                 __syncthreads();
-                follow(v_half(x, 0), pb);
+                follow(pb);
                 stage(sb, pa, k_half(x ^ 1, 0), sa, v_half(x, 0), pb, [](int) {});
                 settle(k + 64, 0, id1, sa);
-                if (k + kWideKeys < k1) follow(v_half(x, 1), pa);
+                if (k + kWideKeys < k1) follow(pa);
                 id0 = id1;
                 id1 = id2;
                 id2 = id3;

@@ -683,6 +683,33 @@ def test_attend_hidden_values(P, dtype, heads, kv, dim, page, chunks, lens):
     assert torch.equal(got.float().nan_to_num(0), want.nan_to_num(0))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 128), (8, 2, 64)])
+@pytest.mark.parametrize("chunks", TILES)
+def test_attend_infinite_values_under_rising_scores(P, dtype, heads, kv, dim, chunks):
+    """An infinity in V that every query sees stays one, where the scores rise by 7 (weights by 2^10) after its key."""
+    lens = [700, 900]
+    s = Sequences(P, lens, chunks, heads, kv, dim, 16, dtype, seed=21)
+    s.q.fill_(1)
+    places, hit = [], torch.zeros((2, dim), dtype=torch.bool, device="cuda")
+    for row, n in enumerate(lens):
+        pos = torch.arange(n, device="cuda")
+        places.append((s.cache.table[row, pos // 16].long(), pos % 16))
+        s.k[row].copy_((pos // 32 % 2 * 7 / dim ** 0.5)[:, None, None].expand(n, kv, dim))
+        s.cache.data[2][places[row][0], :, places[row][1]] = s.k[row]
+    out, lse = s.check(longest=max(chunks))
+    for row, n in enumerate(lens):
+        for i, key in enumerate(range(3, n - max(chunks), 16)):
+            if key // 32 % 2 == 0:
+                s.cache.data[3][places[row][0][key], :, places[row][1][key], 2 * i % dim] = math.inf
+                hit[row, 2 * i % dim] = True
+    got, glse = s.cache.attend(1, s.q, offsets=s.offsets, longest=max(chunks), return_lse=True)
+    assert torch.equal(glse, lse)
+    for a, b, h in zip(got.split(chunks), out.split(chunks), hit):
+        assert (a[:, :, h] == math.inf).all()
+        assert torch.equal(a[:, :, ~h], b[:, :, ~h])
+
+
 def test_attend_slots_and_page_ids(P):
     s = Sequences(P, [33, 70, 5], [4, 9, 1], 8, 2, 64, 16, torch.bfloat16, seed=6, slots=[7, 0, 3])
     out, lse = s.check()
