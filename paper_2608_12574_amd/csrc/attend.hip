@@ -478,6 +478,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
                     }
                 }
             }
+            if (__builtin_expect(a.dim < DP, 0)) {  // K past the last dimension: the queries' zeros there would make an infinity NaN
+                asm volatile("");
+#pragma unroll
+                for (int d = 0; d < kSteps; ++d)
+                    if (32 * d + 8 * grp >= a.dim) x.k[0][d] = x.k[1][d] = u32x4{0, 0, 0, 0};
+            }
             f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -702,8 +708,14 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
     // and its writes: piece `mine` of keys `key`, `key` + kApart, ...
     constexpr int kApart = kThreads / kPieces;
     const int key = threadIdx.x / kPieces, mine = threadIdx.x % kPieces;
-    uint16_t *const k_write = kbuf + key * kKStride + 8 * mine, *const v_write = vbuf + key * kVStride + 8 * mine;
-    const uint32_t in_run = 2 * ((kRuns ? (uint32_t)(key % 16) * (uint32_t)a.token_stride : 0) + (8 * mine < a.dim ? 8 * mine : 0));
+    // (K past the last dimension: zeros from here on, since the queries' zeros there would make an infinity NaN; these lanes write
+    // into the gap between two keys)
+    const bool in_dim = 8 * mine < a.dim;
+    uint16_t *const k_write = kbuf + key * kKStride + (in_dim ? 8 * mine : DP), *const v_write = vbuf + key * kVStride + 8 * mine;
+    if (!in_dim)
+#pragma unroll
+        for (int i = 0; i < 2 * kLoads; ++i) *reinterpret_cast<u32x4 *>(kbuf + (key + i * kApart) * kKStride + 8 * mine) = u32x4{0, 0, 0, 0};
+    const uint32_t in_run = 2 * ((kRuns ? (uint32_t)(key % 16) * (uint32_t)a.token_stride : 0) + (in_dim ? 8 * mine : 0));
 
     while (left > 0) {
         const Row r = p.r;

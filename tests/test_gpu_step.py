@@ -710,6 +710,22 @@ def test_attend_infinite_values_under_rising_scores(P, dtype, heads, kv, dim, ch
         assert torch.equal(a[:, :, ~h], b[:, :, ~h])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 128), (8, 2, 64), (4, 1, 40), (4, 1, 8), (8, 2, 96), (16, 4, 120)])
+@pytest.mark.parametrize("chunks", TILES)
+def test_attend_infinite_keys(P, dtype, heads, kv, dim, chunks):
+    """A key whose scores are -inf has the weight 0, as one whose scores are far below the others."""
+    s = Sequences(P, [700, 90 + chunks[1]], chunks, heads, kv, dim, 16, dtype, seed=22)
+    s.q[:, :, 3] = 1
+    at = int(s.cache.table[0, 2]), slice(None), 7, 3
+    s.cache.data[2][at] = -6e4
+    want = s.cache.attend(1, s.q, offsets=s.offsets, longest=max(chunks), return_lse=True)
+    s.cache.data[2][at] = -math.inf
+    got = s.cache.attend(1, s.q, offsets=s.offsets, longest=max(chunks), return_lse=True)
+    for a, b in zip(want, got):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
 def test_attend_slots_and_page_ids(P):
     s = Sequences(P, [33, 70, 5], [4, 9, 1], 8, 2, 64, 16, torch.bfloat16, seed=6, slots=[7, 0, 3])
     out, lse = s.check()
