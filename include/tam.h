@@ -536,7 +536,7 @@ tam_status tam_adjust_logits(const tam_handle *h, const uint64_t *rows, int64_t 
  * at place t % page_tokens.  The pool has `planes` planes (a K and a V plane per
  * layer), and a page number stands for that page of every plane.  refs[p] counts
  * the table entries that name page p (a caller may add holders of its own); a
- * page at 0 is free.  Table entries past a slot's pages are not read.
+ * page at 0 is free.  Pages do not overlap, whichever of plane and page is the outer axis.  Table entries past a slot's pages are not read.
  */
 typedef struct {
     void *data;            /* device; may be null with planes == 0 */
@@ -608,7 +608,7 @@ tam_status tam_pages_compact(const tam_pages *c, int32_t *info, int32_t *moved, 
  * token j of n has the position length - n + j.  Element (page p, head h, place t,
  * dimension d) of K is at k[p * page_stride + h * head_stride + t * token_stride + d],
  * in elements of `dtype`; V alike.  The strides are multiples of 8 and the
- * pointers 16-byte aligned. */
+ * pointers 16-byte aligned; tam_pages_store asks for vectors that lie apart. */
 typedef struct {
     void *k, *v;
     int64_t page_stride, head_stride, token_stride;
@@ -644,7 +644,7 @@ tam_status tam_pages_store(const tam_chunk *c, const void *k_new, int64_t k_toke
  * out, or NaN where the key's weight is too small for `dtype`.
  *   q     device, element (t, h, d) at q[t * q_token + h * q_head + d]; strides
  *         multiples of 8, 16-byte aligned.
- *   out   device, like q with out_token and out_head; tokens of no row are not written.
+ *   out   device, like q with out_token and out_head, vectors apart from each other; tokens of no row are not written.
  *   lse   device float[tokens][heads], or NULL.
  *   work  tam_attend_work(c, heads) bytes.
  * Errors: TAM_E_INVAL, TAM_E_DEVICE.

@@ -2,6 +2,8 @@
 // and launches.  (tam_adjust_logits, which takes a handle, is in tam_api.cpp.)
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <array>
 #include <climits>
 #include <cstdint>
 
@@ -19,6 +21,25 @@ using tam::api_fail;
 
 bool power_of_two(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
 bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+struct Axis {
+    int64_t count, stride;
+};
+
+// Whether vectors of `size` lie apart: each axis, in the order of the strides, steps over all that those before it
+// span.  (What a launch writes, it must not write twice.)
+template <size_t N>
+bool apart(int64_t size, std::array<Axis, N> axes) {
+    for (Axis &x : axes) x.stride = x.stride < 0 ? (x.stride == INT64_MIN ? INT64_MAX : -x.stride) : x.stride;
+    std::sort(axes.begin(), axes.end(), [](const Axis &x, const Axis &y) { return x.stride < y.stride; });
+    __int128 span = size;
+    for (const Axis &x : axes) {
+        if (x.count < 2) continue;
+        if (x.stride < span) return false;
+        span += (__int128)(x.count - 1) * x.stride;
+    }
+    return true;
+}
 
 // null: fine, else what is wrong
 const char *tables_wrong(const void *table, const void *length, int64_t slots, int64_t max_pages, int64_t stride,
@@ -45,6 +66,7 @@ const char *pages_wrong(const tam_pages *c) {
         if (!c->data) return "null data";
         if (c->page_stride < c->page_bytes || c->plane_stride < 0)
             return "page_stride must be >= page_bytes and plane_stride >= 0";
+        if (!apart<2>(c->page_bytes, {{{c->planes, c->plane_stride}, {c->num_pages, c->page_stride}}})) return "pages overlap";
     }
     return nullptr;
 }
@@ -131,6 +153,8 @@ tam_status tam_pages_store(const tam_chunk *c, const void *k_new, int64_t k_toke
     if (!w && c->tokens > 0 && (!k_new || !v_new)) w = "null device pointer";
     if (!w && (!aligned(k_new, 16) || !aligned(v_new, 16) || k_token % 8 || k_head % 8 || v_token % 8 || v_head % 8))
         w = "k_new and v_new must be 16-byte aligned and their strides multiples of 8";
+    if (!w && !apart<3>(c->head_dim, {{{c->num_pages, c->page_stride}, {c->kv_heads, c->head_stride}, {c->page_tokens, c->token_stride}}}))
+        w = "the pool's vectors overlap";
     if (w) return api_fail(TAM_E_INVAL, w);
     if (c->tokens == 0 || c->rows == 0) return TAM_OK;
     STEP_HIP(hipGetLastError());
@@ -157,6 +181,7 @@ tam_status tam_attend(const tam_chunk *c, const void *q, int64_t q_token, int64_
     if (!w && c->tokens > 0 && !work && tam::attend_work_bytes(*c, heads) > 0) w = "null work";
     if (!w && (!aligned(q, 16) || !aligned(out, 16) || q_token % 8 || q_head % 8 || out_token % 8 || out_head % 8))
         w = "q and out must be 16-byte aligned and their strides multiples of 8";
+    if (!w && !apart<2>(c->head_dim, {{{c->tokens, out_token}, {heads, out_head}}})) w = "out's vectors overlap";
     if (!w && (!aligned(lse, 4) || !aligned(work, 16))) w = "lse must be 4-byte and work 16-byte aligned";
     if (w) return api_fail(TAM_E_INVAL, w);
     if (c->tokens == 0 || c->rows == 0) return TAM_OK;

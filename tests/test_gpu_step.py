@@ -942,3 +942,20 @@ def test_beams_example(P):
             # logits of size 1 from bf16 layers, a few roundings of 2^-8 each
             assert abs(float(want) - score) <= 0.03 * n
     h.close()
+
+
+def test_attend_refuses_outputs_that_overlap(P):
+    s = Sequences(P, [100, 33], [20, 1], 8, 2, 64, 16, torch.bfloat16, seed=23)
+    one = torch.zeros((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    for out in (one.expand(21, 8, 64), torch.zeros((1, 8, 64), dtype=torch.bfloat16, device="cuda").expand(21, 8, 64),
+                torch.zeros((21, 1, 64), dtype=torch.bfloat16, device="cuda").expand(21, 8, 64)):
+        with pytest.raises(P.TamError):
+            s.cache.attend(1, s.q, offsets=s.offsets, out=out)
+    with pytest.raises(P.TamError):
+        P.PageCache(s.cache.data[:1].expand(2, -1, -1, -1, -1), s.cache.table, s.cache.length, s.cache.refs)
+    heads_first = torch.zeros((8, 21, 64), dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    assert torch.equal(s.cache.attend(1, s.q, offsets=s.offsets, out=heads_first), s.cache.attend(1, s.q, offsets=s.offsets))
+    # pages before planes
+    data = s.cache.data.transpose(0, 1).contiguous().transpose(0, 1)
+    c = P.PageCache(data, s.cache.table, s.cache.length, s.cache.refs)
+    assert torch.equal(c.attend(1, s.q, offsets=s.offsets), s.cache.attend(1, s.q, offsets=s.offsets))
