@@ -1,8 +1,8 @@
 """What a decode step does beside the mask: edits of logits, and a paged K/V cache.
 
 As in ``tam``, this module marshals arguments only; every step runs in
-``libtam.so`` on the stream given, or torch's current stream.  Scratch comes from
-torch's caching allocator.
+``libtam.so`` on the stream given, or torch's current stream.  The tensors and the stream of a call
+are of the current device, or it is refused.  Scratch comes from torch's caching allocator.
 """
 from __future__ import annotations
 
@@ -16,21 +16,21 @@ def _bad(where, what):
     return TamError(-1, where, what)
 
 
-def _int32(where, name, t, n):
-    """The pointer of a contiguous device int32 tensor of n elements."""
-    if t.dtype is not _int or not t.is_cuda or t.numel() != n or not t.is_contiguous():
-        raise _bad(where, f"{name} must be a contiguous int32 tensor of {n} elements on the GPU")
+def _int32(where, name, t, n, gpu):
+    """The pointer of a contiguous int32 tensor of n elements on GPU number `gpu`."""
+    if t.dtype is not _int or t.get_device() != gpu or t.numel() != n or not t.is_contiguous():
+        raise _bad(where, f"{name} must be a contiguous int32 tensor of {n} elements on cuda:{gpu}")
     return t.data_ptr()
 
 
-def _rows_of(where, name, t, B, dtype):
-    """(pointer, row stride, columns) of a device [B, n] tensor whose rows are contiguous."""
-    if t.dtype is not dtype or not t.is_cuda or t.dim() != 2:
-        raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on the GPU")
+def _rows_of(where, name, t, B, dtype, gpu):
+    """(pointer, row stride, columns) of a [B, n] tensor on GPU number `gpu` whose rows are contiguous."""
+    if t.dtype is not dtype or t.get_device() != gpu or t.dim() != 2:
+        raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on cuda:{gpu}")
     rows, n = t.shape
     stride, step = t.stride()
     if rows != B or (n > 1 and step != 1):
-        raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on the GPU with contiguous rows")
+        raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on cuda:{gpu} with contiguous rows")
     return t.data_ptr(), stride if rows > 1 else max(stride, n), n
 
 
@@ -46,6 +46,17 @@ def _ready():
     return c
 
 
+def _stream(where, c, stream, gpu):
+    """The HIP stream of a call on GPU number `gpu`, which has to be the current one, as the launch goes there."""
+    if c.device() != gpu:
+        raise _bad(where, f"the tensors lie on cuda:{gpu}, the current device is cuda:{c.device()}")
+    if stream is None:
+        return c.stream_of(gpu)
+    if getattr(stream, "device_index", gpu) != gpu:
+        raise _bad(where, f"the stream is of cuda:{stream.device_index}, the tensors lie on cuda:{gpu}")
+    return stream.cuda_stream
+
+
 def _adjust(logits, stream, handle=None, rows=None, ids=None, tokens=None, length=None, prompt=None, repetition=None,
             frequency=None, presence=None, bias_ids=None, bias=None):
     where = "tam_adjust_logits"
@@ -53,6 +64,8 @@ def _adjust(logits, stream, handle=None, rows=None, ids=None, tokens=None, lengt
     dtype = c.dtypes.get(logits.dtype)
     if dtype is None or not logits.is_cuda or logits.dim() != 2:
         raise _bad(where, "logits must be a [B, V] fp32 or bf16 tensor on the GPU")
+    gpu = logits.get_device()
+    hip_stream = _stream(where, c, stream, gpu)
     B, V = logits.shape
     row_stride, step = logits.stride()
     if V > 1 and step != 1:
@@ -63,38 +76,39 @@ def _adjust(logits, stream, handle=None, rows=None, ids=None, tokens=None, lengt
     if handle is not None:
         if rows is not None or handle._raw is None:
             raise _bad(where, "a handle and mask rows" if handle._raw else "the handle is closed")
+        if not handle.host_only and handle.device.index != gpu:
+            raise _bad(where, f"the handle lies on {handle.device}, the logits on cuda:{gpu}")
         if V < handle.vocab_size:
             raise _bad(where, f"logits have {V} columns, the vocabulary {handle.vocab_size} tokens")
         V, raw = handle.vocab_size, handle._raw
-        ids_p = _int32(where, "node_ids", ids, B)
+        ids_p = _int32(where, "node_ids", ids, B, gpu)
     elif rows is not None:
         if ids is None or rows.dim() != 2:
             raise _bad(where, "rows must be [R, words] and come with row_ids")
-        rows_p, stride, width = _rows_of(where, "rows", rows, rows.shape[0], _long)
+        rows_p, stride, width = _rows_of(where, "rows", rows, rows.shape[0], _long, gpu)
         num_rows = rows.shape[0]
         if width < (V + 63) // 64:
             raise _bad(where, f"rows must have {(V + 63) // 64} words")
-        ids_p = _int32(where, "row_ids", ids, B)
+        ids_p = _int32(where, "row_ids", ids, B, gpu)
         rows_p = rows_p or ids_p and ids_p & -8  # no rows at all have no memory, and none of it is read: nothing is valid
     elif ids is not None:
         raise _bad(where, "row_ids without rows")
-    text_p, text_stride, history = (None, 0, 0) if tokens is None else _rows_of(where, "tokens", tokens, B, _int)
+    text_p, text_stride, history = (None, 0, 0) if tokens is None else _rows_of(where, "tokens", tokens, B, _int, gpu)
     floats = []
     for t in (repetition, frequency, presence):
         if t is None:
             floats.append(None)
             continue
-        if t.dtype is not _float or not t.is_cuda or t.numel() != B or not t.is_contiguous():
-            raise _bad(where, f"repetition, frequency and presence must be contiguous [{B}] fp32 tensors on the GPU")
+        if t.dtype is not _float or t.get_device() != gpu or t.numel() != B or not t.is_contiguous():
+            raise _bad(where, f"repetition, frequency and presence must be contiguous [{B}] fp32 tensors on cuda:{gpu}")
         floats.append(t.data_ptr())
-    named_p, named_stride, named = (None, 0, 0) if bias_ids is None else _rows_of(where, "bias_ids", bias_ids, B, _int)
-    bias_p, other, n = (None, 0, 0) if bias is None else _rows_of(where, "bias", bias, B, _float)
+    named_p, named_stride, named = (None, 0, 0) if bias_ids is None else _rows_of(where, "bias_ids", bias_ids, B, _int, gpu)
+    bias_p, other, n = (None, 0, 0) if bias is None else _rows_of(where, "bias", bias, B, _float, gpu)
     if named_stride != other or named != n:
         raise _bad(where, "bias_ids and bias must have the same shape and strides")
-    e = Edits(text_p, text_stride, history, None if length is None else _int32(where, "length", length, B),
-              None if prompt is None else _int32(where, "prompt", prompt, B), *floats, named_p, bias_p, named_stride, named)
-    rc = c.adjust(raw, rows_p, num_rows, stride, ids_p, ctypes.byref(e), B, V, logits.data_ptr(), dtype, row_stride,
-                  c.stream() if stream is None else stream.cuda_stream)
+    e = Edits(text_p, text_stride, history, None if length is None else _int32(where, "length", length, B, gpu),
+              None if prompt is None else _int32(where, "prompt", prompt, B, gpu), *floats, named_p, bias_p, named_stride, named)
+    rc = c.adjust(raw, rows_p, num_rows, stride, ids_p, ctypes.byref(e), B, V, logits.data_ptr(), dtype, row_stride, hip_stream)
     if rc != TAM_OK:
         _check(rc, where)
     return logits
@@ -137,14 +151,15 @@ class PageCache:
         planes, pages, kv, page, dim = data.shape
         if planes < 2 or planes % 2 or pages < 1 or not data[0, 0].is_contiguous():
             raise _bad(where, "data needs a K and a V plane per layer and contiguous pages")
-        if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_cuda or (
+        self._gpu = gpu = data.get_device()
+        if table.dim() != 2 or table.dtype is not torch.int32 or table.get_device() != gpu or (
                 table.shape[1] > 1 and table.stride(1) != 1):
-            raise _bad(where, "table must be a [slots, max_pages] int32 tensor on the GPU with contiguous rows")
+            raise _bad(where, f"table must be a [slots, max_pages] int32 tensor on cuda:{gpu} with contiguous rows")
         slots, width = table.shape
         stride = table.stride(0) if slots > 1 else width
         self._calls = _tam._calls_made if _int is not None else _ready()
-        length_p = _int32(where, "length", length, slots)
-        refs_p = _int32(where, "refs", refs, pages)
+        length_p = _int32(where, "length", length, slots, gpu)
+        refs_p = _int32(where, "refs", refs, pages, gpu)
         self.data, self.table, self.length, self.refs = data, table, length, refs
         self.layers, self.kv_heads, self.page_tokens, self.head_dim = planes // 2, kv, page, dim
         self._torch, self._device = torch, data.device
@@ -183,24 +198,25 @@ class PageCache:
     def _work(self, stream):
         return self._empty(self._work_bytes, self._torch.uint8, stream)
 
-    def _on(self, stream):
-        return self._calls.stream() if stream is None else stream.cuda_stream
+    def _on(self, where, stream):
+        return _stream(where, self._calls, stream, self._gpu)
 
     def fork(self, slots, parents, lengths=None, stream=None):
         """Slot ``slots[i]`` becomes a copy of the first ``lengths[i]`` tokens (all of them without
         ``lengths``) of slot ``parents[i]`` as it was before the call; a parent outside the
         slots (-1) frees the slot.  Pages are shared, not copied."""
         where = "tam_pages_fork"
-        n = slots.numel()
-        s, p = _int32(where, "slots", slots, n), _int32(where, "parents", parents, n)
-        keep = None if lengths is None else _int32(where, "lengths", lengths, n)
+        n, gpu, on = slots.numel(), self._gpu, self._on(where, stream)
+        s, p = _int32(where, "slots", slots, n, gpu), _int32(where, "parents", parents, n, gpu)
+        keep = None if lengths is None else _int32(where, "lengths", lengths, n, gpu)
         work = self._work(stream)
-        rc = self._lib.tam_pages_fork(self._pages_ref, s, p, keep, n, work.data_ptr(), self._on(stream))
+        rc = self._lib.tam_pages_fork(self._pages_ref, s, p, keep, n, work.data_ptr(), on)
         if rc != TAM_OK:
             _check(rc, where)
 
     def free(self, slots, stream=None):
         """The slots' sequences end; pages that no other slot names are free."""
+        self._on("tam_pages_fork", stream)
         parents = self._empty(slots.shape, slots.dtype, stream)
         if stream is None:
             parents.fill_(-1)
@@ -215,11 +231,11 @@ class PageCache:
         (else 0, and nothing has changed), pages needed, pages that were free, slots that
         ``max_pages`` is too small for."""
         where = "tam_pages_extend"
-        n = slots.numel()
-        s, c = _int32(where, "slots", slots, n), _int32(where, "counts", counts, n)
+        n, gpu, on = slots.numel(), self._gpu, self._on(where, stream)
+        s, c = _int32(where, "slots", slots, n, gpu), _int32(where, "counts", counts, n, gpu)
         work = self._work(stream)
         info = self._empty(4, self._torch.int32, stream)
-        rc = self._lib.tam_pages_extend(self._pages_ref, s, c, n, info.data_ptr(), work.data_ptr(), self._on(stream))
+        rc = self._lib.tam_pages_extend(self._pages_ref, s, c, n, info.data_ptr(), work.data_ptr(), on)
         if rc != TAM_OK:
             _check(rc, where)
         return info
@@ -227,13 +243,14 @@ class PageCache:
     def compact(self, stream=None):
         """The pages in use move to the front of the pool.  Returns int32 [2] (pages in use,
         pages moved) and int32 [pages] (each page's new number, -1 of a free one), both on the GPU."""
+        where = "tam_pages_compact"
+        on = self._on(where, stream)
         work = self._work(stream)
         info = self._empty(2, self._torch.int32, stream)
         moved = self._empty(self.refs.shape, self._torch.int32, stream)
-        rc = self._lib.tam_pages_compact(self._pages_ref, info.data_ptr(), moved.data_ptr(), work.data_ptr(),
-                                          self._on(stream))
+        rc = self._lib.tam_pages_compact(self._pages_ref, info.data_ptr(), moved.data_ptr(), work.data_ptr(), on)
         if rc != TAM_OK:
-            _check(rc, "tam_pages_compact")
+            _check(rc, where)
         return info, moved
 
     # -- a layer's new tokens ------------------------------------------------------
@@ -245,10 +262,10 @@ class PageCache:
             rows = offsets.numel() - 1
             if rows < 0:
                 raise _bad(where, "offsets must be [rows + 1]")
-            c.offsets = _int32(where, "offsets", offsets, rows + 1)
+            c.offsets = _int32(where, "offsets", offsets, rows + 1, self._gpu)
         else:
             rows, c.offsets = tokens, None
-        c.slot_ids = None if slots is None else _int32(where, "slots", slots, rows)
+        c.slot_ids = None if slots is None else _int32(where, "slots", slots, rows, self._gpu)
         plane = self._pages.plane_stride
         c.k = self._pages.data + 2 * layer * plane
         c.v = c.k + plane
@@ -257,10 +274,10 @@ class PageCache:
 
     def _vectors(self, where, name, t, heads=None):
         """(pointer, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
-        if (t.dim() != 3 or not t.is_cuda or t.dtype is not self.data.dtype or t.shape[2] != self.head_dim
+        if (t.dim() != 3 or t.get_device() != self._gpu or t.dtype is not self.data.dtype or t.shape[2] != self.head_dim
                 or t.stride(2) != 1 or (heads is not None and t.shape[1] != heads)):
             raise _bad(where, f"{name} must be a [tokens, {heads or 'heads'}, {self.head_dim}] {self.data.dtype} tensor "
-                              "on the GPU with contiguous vectors")
+                              f"on cuda:{self._gpu} with contiguous vectors")
         # of a single token or head any stride will do
         return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
 
@@ -269,11 +286,11 @@ class PageCache:
         ``offsets[i]:offsets[i + 1]`` (one token per row without ``offsets``), the last ones of slot ``slots[i]``
         (slot i without ``slots``), whose length counts them already (``extend``)."""
         where = "tam_pages_store"
+        on = self._on(where, stream)
         kp, vp = self._vectors(where, "k", k, self.kv_heads), self._vectors(where, "v", v, self.kv_heads)
         if k.shape[0] != v.shape[0]:
             raise _bad(where, "k and v have different numbers of tokens")
-        rc = self._lib.tam_pages_store(self._new(where, layer, k.shape[0], offsets, slots, longest), *kp, *vp,
-                                        self._on(stream))
+        rc = self._lib.tam_pages_store(self._new(where, layer, k.shape[0], offsets, slots, longest), *kp, *vp, on)
         if rc != TAM_OK:
             _check(rc, where)
 
@@ -285,6 +302,7 @@ class PageCache:
         row, or more, if the host knows (a hint).  Returns ``out`` (like ``q``; tokens of no row and the memory
         between are not written) and with ``return_lse`` the fp32 [tokens, heads] logarithms of the sums."""
         where = "tam_attend"
+        on = self._on(where, stream)
         qp = self._vectors(where, "q", q)
         T, heads = q.shape[0], q.shape[1]
         if out is None:
@@ -300,7 +318,7 @@ class PageCache:
             _check(-1, where)
         work = self._empty(size, self._torch.uint8, stream) if size else None
         rc = lib.tam_attend(chunk, *qp, heads, self.head_dim ** -0.5 if scale is None else scale, *op,
-                            lse.data_ptr() if return_lse else None, work.data_ptr() if size else None, self._on(stream))
+                            lse.data_ptr() if return_lse else None, work.data_ptr() if size else None, on)
         if rc != TAM_OK:
             _check(rc, where)
         return (out, lse) if return_lse else out

@@ -250,6 +250,8 @@ class _Calls:
         dev = getattr(torch._C, "_cuda_getDevice", None)
         # callers hold device tensors, so torch has initialised the device
         self.stream = (lambda: raw(dev())) if raw is not None and dev is not None else (lambda: _stream_ptr(None))
+        self.device = dev if dev is not None else torch.cuda.current_device
+        self.stream_of = raw if raw is not None else (lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
 
 
 _calls_made = None
