@@ -31,7 +31,7 @@ def _rows_of(where, name, t, B, dtype, gpu):
     stride, step = t.stride()
     if rows != B or (n > 1 and step != 1):
         raise _bad(where, f"{name} must be a [{B}, n] {dtype} tensor on cuda:{gpu} with contiguous rows")
-    return t.data_ptr(), stride if rows > 1 else max(stride, n), n
+    return t.data_ptr(), stride if rows > 1 else n, n
 
 
 _int = _float = _long = None  # torch's types, once torch is there

@@ -195,6 +195,21 @@ def test_adjust_keeps_and_masks_special_values(P):
     assert (x == -math.inf).all()  # NaN and infinities among them
 
 
+def test_adjust_one_row_of_any_stride(P):
+    """Of a single row the stride says nothing: one row of larger lists."""
+    x = torch.randn((3, 5003), generator=gen(6), device="cuda")
+    want = x.clone()
+    tokens, ids = (torch.randint(0, 5003, (3, n), generator=gen(n), device="cuda", dtype=torch.int32) for n in (40, 9))
+    bias, presence = torch.randn((3, 9), generator=gen(7), device="cuda"), torch.ones(3, device="cuda")
+    rows = torch.randint(-2 ** 62, 2 ** 62, (3, 90), generator=gen(8), device="cuda")
+    P.adjust_logits(want, tokens=tokens[:, :30].contiguous(), presence=presence, bias_ids=ids[:, :5].contiguous(),
+                    bias=bias[:, :5].contiguous(), rows=rows, row_ids=ints([0, 1, 2]))
+    for b in range(3):
+        P.adjust_logits(x[b:b + 1], tokens=tokens[b:b + 1, :30], presence=presence[b:b + 1], bias_ids=ids[b:b + 1, :5],
+                        bias=bias[b:b + 1, :5].clone(), rows=rows[b:b + 1], row_ids=ints([0]))
+    assert torch.equal(x, want)
+
+
 def test_adjust_refusals(P):
     x = torch.zeros((2, 100), device="cuda")
     t = ints([[1], [2]])

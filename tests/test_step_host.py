@@ -134,6 +134,16 @@ def test_tensors_of_another_gpu_are_refused(P, two_gpus):
             two_gpus(1, **kw)
 
 
+def test_adjust_takes_one_row_of_any_stride(P, two_gpus):
+    """Of a single row the stride says nothing: a bias beside ids that are part of a larger list."""
+    ids, bias = torch.zeros((4, 9), dtype=torch.int32)[2:3, :3], torch.zeros((1, 3))
+    with pytest.raises(Launched):
+        P.adjust_logits(On(torch.zeros((1, 128)), 0), bias_ids=On(ids, 0), bias=On(bias, 0))
+    with pytest.raises(P.TamError):
+        P.adjust_logits(On(torch.zeros((2, 128)), 0), bias_ids=On(torch.zeros((4, 9), dtype=torch.int32)[:2, :3], 0),
+                        bias=On(torch.zeros((2, 3)), 0))
+
+
 def test_logits_of_another_gpu_are_refused(P, two_gpus):
     from types import SimpleNamespace
 
