@@ -178,6 +178,34 @@ def test_adjust_mask_alone(P, dtype, B, V, pad, offset):
         check_adjusted(P, B, V, dtype, seed, pad=pad, offset=offset, history=None, biases=0)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,V,pad,offset,history", [(9, 4101, 3, 1, None), (4, 8192, 0, 5, None), (1, 63, 0, 1, None), (6, 200, 5, 0, 40),
+                                                    (110, 262143, 1, 1, 300), (110, 262144, 0, 3, 300)])
+def test_adjust_rows_as_wide_as_the_vocabulary(P, dtype, B, V, pad, offset, history):
+    """Mask rows of ceil(V/64) words with bits set past V, the last one at the end of its memory, logits of any alignment:
+    the mask alone, in one pass with the edits, and after them."""
+    rng = np.random.default_rng(V + B)
+    words = -(-V // 64)
+    bits = rng.random((7, words * 64)) < np.array([0, 1, 0.5, 2 / V, 0.02, 0.9, 0.3])[:, None]
+    bits[:, V:] = True
+    rows = torch.as_tensor(np.packbits(bits, axis=1, bitorder="little").view(np.int64), device="cuda")
+    ids = rng.integers(-1, 8, B)
+    buf = (torch.randn((B, offset + V + pad), generator=gen(B), device="cuda") * 4).to(dtype)
+    before, kw = buf.clone(), {}
+    if history:
+        kw = dict(tokens=ints(rng.integers(-1, V + 2, (B, history)).astype(np.int32)),
+                  presence=torch.as_tensor(rng.uniform(-0.5, 1, B), dtype=torch.float32, device="cuda"))
+    logits = buf[:, offset:offset + V]
+    valid = torch.as_tensor(bits[np.clip(ids, 0, 6), :V] & ((ids >= 0) & (ids < 7))[:, None], device="cuda")
+    want, bound, kept = (torch.as_tensor(x, device="cuda") for x in adjusted(logits, V, **kw))
+    P.adjust_logits(logits, rows=rows, row_ids=ints(ids), **kw)
+    assert ((logits == -math.inf) == ~valid).all()
+    assert ((logits.double() - want).abs() <= bound)[valid].all()
+    raw = torch.int16 if dtype is torch.bfloat16 else torch.int32
+    same = buf.view(raw) == before.view(raw)
+    assert same[:, offset:offset + V][kept & valid].all() and same[:, :offset].all() and same[:, offset + V:].all()
+
+
 @pytest.mark.parametrize("name", ["length", "prompt", "repetition", "frequency", "presence"])
 def test_adjust_parts_left_out(P, name):
     check_adjusted(P, 4, 1000, torch.float32, 8, **{name: None})
@@ -463,6 +491,54 @@ def test_pages_unaligned_pool(P):
     assert torch.equal(whole[:, 2], whole[:, 2])
 
 
+@pytest.mark.parametrize("dim", [12, 16])
+def test_pages_stay_in_their_planes(P, dim):
+    """Copies and moves in a pool with gaps between planes and between pages, in bytes (dim 12) and in pieces (16)."""
+    whole = torch.randn((4, 5, 11, 3, 1, 1, dim), generator=gen(24), device="cuda").to(torch.bfloat16)
+    before = whole.clone()
+    c = P.PageCache(whole[:, 3, :, 1], torch.full((3, 5), -1, dtype=torch.int32, device="cuda"), ints([0, 0, 0]), ints([0] * 11))
+    assert c.page_tokens == 1
+    m = Model(c)
+    for s, n in (([0, 1, 2], [3, 1, 4]), ([1], [2])):
+        assert c.extend(ints(s), ints(n)).tolist() == m.extend(s, n)
+    c.fork(ints([0]), ints([-1]))
+    m.fork([0], [-1])
+    info, moved = c.compact()
+    want = m.compact()
+    assert info.tolist() == want[0] and want[0][1] > 0 and moved.tolist() == want[1]
+    m.same(c)
+    before[:, 3, :, 1] = c.data
+    assert torch.equal(whole.view(torch.int16), before.view(torch.int16))
+
+
+@pytest.mark.parametrize("dim", [12, 16])
+def test_shared_pages_are_copied_in_their_planes(P, dim):
+    whole = torch.randn((4, 5, 11, 3, 1, 4, dim), generator=gen(25), device="cuda").to(torch.bfloat16)
+    before = whole.clone()
+    c = P.PageCache(whole[:, 3, :, 1], torch.full((3, 5), -1, dtype=torch.int32, device="cuda"), ints([0, 0, 0]), ints([0] * 11))
+    m = Model(c)
+    for call in (lambda x: x.extend([0], [6]), lambda x: x.fork([1, 2], [0, 0], [6, 5]), lambda x: x.extend([0, 1, 2], [1, 3, 1])):
+        want = call(m)
+        got = call(OnLists(c))
+        assert want == got
+    m.same(c)
+    before[:, 3, :, 1] = c.data
+    assert torch.equal(whole.view(torch.int16), before.view(torch.int16))
+
+
+class OnLists:
+    """A cache that takes lists, as the model does."""
+
+    def __init__(self, cache):
+        self.cache = cache
+
+    def extend(self, *lists):
+        return self.cache.extend(*map(ints, lists)).tolist()
+
+    def fork(self, *lists):
+        return self.cache.fork(*map(ints, lists))
+
+
 def test_pages_refusals(P):
     import ctypes
     c = page_cache(P, 6, 3, 8)
@@ -588,6 +664,8 @@ class Sequences:
         assert ((lse.double() - wl).abs()[fin] <= ltol[fin]).all()
 
 
+# chunks of tiles of 16, 128 and 256 rows with four heads to a K/V head
+TILES = [[4, 2], [20, 30], [200, 90]]
 HEADS = [(8, 8, 64), (8, 2, 128), (16, 1, 128), (6, 2, 96), (5, 5, 40), (7, 1, 8), (40, 1, 64), (12, 4, 120)]
 
 
@@ -664,10 +742,6 @@ def test_attend_nan_stays_in_its_row(P, chunks):
     bad[chunks[0]:, 4:] = True
     assert torch.isnan(glse[bad]).all() and torch.isnan(got[bad]).all()
     assert torch.equal(glse[~bad], lse[~bad]) and torch.equal(got[~bad], out[~bad])
-
-
-# chunks of tiles of 16, 128 and 256 rows with four heads to a K/V head
-TILES = [[4, 2], [20, 30], [200, 90]]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
@@ -751,6 +825,49 @@ def test_attend_slots_and_page_ids(P):
     assert torch.isfinite(again).all()
     assert (again[13:] == 0).all() and (l2[13:] == -math.inf).all()
     assert (l2[:13] < lse[:13]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("heads,kv,dim,page", [(8, 2, 128, 16), (8, 2, 64, 4), (4, 1, 40, 1)])
+@pytest.mark.parametrize("chunks", [[1, 1]] + TILES)
+@pytest.mark.parametrize("where", [[0], [-1], [3, 9], [0, 1, 2, 3, 4, 5, 6, 7, 8, -1]])
+def test_attend_pages_outside_the_pool(P, dtype, heads, kv, dim, page, chunks, where):
+    """A page number outside the pool names no tokens: the others' attention is as if its keys were hidden."""
+    lens = [700, 260]
+    s = Sequences(P, lens, chunks, heads, kv, dim, page, dtype, seed=26)
+    for row, bad in ((0, -1), (1, s.cache.refs.numel())):
+        for at in where:
+            s.cache.table[row, at % -(-lens[row] // page)] = bad
+    got = s.cache.attend(1, s.q, offsets=s.offsets, longest=max(chunks), return_lse=True)
+    t0, u, scale = 0, U[dtype], dim ** -0.5
+    for n, x, k, v in zip(lens, chunks, s.k, s.v):
+        missing = [p // page in {at % -(-n // page) for at in where} for p in range(n)]
+        hidden = torch.arange(n, device="cuda") > torch.arange(n - x, n, device="cuda")[:, None]
+        hidden = (hidden | torch.tensor(missing, device="cuda")).repeat(heads // kv, 1)  # [group of queries, keys]
+        for h in range(kv):
+            at = slice(t0, t0 + x), slice(h * (heads // kv), (h + 1) * (heads // kv))
+            q, kk, vv = s.q[at].double().transpose(0, 1).reshape(-1, dim), k[:, h].double(), v[:, h].double()
+            score = (q @ kk.T.contiguous() * scale).masked_fill(hidden, -math.inf)
+            want = torch.logsumexp(score, 1)
+            w = torch.exp(score - want[:, None])
+            o, size = w @ vv, w @ vv.abs()
+            es = (dim + 8) * 2.0 ** -24 * scale * (q.abs() @ kk.abs().T.contiguous()).amax(1)
+            # (fp16 weights are held to 2^-25 under a highest one of 2^7 or more)
+            tol = u * (size + o.abs()) + (torch.exp(2 * es) - 1 + (n + 16) * 2.0 ** -24)[:, None] * size + (
+                2.0 ** -32 * vv.abs().sum(0) if dtype is torch.float16 else 0) + 1e-30
+            y, z = (g[at].transpose(0, 1).flatten(0, 1).double() for g in got)
+            assert ((y - o).abs() <= tol).all()
+            assert ((z - want).abs() <= es + (n + 16) * 2.0 ** -24 + 4 * 2.0 ** -24 * want.abs()).all()
+        t0 += x
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(8, 2, 128), (16, 1, 64)])
+@pytest.mark.parametrize("lens,chunks", [([700, 3000, 90], [130, 40, 90]), ([64, 33, 500], [1, 1, 4])])
+def test_attend_hints(P, heads, kv, dim, lens, chunks):
+    """`longest` chooses tiles of 16, 128 and 256 rows; the result agrees whichever it is, below the rows' length too."""
+    s = Sequences(P, lens, chunks, heads, kv, dim, 16, torch.bfloat16, seed=27)
+    for longest in (1, 2, 5, 8, 20, 33, 70, 200, 5000):
+        s.check(longest=longest)
 
 
 @pytest.mark.parametrize("chunks", [[1, 1, 1], [60, 200, 1]])
