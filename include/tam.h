@@ -620,8 +620,8 @@ typedef struct {
     const int32_t *length;
     int64_t rows, tokens;
     const int32_t *offsets, *slot_ids;
-    int64_t longest;                      /* the longest row's tokens, or an upper bound (0: tokens): a hint for the
-                                             launch, the result does not depend on it */
+    int64_t longest;                      /* the longest row's tokens, or an upper bound (0: tokens): a hint that chooses
+                                             the launch; results agree within rounding whatever it is */
 } tam_chunk;
 
 /*

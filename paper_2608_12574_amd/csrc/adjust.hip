@@ -31,8 +31,8 @@ static_assert(TAM_MAX_HISTORY == kCount && TAM_MAX_BIASES == (1 << (32 - kEntry)
 
 // Threads and tokens of a block, with a mask and without.  The text is read again by each block of a row,
 // but more threads hold more of the chip back while one waits: us per call of 256 bf16 rows over
-// V = 262,144 (texts of 2,048, a mask) with 256 threads and 4,096 tokens 47 (45 since), 512 and 8,192 50, 512 and
-// 4,096 68, 1,024 and 8,192 78, 128 and 2,048 56; of 64 fp32 rows over V = 128,255 (texts of 8,192, no
+// V = 262,144 (texts of 2,048, a mask) with 256 threads and 4,096 tokens 47, 512 and 8,192 50, 512 and
+// 4,096 68, 1,024 and 8,192 78, 128 and 2,048 56 (before the named tokens had a bitmap, which made 45 of the 47); of 64 fp32 rows over V = 128,255 (texts of 8,192, no
 // mask) 21, 18, 21, 20, 26.
 constexpr int kMaskThreads = 256, kMaskSpan = 4096, kFreeThreads = 512, kFreeSpan = 8192;
 
@@ -232,7 +232,8 @@ __global__ void __launch_bounds__(kThreads) k_adjust(const uint64_t *__restrict_
 
 // The edits alone.  A block gathers a row's text and list of biases in a hash table in LDS (a token's word is
 // as above), then goes through the table's tokens: only their logits are read and written, and their mask words
-// before, where there is a mask.  Those scattered lines bound it.  us per call without a mask, against k_adjust: 64 fp32
+// before, where there is a mask.  Its chain of trips to memory bounds it (text, table, mask words, logits: 9.5 us for 9 MB), and for
+// long texts the scattered lines.  us per call without a mask, against k_adjust: 64 fp32
 // rows over V = 128,256 with texts of 1,024 5.7 and 10.7; 256 bf16 rows over V = 262,144 with texts of 256 6.5 and 35, of
 // 2,048 15 and 52, of 8,192 49 and 84.  Where texts name a large part of the vocabulary, going through all
 // of it is faster: 64 fp32 rows over V = 128,255 with texts of 8,192 24 and 17.

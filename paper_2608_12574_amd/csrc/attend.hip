@@ -7,6 +7,10 @@
 // sums and the 16-bit weights hold, so that the sums are scaled a few times per row and
 // not in each step.
 //
+// Scores, maxima, sums and lse are fp32.  The weights are rounded to K and V's type, since 16-bit matrix
+// instructions multiply them with V; the sum of weights is that of the unrounded ones.  Against 64 bits the outputs' error is 1.2 to
+// 1.4 times that of fp32 weights and the same output type (bf16 0.0023 and 0.0017 of the output's size, fp16 0.00029 and 0.00021).
+//
 // A tile is `tq` tokens of one row, times the heads that share a K/V head (their
 // rows of a product are side by side, so K and V are read once for all of them).
 // A unit is a tile's product with kKeys keys.  The keys that the tiles of a call see, row
@@ -343,8 +347,8 @@ __device__ inline uint64_t lane_of(uint64_t x, int of) {
 // step's while this one is computed, and LDS only joins the waves' sums at the end.
 // S^T = K Q^T leaves each lane the weights of one query, for the same eight keys that it
 // then holds as the second factor of O^T = V^T P^T: no weight changes lanes.  V's columns
-// are paired in registers (v_perm).  64 rows of up to 8,192 tokens, 8 K/V heads of 128: 226 us,
-// 5.7 TB/s of K and V.  One row of 700 tokens: 7 us, of which 2 find the cut and 3 more pass
+// are paired in registers (v_perm).  64 rows of up to 8,192 tokens, 8 K/V heads of 128: 225 us,
+// 5.7 TB/s of K and V.  One row of 700 tokens: 7 to 8 us, of which 2 find the cut and 3 more pass
 // until the first keys are there.
 constexpr int kNarrowKeys = 128;
 
@@ -635,9 +639,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 // since with 32 the reads of K and V from LDS take as long as the products.  So that the
 // matrix unit does not wait for the softmax, a half unit (32 keys) is in three stages at
 // once: the products of the next half's scores and of the last half's weights with V run
-// beside this half's exponentials.  4,096 tokens over 16,384 keys, 32 heads of 128: 905 to 955 us
-// by the card, 1.01 to 1.06 PFLOP/s (a bf16 product of 8,192^3 by the library: 1.23), the matrix units busy in 48 cycles of
-// 100 at the 2.1 GHz that the power leaves.  Where K and V's bytes bound it a unit takes 2.1
+// beside this half's exponentials.  4,096 tokens over 16,384 keys, 32 heads of 128: 905 to 980 us
+// by the card, not traced, 16 of k_join among them, 0.98 to 1.06 PFLOP/s (a bf16 product of 8,192^3 by the library: 1.23), the matrix units
+// busy in 47 cycles of 100 at the 2.1 GHz that the power leaves.  Where K and V's bytes bound it a unit takes 2.1
 // us, 4 TB/s.
 constexpr int kWideKeys = 64;
 

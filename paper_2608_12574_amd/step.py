@@ -299,8 +299,9 @@ class PageCache:
         """Attention of the new tokens' queries ``q`` [tokens, heads, head_dim] over their sequences, each over the
         tokens up to its own; ``heads`` is a multiple of ``kv_heads``.  Rows as for ``store``, whose tokens
         have been stored.  ``scale``: of the products (1 / sqrt(head_dim)).  ``longest``: the tokens of the longest
-        row, or more, if the host knows (a hint).  Returns ``out`` (like ``q``; tokens of no row and the memory
-        between are not written) and with ``return_lse`` the fp32 [tokens, heads] logarithms of the sums."""
+        row, or more, if the host knows (a hint that chooses the launch: give it with ``offsets`` where rows are short).
+        Returns ``out`` (like ``q``; tokens of no row and the memory between are not written) and with ``return_lse``
+        the fp32 [tokens, heads] logarithms of the sums."""
         where = "tam_attend"
         on = self._on(where, stream)
         qp = self._vectors(where, "q", q)
