@@ -652,8 +652,103 @@ tam_status tam_pages_store(const tam_chunk *c, const void *k_new, int64_t k_toke
 tam_status tam_attend(const tam_chunk *c, const void *q, int64_t q_token, int64_t q_head, int64_t heads, float scale,
                       void *out, int64_t out_token, int64_t out_head, float *lse, void *work, void *stream);
 
-/* tam_attend_work -- bytes of scratch of tam_attend (-1 on a bad argument). */
+/* tam_attend_work -- bytes of scratch of tam_attend and tam_attend_seen (-1 on a bad argument). */
 int64_t tam_attend_work(const tam_chunk *c, int64_t heads);
+
+/* ---------------------------------------------------------------------------
+ * Trees of drafted tokens.  A row's new tokens (tam_chunk) may be a forest instead of a run of text: token j of the row
+ * follows token p = parents[j] of the row if 0 <= p < j, else the text before the row.  One step of the model then looks at
+ * many continuations at once:
+ *     tam_pages_extend    room for the row's tokens;
+ *     tam_tree_masks      which tokens each one sees, and its depth, once for all layers;
+ *     tam_pages_append    per layer: K, turned by the position that the depth gives, and V into the tokens' places; queries turned;
+ *     tam_attend_seen     per layer: attention over the text and the token's own ancestors;
+ *     tam_pages_accept    the path that the model's choices follow stays in the cache, the rest is cut off.
+ */
+
+/*
+ * tam_tree_masks -- bit j % 64 of word seen[t][j / 64] says whether token t sees token j of its row: itself and its ancestors.
+ * depth[t]: the number of its ancestors.
+ *   parents  device int32[tokens].
+ *   offsets  device int32[rows + 1], as in tam_chunk (NULL: one token per row).
+ *   seen     device uint64[tokens][words], words >= 1; bits of tokens 64 * words and on are left out.
+ *   depth    device int32[tokens].
+ * Tokens of no row are not written.  Errors: TAM_E_INVAL, TAM_E_DEVICE.
+ */
+tam_status tam_tree_masks(const int32_t *parents, const int32_t *offsets, int64_t rows, int64_t tokens, uint64_t *seen,
+                          int64_t words, int32_t *depth, void *stream);
+
+/* How K and queries turn by their positions: pair i of a vector by position * frequencies[i], from its first element
+ * to its second. */
+typedef struct {
+    const float *frequencies;  /* device float[pairs], radians per token */
+    int64_t pairs;             /* 0 .. head_dim / 2, a multiple of 4; the elements from 2 * pairs on stay as they are */
+    int adjacent;              /* pair i is elements 2 i and 2 i + 1 (1), or i and pairs + i (0) */
+    const int32_t *depth;      /* device int32[tokens]: a token's position is its row's first one's and this; NULL: its place */
+} tam_rotation;
+
+/*
+ * tam_pages_append -- tam_pages_store of the new tokens with K turned by their positions, and their queries turned alike:
+ * out[t][h] of q[t][h].  Angles are exact to fp32 at any position; elements are turned in fp32 and rounded once.  The
+ * tokens' places do not depend on `depth`.
+ *   k_new, v_new   as for tam_pages_store; the tokens that are left out there are here too.
+ *   q, heads, out  as for tam_attend (any number of heads); heads == 0: no queries.  Every token of a row is written; `out` may be
+ *                  `q` itself, with its strides.
+ * Errors: TAM_E_INVAL, TAM_E_DEVICE.
+ */
+tam_status tam_pages_append(const tam_chunk *c, const tam_rotation *r, const void *k_new, int64_t k_token, int64_t k_head,
+                            const void *v_new, int64_t v_token, int64_t v_head, const void *q, int64_t q_token, int64_t q_head,
+                            int64_t heads, void *out, int64_t out_token, int64_t out_head, void *stream);
+
+/*
+ * tam_attend_seen -- tam_attend with a mask among the row's new tokens: a token sees the keys of its slot before the row's
+ * first token, and token j of the row if j < 64 * words and bit j % 64 of seen[t * seen_stride + j / 64] is set (its own and
+ * later ones too).  Bits of tokens that the row does not have are not looked at.
+ *   seen  device uint64, 8-byte aligned; words >= 1; seen_stride >= words.
+ */
+tam_status tam_attend_seen(const tam_chunk *c, const void *q, int64_t q_token, int64_t q_head, int64_t heads, float scale,
+                           const uint64_t *seen, int64_t words, int64_t seen_stride, void *out, int64_t out_token,
+                           int64_t out_head, float *lse, void *work, void *stream);
+
+/*
+ * tam_pages_accept -- the row's token 0 stays, and after a token that stays the first token of the row that follows it
+ * (`parents`) and is picks[of the token that stays].  K and V of those that stay move, in every plane, to the places after
+ * the text before the row in the order of their depth; the slot ends behind them, and pages past its end are given back
+ * (their table entries become -1).
+ *   c, n     the cache, and the new tokens of the call: n names c's tables, and its strides, kv_heads, head_dim and dtype
+ *            say where a vector lies in a page; k and v are not read.
+ *   tokens, picks, parents  device int32[n->tokens]: the drafted tokens, the model's choice after each, their parents.
+ *   path     device int32[n->tokens]: the numbers, in the row, of its tokens that stay, then -1.
+ *   count    device int32[n->rows]: how many stay (0 for a row without tokens or outside the slots, which changes nothing).
+ *   last     device int32[n->rows]: the choice after the last of them (-1 if none): the next token of the text.
+ *   work     tam_pages_accept_work(n) bytes.
+ * The slots of the rows are distinct, and the pages of the rows' tokens their own (as tam_pages_extend leaves them).
+ * Tokens without a place (tam_pages_store) do not move.  Errors: TAM_E_INVAL, TAM_E_DEVICE.
+ */
+tam_status tam_pages_accept(const tam_pages *c, const tam_chunk *n, const int32_t *tokens, const int32_t *picks,
+                            const int32_t *parents, int32_t *path, int32_t *count, int32_t *last, void *work, void *stream);
+
+/* tam_pages_accept_work -- bytes of scratch of tam_pages_accept (-1 on a bad argument). */
+int64_t tam_pages_accept_work(const tam_chunk *n);
+
+enum { TAM_MAX_TOP = 64, TAM_MAX_TOP_COLUMNS = 1 << 21, TAM_MAX_TOP_ROWS = 65535 };
+
+/*
+ * tam_top_tokens -- the k largest logits of each row: tokens[b][i] is the token of the i-th largest, of equal ones the lowest
+ * token first, logprobs[b][i] its logit - lse[b], and lse[b] = log sum_v exp(logits[b][v]), in fp32.  -inf is no logit:
+ * where fewer than k are left, the rest of the row is token -1 at -inf.  A NaN is larger than every number, and makes
+ * lse and all of its row's logprobs NaN; -0 equals 0.
+ *   logits   device, as for tam_apply_mask (TAM_DTYPE_FP32 or TAM_DTYPE_BF16), V in 1 .. TAM_MAX_TOP_COLUMNS, B in
+ *            0 .. TAM_MAX_TOP_ROWS, row_stride >= 0 (rows may overlap).
+ *   tokens   device int32[B][k], 1 <= k <= TAM_MAX_TOP;  logprobs  device float[B][k];  lse  device float[B], or NULL.
+ *   work     tam_top_tokens_work(B, V, k, dtype) bytes (NULL if that is 0).
+ * Errors: TAM_E_INVAL, TAM_E_DEVICE.
+ */
+tam_status tam_top_tokens(const void *logits, int dtype, int64_t B, int64_t V, int64_t row_stride, int64_t k, int32_t *tokens,
+                          float *logprobs, float *lse, void *work, void *stream);
+
+/* tam_top_tokens_work -- bytes of scratch of tam_top_tokens (-1 on a bad argument). */
+int64_t tam_top_tokens_work(int64_t B, int64_t V, int64_t k, int dtype);
 
 /* Message of the last failing call on this thread ("" if none). */
 const char *tam_last_error(void);

@@ -60,6 +60,9 @@ struct Attend {
     int32_t unit, extra;  // keys of a unit, a power of two; keys that stand for a tile's own cost
     float *sums;    // [2 blocks][tile rows][DP] partial sums, then [2 blocks][tile rows][2] their m and sum of weights
     struct Cut *cuts;  // [blocks] what each block's piece begins with
+    // kSeen: which of the row's tokens each one sees
+    const uint64_t *seen;
+    int64_t seen_stride, seen_words;
 };
 
 // The tile in whose middle a block's piece begins.
@@ -109,17 +112,23 @@ __device__ inline Row uniform(Row r) {
     return r;
 }
 
-// Keys on the line before tile t of a row and head: tile i < t sees base + (i + 1) tq.
+// In what follows, kSeen: a token sees what lies before its row's tokens, and those of them that its bits name, so that all tiles
+// of a row go through all of its keys.
+
+// Keys on the line before tile t of a row and head: tile i < t sees base + (i + 1) tq, or all.
+template <bool kSeen>
 __device__ inline int64_t keys_before(const Attend &a, const Row &r, int64_t t) {
+    if constexpr (kSeen) return t * ((int64_t)max(r.base, 0) + r.n + a.extra);
     return t * (max(r.base, 0) + a.extra) + a.tq * (t * (t + 1) / 2);
 }
 
 // Keys on the line of a row and head.  A row of one tile takes whole units, so that a
 // batch of them is cut between units.
+template <bool kSeen>
 __device__ inline int64_t row_keys(const Attend &a, const Row &r) {
     const int64_t all = (int64_t)max(r.base, 0) + r.n + a.extra;
     if (r.n <= a.tq) return r.n ? (all + a.unit - 1) & -(int64_t)a.unit : 0;
-    return keys_before(a, r, (r.n - 1) / a.tq) + all;
+    return keys_before<kSeen>(a, r, (r.n - 1) / a.tq) + all;
 }
 
 // A place on the line.
@@ -131,6 +140,7 @@ struct Place {
 
 // Where piece number `share` (this block's) begins, and the keys of a piece.  All threads of
 // the block call it; row < 0 past the line's end.
+template <bool kSeen>
 __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
     __shared__ int64_t sums[kThreads / kWave];
     __shared__ int64_t found[2];
@@ -142,7 +152,7 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
     Row r{};
     for (int64_t i = lo; i < hi; ++i) {
         r = row_at(a, i);
-        mine += heads * row_keys(a, r);
+        mine += heads * row_keys<kSeen>(a, r);
     }
     int64_t upto = mine;
 #pragma unroll
@@ -170,7 +180,7 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
         if (per > 1) {
             for (; i < hi; ++i) {
                 r = row_at(a, i);
-                const int64_t u = heads * row_keys(a, r);
+                const int64_t u = heads * row_keys<kSeen>(a, r);
                 if (rest < u) break;
                 rest -= u;
             }
@@ -194,14 +204,15 @@ struct Tile {
     int64_t rest, keys;           // keys of it on the line before the place, and all of them
 };
 
+template <bool kSeen>
 __device__ inline Tile tile_at(const Attend &a, const Row &r, int64_t rest) {
-    const int64_t u = row_keys(a, r);
+    const int64_t u = row_keys<kSeen>(a, r);
     const int32_t vh = (int32_t)(rest / u);
     rest -= vh * u;
     int32_t lo = 0, hi = (r.n + a.tq - 1) / a.tq;  // keys_before(lo) <= rest < keys_before(hi)
     while (hi - lo > 1) {
         const int32_t mid = (lo + hi) >> 1;
-        if (keys_before(a, r, mid) <= rest) lo = mid;
+        if (keys_before<kSeen>(a, r, mid) <= rest) lo = mid;
         else hi = mid;
     }
     Tile t;
@@ -211,8 +222,8 @@ __device__ inline Tile tile_at(const Attend &a, const Row &r, int64_t rest) {
     t.first = lo * a.tq;
     t.n = min(a.tq, r.n - t.first);
     t.heads = min(a.group, a.heads / a.kv_heads - t.part * a.group);
-    t.rest = rest - keys_before(a, r, lo);
-    t.keys = r.n <= a.tq ? u : (int64_t)max(r.base, 0) + t.first + t.n + a.extra;
+    t.rest = rest - keys_before<kSeen>(a, r, lo);
+    t.keys = r.n <= a.tq ? u : (int64_t)max(r.base, 0) + (kSeen ? r.n : t.first + t.n) + a.extra;
     return t;
 }
 
@@ -329,6 +340,21 @@ __device__ inline float not_finite(uint16_t x) {
     return (x & kAll) == kAll ? to_float<kHalf>(x) : 0.f;
 }
 
+// kSeen: bit i says whether a token (of the call's) sees key k0 + i of its sequence; 32 keys, of which those past the row's
+// tokens are not seen.
+__device__ inline uint32_t seen_of(const Attend &a, const Row &r, int64_t token, int32_t k0) {
+    const int32_t at = k0 - r.base, end = r.n - at;  // k0 among the row's tokens; bits from `end` on are past them
+    if (at <= -32) return 0xFFFFFFFFu;
+    if (end <= 0) return 0;
+    const uint64_t *const row = a.seen + token * a.seen_stride;
+    const int32_t w = max(at, 0) >> 6, in = max(at, 0) & 63;
+    uint64_t x = w < a.seen_words ? row[w] >> in : 0;
+    if (in > 32 && w + 1 < a.seen_words) x |= row[w + 1] << (64 - in);
+    uint32_t y = (uint32_t)x;
+    if (at < 0) y = y << -at | ((1u << -at) - 1);
+    return end < 32 ? y & ((1u << end) - 1) : y;
+}
+
 // V of a key, of a head of which `v` is the first element, or null where the key lies in no page.
 __device__ inline const uint16_t *v_of(const Attend &a, const uint16_t *v, const int32_t *pages, int32_t key) {
     const int32_t id = pages[(uint32_t)key >> a.shift];
@@ -352,7 +378,7 @@ __device__ inline uint64_t lane_of(uint64_t x, int of) {
 // until the first keys are there.
 constexpr int kNarrowKeys = 128;
 
-template <int DP, bool kHalf, bool kRuns>
+template <int DP, bool kHalf, bool kRuns, bool kSeen>
 __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
     constexpr int kKeys = kNarrowKeys;
     constexpr int kSteps = DP / 32;  // products of 32 dimensions
@@ -372,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
         k_in[s] = 2 * ((32 * s + 8 * grp < a.dim ? 32 * s + 8 * grp : 0) + (kRuns ? (uint32_t)col * (uint32_t)a.token_stride : 0));
     const uint32_t v_in = 2 * ((kCols * col < a.dim ? kCols * col : 0) + (kRuns ? (uint32_t)(4 * grp) * (uint32_t)a.token_stride : 0));
     int64_t piece;
-    Place p = find(a, blockIdx.x, &piece);
+    Place p = find<kSeen>(a, blockIdx.x, &piece);
     if (p.row < 0) {
         if (threadIdx.x == 0) a.cuts[blockIdx.x].is = 0;
         return;
@@ -383,12 +409,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
     const float c = a.scale * kLog2e;
     while (left > 0) {
         const Row r = p.r;
-        if (p.rest >= row_keys(a, r) * a.kv_heads * a.parts) {
+        if (p.rest >= row_keys<kSeen>(a, r) * a.kv_heads * a.parts) {
             p.r = uniform(row_at(a, ++p.row));
             p.rest = 0;
             continue;
         }
-        const Tile t = tile_at(a, r, p.rest);
+        const Tile t = tile_at<kSeen>(a, r, p.rest);
         const Share share = share_of<kKeys>(a, t, left);
         if (left == whole_piece) note<kKeys>(a, blockIdx.x, r, t, piece);
         p.rest += t.keys - t.rest;
@@ -398,10 +424,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
         // dimension read others of the vector (queries: zero).
         u32x4 q[kSteps];
         const int32_t all = max(0, r.base + r.n);  // tokens of the sequence, chunk included
-        const int32_t most = max(0, min(r.base + t.first + t.n, all)), least = max(0, min(r.base + t.first + 1, all));
+        const int32_t most = kSeen ? all : max(0, min(r.base + t.first + t.n, all));
+        const int32_t least = max(0, min(kSeen ? r.base : r.base + t.first + 1, all));
         const int row = col, tok = row / t.heads, h = row - tok * t.heads;
         const bool is = tok < t.n;
-        const int32_t seen = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;  // keys that the query sees
+        const int32_t seen = !is ? 0 : kSeen ? all : max(0, min(r.base + t.first + tok + 1, all));  // keys that the query sees
         const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
                               (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
 #pragma unroll
@@ -495,6 +522,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
                 for (int d = 0; d < kSteps; ++d) s[i] = mfma16<kHalf>(x.k[i][d], q[d], s[i]);
             if (__builtin_expect(k0 + 32 > clear, 0)) {
                 asm volatile("");
+                if constexpr (kSeen) have &= is ? seen_of(a, r, r.first + t.first + tok, k0) : 0;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const int key = 16 * (j / 4) + 4 * grp + j % 4;
@@ -590,8 +618,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
                 for (int j = 0; j < kCols; ++j) sum[j] += joint[w][out_row][d0 + j];
             }
             if (least < most && __builtin_expect(odd[0] | odd[1] | odd[2] | odd[3], 0) && d0 < a.dim) {
-                const int32_t end = min(min(r.base + t.first + out_tok + 1, most), share.to * kKeys);
+                const int32_t end = min(kSeen ? most : min(r.base + t.first + out_tok + 1, most), share.to * kKeys);
                 for (int32_t k = max(least, share.from * kKeys); k < end; ++k) {
+                    if (kSeen && !(seen_of(a, r, r.first + t.first + out_tok, k) & 1)) continue;
                     const uint16_t *v = v_of(a, a.v + (int64_t)t.head * a.head_stride + d0, pages, k);
                     if (!v) continue;
 #pragma unroll
@@ -647,7 +676,7 @@ constexpr int kWideKeys = 64;
 
 // What is not finite in V of the keys from .. to - 1, added to the sums or outputs that this lane has written (lanes and rows as
 // below).  Apart from these, and from the thread's number on, so that it takes none of their registers.
-template <int DP, int kBlocks, bool kHalf>
+template <int DP, int kBlocks, bool kHalf, bool kSeen>
 __device__ inline void add_values(const Attend &a, const Row &r, const Tile &t, int32_t from, int32_t to, bool whole, int64_t at) {
     constexpr int kWaveRows = 32 * kBlocks, kRows = 4 * kWaveRows;
     int32_t thread = threadIdx.x;
@@ -660,9 +689,10 @@ __device__ inline void add_values(const Attend &a, const Row &r, const Tile &t, 
         const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
         uint16_t *const out = a.out + token * a.out_token + head * a.out_head;
         float *const sum = a.sums + (at * kRows + row) * DP;
-        const int32_t end = min(to, r.base + t.first + tok + 1);
+        const int32_t end = kSeen ? to : min(to, r.base + t.first + tok + 1);
 #pragma unroll 1
         for (int32_t key = from; key < end; ++key) {
+            if (kSeen && !(seen_of(a, r, token, key) & 1)) continue;
             const uint16_t *const v = v_of(a, a.v + (int64_t)t.head * a.head_stride, pages, key);
             if (!v) continue;
 #pragma unroll 1
@@ -676,7 +706,7 @@ __device__ inline void add_values(const Attend &a, const Row &r, const Tile &t, 
     }
 }
 
-template <int DP, int kBlocks, bool kHalf, bool kRuns>
+template <int DP, int kBlocks, bool kHalf, bool kRuns, bool kSeen>
 __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_attend_wide(Attend a) {
     constexpr int kWaveRows = 32 * kBlocks, kRows = 4 * kWaveRows;
     constexpr int kPieces = DP / 8;            // 16-byte pieces of a key
@@ -696,7 +726,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
     int32_t number = 0;
     if (threadIdx.x == 0) odd = 0;
     int64_t piece;
-    Place p = find(a, block, &piece);
+    Place p = find<kSeen>(a, block, &piece);
     if (p.row < 0) {
         if (threadIdx.x == 0) a.cuts[block].is = 0;
         return;
@@ -723,20 +753,20 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
 
     while (left > 0) {
         const Row r = p.r;
-        if (p.rest >= row_keys(a, r) * a.kv_heads * a.parts) {
+        if (p.rest >= row_keys<kSeen>(a, r) * a.kv_heads * a.parts) {
             p.r = uniform(row_at(a, ++p.row));
             p.rest = 0;
             continue;
         }
-        const Tile t = tile_at(a, r, p.rest);
+        const Tile t = tile_at<kSeen>(a, r, p.rest);
         const Share share = share_of<kWideKeys>(a, t, left);
         if (left == whole_piece) note<kWideKeys>(a, block, r, t, piece);
         p.rest += t.keys - t.rest;
         left -= t.keys - t.rest;
         if (share.from == share.to) continue;  // (the piece ends before the next unit)
         const int32_t all = max(0, r.base + r.n);
-        const int32_t most = max(0, min(r.base + t.first + t.n, all));
-        const int32_t shared_keys = max(0, min(r.base + t.first + 1, all));  // that every query of the tile's sees
+        const int32_t most = kSeen ? all : max(0, min(r.base + t.first + t.n, all));
+        const int32_t shared_keys = max(0, min(kSeen ? r.base : r.base + t.first + 1, all));  // that every query of the tile's sees
         ++number;
         u32x4 q[kBlocks][kSteps];
         int32_t seen[kBlocks];
@@ -744,7 +774,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         for (int b = 0; b < kBlocks; ++b) {
             const int row = kWaveRows * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
             const bool is = tok < t.n;
-            seen[b] = is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
+            // (kSeen: the token)
+            seen[b] = kSeen ? (is ? r.first + t.first + tok : -1) : is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
             const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
                                   (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
 #pragma unroll
@@ -755,7 +786,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         }
         // keys that every query of the wave's sees (what rows past the tile's come to is written nowhere)
         const int32_t least = kWaveRows * wave / t.heads < t.n
-                                  ? max(0, min(r.base + t.first + kWaveRows * wave / t.heads + 1, all)) : INT_MAX;
+                                  ? (kSeen ? shared_keys : max(0, min(r.base + t.first + kWaveRows * wave / t.heads + 1, all))) : INT_MAX;
         f32x16 o[kBlocks][kCols], sa[kBlocks], sb[kBlocks];
         u32x4 pa[kBlocks][2], pb[kBlocks][2];
         // m and m c; the score above which m follows; sums of weights; the highest of the last scores (this lane's)
@@ -858,8 +889,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                 const uint32_t ok = (uint32_t)(__ballot((uint32_t)id < (uint32_t)a.pages) >> 32 * h);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    const int32_t rest = seen[b] - k0 - 4 * half;
-                    const uint32_t have = ok >> 4 * half;
+                    const int32_t rest = kSeen ? 32 : seen[b] - k0 - 4 * half;
+                    const uint32_t have = (kSeen ? ok & (seen[b] < 0 ? 0 : seen_of(a, r, seen[b], k0)) : ok) >> 4 * half;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int x = 8 * (i / 4) + i % 4;
@@ -1060,7 +1091,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         }
         // (`odd` was written before the last barrier, and the next tile writes it after one)
         if (__builtin_expect(k1 > shared_keys && shared_keys < most && odd == number, 0))
-            add_values<DP, kBlocks, kHalf>(a, r, t, max(k0, shared_keys), min(k1, most), whole, at);
+            add_values<DP, kBlocks, kHalf, kSeen>(a, r, t, max(k0, shared_keys), min(k1, most), whole, at);
     }
 }
 
@@ -1182,25 +1213,30 @@ bool runs(const Attend &a) {
     return a.shift >= 4 && a.page_stride <= INT32_MAX && a.token_stride <= (INT32_MAX / 2) >> a.shift;
 }
 
-template <int DP, int kBlocks, bool kHalf>
+template <int DP, int kBlocks, bool kHalf, bool kSeen>
 hipError_t launch_wide(const Attend &a, hipStream_t s) {
     constexpr size_t kLds = 2 * kWideKeys * (DP + 8 + DP + 16) * sizeof(uint16_t);
     if (runs(a))
-        hipLaunchKernelGGL((k_attend_wide<DP, kBlocks, kHalf, true>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
+        hipLaunchKernelGGL((k_attend_wide<DP, kBlocks, kHalf, true, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
     else
-        hipLaunchKernelGGL((k_attend_wide<DP, kBlocks, kHalf, false>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
+        hipLaunchKernelGGL((k_attend_wide<DP, kBlocks, kHalf, false, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
     return launch_join<DP, 128 * kBlocks, kHalf>(a, s);
+}
+
+template <int DP, bool kHalf, bool kSeen>
+hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
+    if (sh.rows == 256) return launch_wide<DP, 2, kHalf, kSeen>(a, s);
+    if (sh.rows == 128) return launch_wide<DP, 1, kHalf, kSeen>(a, s);
+    if (runs(a))
+        hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, true, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, false, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
+    return launch_join<DP, 16, kHalf>(a, s);
 }
 
 template <int DP, bool kHalf>
 hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
-    if (sh.rows == 256) return launch_wide<DP, 2, kHalf>(a, s);
-    if (sh.rows == 128) return launch_wide<DP, 1, kHalf>(a, s);
-    if (runs(a))
-        hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, true>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, false>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
-    return launch_join<DP, 16, kHalf>(a, s);
+    return a.seen ? launch<DP, kHalf, true>(a, sh, s) : launch<DP, kHalf, false>(a, sh, s);
 }
 
 }  // namespace
@@ -1210,7 +1246,7 @@ int64_t attend_work_bytes(const tam_chunk &c, int64_t heads) {
     return 2 * (int64_t)sh.grid * sh.rows * (padded(c.head_dim) + 2) * 4 + sh.grid * (int64_t)sizeof(Cut);
 }
 
-hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipStream_t s) {
+hipError_t launch_attend(const tam_chunk &c, const Queries &q, const Seen &seen, void *work, hipStream_t s) {
     const Shape sh = shape_of(c, q.heads);
     const int64_t group = q.heads / c.kv_heads;
     Attend a{static_cast<const uint16_t *>(c.k), static_cast<const uint16_t *>(c.v),
@@ -1218,7 +1254,7 @@ hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipSt
              c.head_stride, c.token_stride, q.q_token, q.q_head, q.out_token, q.out_head, c.table, c.length,
              c.offsets, c.slot_ids, c.table_stride, c.slots, c.max_pages, c.rows, c.tokens, (int32_t)c.num_pages,
              __builtin_ctzll((unsigned long long)c.page_tokens), (int32_t)q.heads, (int32_t)c.kv_heads,
-             (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, 0, nullptr, nullptr};
+             (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, 0, nullptr, nullptr, seen.bits, seen.stride, seen.words};
     a.group = (int32_t)std::min<int64_t>(group, sh.rows);
     a.parts = (int32_t)((group + a.group - 1) / a.group);
     a.tq = sh.rows / a.group;

@@ -1,5 +1,5 @@
-// Launchers of the decode step's operators beside the mask (adjust.hip,
-// attend.hip, pages.hip) and what their C entry points (step_api.cpp) share.
+// Launchers of the decode step's operators beside the mask (adjust.hip, append.hip,
+// attend.hip, pages.hip, top.hip, trees.hip) and what their C entry points (step_api.cpp) share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -39,7 +39,35 @@ struct Queries {
     int64_t heads;
     float scale;
 };
-hipError_t launch_attend(const tam_chunk &c, const Queries &q, void *work, hipStream_t s);
+// which of its row's tokens each one sees (tam_attend_seen); bits null: those up to itself
+struct Seen {
+    const uint64_t *bits;
+    int64_t words, stride;
+};
+hipError_t launch_attend(const tam_chunk &c, const Queries &q, const Seen &seen, void *work, hipStream_t s);
 int64_t attend_work_bytes(const tam_chunk &c, int64_t heads);
+
+// what tam_pages_append is called with beside the chunk and the rotation
+struct Fresh {
+    const void *k;
+    int64_t k_token, k_head;
+    const void *v;
+    int64_t v_token, v_head;
+    const void *q;
+    int64_t q_token, q_head, heads;
+    void *out;
+    int64_t out_token, out_head;
+};
+hipError_t launch_pages_append(const tam_chunk &c, const tam_rotation &r, const Fresh &x, hipStream_t s);
+
+hipError_t launch_tree_masks(const int32_t *parents, const int32_t *offsets, int64_t rows, int64_t tokens, uint64_t *seen,
+                             int64_t words, int32_t *depth, hipStream_t s);
+hipError_t launch_pages_accept(const tam_pages &c, const tam_chunk &n, const int32_t *tokens, const int32_t *picks,
+                               const int32_t *parents, int32_t *path, int32_t *count, int32_t *last, void *work, hipStream_t s);
+int64_t accept_work_bytes(const tam_chunk &n);
+
+hipError_t launch_top_tokens(const void *logits, int dtype, int64_t B, int64_t V, int64_t row_stride, int k, int32_t *tokens,
+                             float *logprobs, float *lse, void *work, hipStream_t s);
+int64_t top_work_bytes(int64_t B, int64_t V, int k, int dtype);
 
 }  // namespace tam

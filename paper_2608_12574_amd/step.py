@@ -1,4 +1,4 @@
-"""What a decode step does beside the mask: edits of logits, and a paged K/V cache.
+"""What a decode step does beside the mask: edits of logits, the best tokens, trees of drafted tokens, and a paged K/V cache.
 
 As in ``tam``, this module marshals arguments only; every step runs in
 ``libtam.so`` on the stream given, or torch's current stream.  The tensors and the stream of a call
@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 
 from . import tam as _tam
-from .tam import DTYPE_BF16, DTYPE_FP16, TAM_OK, Chunk, Edits, Pages, TamError, _calls, _check
+from .tam import DTYPE_BF16, DTYPE_FP16, TAM_OK, Chunk, Edits, Pages, Rotation, TamError, _calls, _check
 
 
 def _bad(where, what):
@@ -131,6 +131,80 @@ def adjust_logits(logits, tokens=None, length=None, prompt=None, repetition=None
                    repetition=repetition, frequency=frequency, presence=presence, bias_ids=bias_ids, bias=bias)
 
 
+def _scratch(shape, dtype, device, stream):
+    """Memory for a call on ``stream``: from that stream's share of torch's allocator, so that
+    nothing still running on another stream holds it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def top_tokens(logits, k, return_lse=False, stream=None):
+    """The ``k`` (1 to 64) largest of each row of ``logits`` [B, V] (fp32 or bf16), as ``adjust_logits`` or ``apply_mask``
+    leave them: (int32 [B, k] tokens, fp32 [B, k] log probabilities) in descending order, of equal logits the lowest token
+    first, and with ``return_lse`` the fp32 [B] logarithms of the sums.  Where fewer than ``k`` logits are left (-inf is
+    none), the rest is token -1 at -inf.  A NaN is larger than every number, and its row's log probabilities are NaN."""
+    import torch
+    where = "tam_top_tokens"
+    c = _tam._calls_made if _int is not None else _ready()
+    dtype = c.dtypes.get(logits.dtype)
+    if dtype is None or not logits.is_cuda or logits.dim() != 2:
+        raise _bad(where, "logits must be a [B, V] fp32 or bf16 tensor on the GPU")
+    gpu = logits.get_device()
+    on = _stream(where, c, stream, gpu)
+    B, V = logits.shape
+    row_stride, step = logits.stride()
+    if V > 1 and step != 1:
+        raise _bad(where, "logits must have contiguous rows")
+    row_stride = row_stride if B > 1 else V
+    lib = _tam.lib()
+    size = lib.tam_top_tokens_work(B, V, k, dtype)
+    if size < 0:
+        _check(-1, where)
+    device = logits.device
+    tokens, logprobs = _scratch((B, k), _int, device, stream), _scratch((B, k), _float, device, stream)
+    lse = _scratch(B, _float, device, stream) if return_lse else None
+    work = _scratch(size, torch.uint8, device, stream) if size else None
+    rc = lib.tam_top_tokens(logits.data_ptr(), dtype, B, V, row_stride, k, tokens.data_ptr(), logprobs.data_ptr(),
+                            lse.data_ptr() if return_lse else None, work.data_ptr() if size else None, on)
+    if rc != TAM_OK:
+        _check(rc, where)
+    return (tokens, logprobs, lse) if return_lse else (tokens, logprobs)
+
+
+def tree_masks(parents, offsets=None, longest=None, stream=None):
+    """Which tokens of its row each drafted token sees.  ``parents`` int32 [tokens]: the number, in its row, of the
+    token that each one follows; -1 (or whatever is no earlier token of the row): the text before the row.  Row i is
+    ``offsets[i]:offsets[i + 1]`` (one token per row without ``offsets``).  ``longest``: tokens of the longest row, or more, if the
+    host knows (else all of them): the width of the masks.  Returns (int64 [tokens, ceil(longest / 64)]: bit j % 64 of word
+    j // 64 is set for the token itself and its ancestors, as ``PageCache.attend`` takes it; int32 [tokens]: how many ancestors,
+    as ``PageCache.append`` takes it).  Tokens of no row are not written."""
+    where = "tam_tree_masks"
+    c = _tam._calls_made if _int is not None else _ready()
+    if not parents.is_cuda:
+        raise _bad(where, "parents must lie on the GPU")
+    gpu = parents.get_device()
+    on = _stream(where, c, stream, gpu)
+    T = parents.numel()
+    up = _int32(where, "parents", parents, T, gpu)
+    rows, off = T, None
+    if offsets is not None:
+        rows = offsets.numel() - 1
+        if rows < 0:
+            raise _bad(where, "offsets must be [rows + 1]")
+        off = _int32(where, "offsets", offsets, rows + 1, gpu)
+    if longest is None:
+        longest = T if offsets is not None else 1
+    words = max(1, (longest + 63) // 64)
+    seen, depth = _scratch((T, words), _long, parents.device, stream), _scratch(T, _int, parents.device, stream)
+    rc = _tam.lib().tam_tree_masks(up, off, rows, T, seen.data_ptr(), words, depth.data_ptr(), on)
+    if rc != TAM_OK:
+        _check(rc, where)
+    return seen, depth
+
+
 class PageCache:
     """A paged K/V cache.
 
@@ -187,13 +261,7 @@ class PageCache:
 
     # -- pages -----------------------------------------------------------------
     def _empty(self, shape, dtype, stream):
-        """Memory for a call on ``stream``: from that stream's share of torch's allocator, so that
-        nothing still running on another stream holds it."""
-        torch = self._torch
-        if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self._device)
-        with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=dtype, device=self._device)
+        return _scratch(shape, dtype, self._device, stream)
 
     def _work(self, stream):
         return self._empty(self._work_bytes, self._torch.uint8, stream)
@@ -294,15 +362,52 @@ class PageCache:
         if rc != TAM_OK:
             _check(rc, where)
 
+    def append(self, layer, q, k, v, frequencies, depth=None, adjacent=False, offsets=None, slots=None, longest=None,
+               out=None, stream=None):
+        """``store`` of ``k`` and ``v`` with K turned by its tokens' positions; returns ``q`` [tokens, heads, head_dim] turned
+        alike (into ``out``, which may be ``q``; ``q`` None: no queries).  ``frequencies`` fp32 [pairs]: pair i of a vector, its
+        elements i and pairs + i, or with ``adjacent`` 2 i and 2 i + 1, turns by position * frequencies[i]; what follows the
+        pairs (a multiple of 4) stays.  A token's position is its place in its sequence, or with ``depth`` int32 [tokens] that
+        many after the place of its row's first token (``tree_masks``).  Tokens of no row are not written."""
+        where = "tam_pages_append"
+        on = self._on(where, stream)
+        kp, vp = self._vectors(where, "k", k, self.kv_heads), self._vectors(where, "v", v, self.kv_heads)
+        T = k.shape[0]
+        qp = op = (None, 0, 0)
+        heads = 0
+        if q is not None:
+            qp, heads = self._vectors(where, "q", q), q.shape[1]
+            if out is None:
+                out = self._empty((T, heads, self.head_dim), q.dtype, stream)
+            elif out.shape != q.shape:
+                raise _bad(where, "out must have q's shape")
+            op = self._vectors(where, "out", out)
+        elif out is not None:
+            raise _bad(where, "out without q")
+        if v.shape[0] != T or (q is not None and q.shape[0] != T):
+            raise _bad(where, "q, k and v have different numbers of tokens")
+        if frequencies.dtype is not _float or frequencies.get_device() != self._gpu or frequencies.dim() != 1 or (
+                not frequencies.is_contiguous()):
+            raise _bad(where, f"frequencies must be a contiguous [pairs] fp32 tensor on cuda:{self._gpu}")
+        turn = Rotation(frequencies.data_ptr(), frequencies.numel(), bool(adjacent),
+                        None if depth is None else _int32(where, "depth", depth, T, self._gpu))
+        rc = self._lib.tam_pages_append(self._new(where, layer, T, offsets, slots, longest), ctypes.byref(turn), *kp, *vp,
+                                        *qp, heads, *op, on)
+        if rc != TAM_OK:
+            _check(rc, where)
+        return out
+
     def attend(self, layer, q, offsets=None, slots=None, longest=None, scale=None, out=None, return_lse=False,
-               stream=None):
+               seen=None, stream=None):
         """Attention of the new tokens' queries ``q`` [tokens, heads, head_dim] over their sequences, each over the
         tokens up to its own; ``heads`` is a multiple of ``kv_heads``.  Rows as for ``store``, whose tokens
         have been stored.  ``scale``: of the products (1 / sqrt(head_dim)).  ``longest``: the tokens of the longest
         row, or more, if the host knows (a hint that chooses the launch: give it with ``offsets`` where rows are short).
+        ``seen`` int64 [tokens, words]: a token sees, of its row's tokens, those j whose bit j % 64 of word j // 64 is set
+        (``tree_masks``; any will do), instead of those up to itself, and all that lies before the row's first one.
         Returns ``out`` (like ``q``; tokens of no row and the memory between are not written) and with ``return_lse``
         the fp32 [tokens, heads] logarithms of the sums."""
-        where = "tam_attend"
+        where = "tam_attend" if seen is None else "tam_attend_seen"
         on = self._on(where, stream)
         qp = self._vectors(where, "q", q)
         T, heads = q.shape[0], q.shape[1]
@@ -318,8 +423,39 @@ class PageCache:
         if size < 0:
             _check(-1, where)
         work = self._empty(size, self._torch.uint8, stream) if size else None
-        rc = lib.tam_attend(chunk, *qp, heads, self.head_dim ** -0.5 if scale is None else scale, *op,
-                            lse.data_ptr() if return_lse else None, work.data_ptr() if size else None, on)
+        scale = self.head_dim ** -0.5 if scale is None else scale
+        rest = *op, lse.data_ptr() if return_lse else None, work.data_ptr() if size else None, on
+        if seen is None:
+            rc = lib.tam_attend(chunk, *qp, heads, scale, *rest)
+        else:
+            bits, stride, words = _rows_of(where, "seen", seen, T, _long, self._gpu)
+            rc = lib.tam_attend_seen(chunk, *qp, heads, scale, bits, words, stride, *rest)
         if rc != TAM_OK:
             _check(rc, where)
         return (out, lse) if return_lse else out
+
+    # -- a tree of drafted tokens ----------------------------------------------------
+    def accept(self, tokens, picks, parents, offsets=None, slots=None, longest=None, stream=None):
+        """Of the new tokens' trees the path that the model's choices follow stays in the cache, in every layer.  Rows as for
+        ``store``; ``tokens``, ``picks`` and ``parents`` int32 [tokens]: the drafted tokens, the choice after each, and their
+        parents (as for ``tree_masks``).  A row's token 0 stays; after a token that stays, the first one that follows it and
+        is its choice.  They move to the places behind the text before the row, the slot ends there, and pages past its
+        end are given back.  Returns, on the GPU, int32 [tokens]: the numbers in the row of its tokens that stay, then -1;
+        int32 [rows]: how many; int32 [rows]: the choice after the last one (-1 for an empty row)."""
+        where = "tam_pages_accept"
+        on = self._on(where, stream)
+        T, gpu = tokens.numel(), self._gpu
+        lists = [_int32(where, name, t, T, gpu) for name, t in (("tokens", tokens), ("picks", picks), ("parents", parents))]
+        chunk = self._new(where, 0, T, offsets, slots, longest)
+        rows = T if offsets is None else offsets.numel() - 1
+        size = self._lib.tam_pages_accept_work(chunk)
+        if size < 0:
+            _check(-1, where)
+        int32 = self._torch.int32
+        path, count, last = self._empty(T, int32, stream), self._empty(rows, int32, stream), self._empty(rows, int32, stream)
+        work = self._empty(size, self._torch.uint8, stream)
+        rc = self._lib.tam_pages_accept(self._pages_ref, chunk, *lists, path.data_ptr(), count.data_ptr(), last.data_ptr(),
+                                        work.data_ptr(), on)
+        if rc != TAM_OK:
+            _check(rc, where)
+        return path, count, last

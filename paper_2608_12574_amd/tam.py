@@ -36,7 +36,9 @@ ENTRY_POINTS = ("tam_compile", "tam_vocab_create", "tam_compile_vocab", "tam_com
                 "tam_timing_get",
                 "tam_format_rows_noalloc", "tam_vocab_destroy", "tam_destroy", "tam_last_error",
                 "tam_adjust_logits", "tam_pages_work", "tam_pages_fork", "tam_pages_extend", "tam_pages_compact",
-                "tam_pages_store", "tam_attend", "tam_attend_work")
+                "tam_pages_store", "tam_attend", "tam_attend_work",
+                "tam_tree_masks", "tam_pages_append", "tam_attend_seen", "tam_pages_accept", "tam_pages_accept_work",
+                "tam_top_tokens", "tam_top_tokens_work")
 
 
 class TamError(RuntimeError):
@@ -103,6 +105,11 @@ class Chunk(ctypes.Structure):
                 ("slot_ids", ctypes.c_void_p), ("longest", ctypes.c_int64)]
 
 
+class Rotation(ctypes.Structure):
+    _fields_ = [("frequencies", ctypes.c_void_p), ("pairs", ctypes.c_int64), ("adjacent", ctypes.c_int),
+                ("depth", ctypes.c_void_p)]
+
+
 class Timing(ctypes.Structure):
     _fields_ = [("host_trie_ms", ctypes.c_double), ("host_vocab_ms", ctypes.c_double),
                 ("upload_ms", ctypes.c_double), ("dev_lists_ms", ctypes.c_float),
@@ -154,6 +161,13 @@ def lib() -> ctypes.CDLL:
         L.tam_pages_store.argtypes = [chunk, P, i64, i64, P, i64, i64, P]
         L.tam_attend.argtypes = [chunk, P, i64, i64, i64, ctypes.c_float, P, i64, i64, P, P, P]
         L.tam_attend_work.argtypes = [chunk, i64]
+        L.tam_tree_masks.argtypes = [P, P, i64, i64, P, i64, P, P]
+        L.tam_pages_append.argtypes = [chunk, ctypes.POINTER(Rotation), P, i64, i64, P, i64, i64, P, i64, i64, i64, P, i64, i64, P]
+        L.tam_attend_seen.argtypes = [chunk, P, i64, i64, i64, ctypes.c_float, P, i64, i64, P, i64, i64, P, P, P]
+        L.tam_pages_accept.argtypes = [pages, chunk, P, P, P, P, P, P, P, P]
+        L.tam_pages_accept_work.argtypes = [chunk]
+        L.tam_top_tokens.argtypes = [P, ctypes.c_int, i64, i64, i64, i64, P, P, P, P, P]
+        L.tam_top_tokens_work.argtypes = [i64, i64, i64, ctypes.c_int]
         L.tam_destroy.argtypes = [P]
         L.tam_destroy.restype = None
         L.tam_last_error.restype = ctypes.c_char_p
@@ -161,6 +175,7 @@ def lib() -> ctypes.CDLL:
             if name not in ("tam_vocab_destroy", "tam_destroy", "tam_last_error"):
                 getattr(L, name).restype = ctypes.c_int
         L.tam_pages_work.restype = L.tam_attend_work.restype = i64
+        L.tam_pages_accept_work.restype = L.tam_top_tokens_work.restype = i64
         _lib = L
     return _lib
 
