@@ -5,14 +5,13 @@
 // k-th largest of the parts' maxima is no larger than the k-th largest logit, so only logits from there on can be among the best.
 //
 // k_top: a block holds a span of a row in registers, read once.  Each thread finds its maximum and its sum; the k-th largest of
-// the threads' maxima (found by halving, in each wave by itself) leaves a few more than k candidates, which go to LDS and
-// are ranked by counting.  Where equal logits leave too many, the k-th key itself is found by halving.
+// the threads' maxima (found by cutting the range of values, in each wave by itself) leaves a few more than k candidates,
+// which go to LDS and are ranked by counting.  Where equal logits leave too many, the k-th key itself is found.
 // k_top_join: the spans' best, in the same way, and the sum of the sums.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <climits>
-#include <type_traits>
 
 #include "step.hpp"
 
@@ -20,26 +19,26 @@ namespace tam {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kWave = 64, kThreads = 512, kWaves = kThreads / kWave;
-constexpr int kCandidates = 1280;
+constexpr int kWave = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Keys: the logit's order in the upper half (-0 and 0 alike, NaN above all), then the lowest token first.  0: no token.
-__device__ inline uint64_t key_of(uint32_t bits, uint32_t token) {
+// The order of logits, as unsigned integers: -0 and 0 alike, NaN above all.
+__device__ inline uint32_t order_of(float x) {
+    uint32_t bits = __float_as_uint(x);
     if (bits == 0x80000000u) bits = 0;
-    if ((bits & 0x7FFFFFFFu) > 0x7F800000u) bits = 0x7FFFFFFFu;
-    const uint32_t order = bits ^ ((bits & 0x80000000u) ? 0xFFFFFFFFu : 0x80000000u);
-    return (uint64_t)order << 32 | (0xFFFFFFFFu - token);
+    if (x != x) bits = 0x7FFFFFFFu;
+    return bits ^ ((bits & 0x80000000u) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-__device__ inline float logit_of(uint64_t key) {
-    const uint32_t order = (uint32_t)(key >> 32);
-    return __uint_as_float(order ^ ((order & 0x80000000u) ? 0x80000000u : 0xFFFFFFFFu));
-}
+__device__ inline float logit_of(uint32_t order) { return __uint_as_float(order ^ ((order & 0x80000000u) ? 0x80000000u : 0xFFFFFFFFu)); }
 
-// How a type's logits lie in a 16-byte vector, and their order as signed integers (-0 under 0; a NaN with a sign under -inf).
+constexpr uint32_t kNone = 0x007FFFFFu;  // the order of -inf
+
+// Keys: the order in the upper half, then the lowest token first.  0: no token.
+__device__ inline uint64_t key_of(float x, uint32_t token) { return (uint64_t)order_of(x) << 32 | (0xFFFFFFFFu - token); }
+
+// How a type's logits lie in a 16-byte vector.
 template <typename T>
 struct In;
 
@@ -47,37 +46,18 @@ template <>
 struct In<float> {
     static constexpr int n = 4;
     static constexpr uint32_t kMinusInf = 0xFF800000u;  // a word of it
-    static constexpr int32_t kLowest = (int32_t)0x80800000u, kAbove = INT_MAX;  // orders of what lies just above -inf; of all
-    static __device__ uint32_t bits(u32x4 x, int i) { return x[i]; }
+    static __device__ float get(u32x4 x, int i) { return __uint_as_float(x[i]); }
     static __device__ void drop(u32x4 &x, int i) { x[i] = kMinusInf; }
-    static __device__ int32_t order(u32x4 x, int i) { return (int32_t)(x[i] ^ ((uint32_t)((int32_t)x[i] >> 31) & 0x7FFFFFFFu)); }
-    static __device__ int32_t highest(u32x4 x) { return max(max(order(x, 0), order(x, 1)), max(order(x, 2), order(x, 3))); }
-    static __device__ float value(int32_t order) { return __int_as_float(order ^ (int32_t)((uint32_t)(order >> 31) & 0x7FFFFFFFu)); }
+    static __device__ float load(const float *p) { return *p; }
 };
 
 template <>
 struct In<uint16_t> {  // bf16
     static constexpr int n = 8;
     static constexpr uint32_t kMinusInf = 0xFF80FF80u;
-    static constexpr int32_t kLowest = -32640, kAbove = 32767;
-    static __device__ uint32_t bits(u32x4 x, int i) { return i & 1 ? x[i >> 1] & 0xFFFF0000u : x[i >> 1] << 16; }
+    static __device__ float get(u32x4 x, int i) { return __uint_as_float(i & 1 ? x[i >> 1] & 0xFFFF0000u : x[i >> 1] << 16); }
     static __device__ void drop(u32x4 &x, int i) { x[i >> 1] = i & 1 ? (x[i >> 1] & 0xFFFFu) | 0xFF800000u : (x[i >> 1] & 0xFFFF0000u) | 0xFF80u; }
-    static __device__ i16x2 orders(uint32_t w) {
-        const i16x2 x = __builtin_bit_cast(i16x2, w);
-        return x ^ ((x >> (int16_t)15) & (int16_t)0x7FFF);
-    }
-    static __device__ int32_t order(u32x4 x, int i) {
-        const int16_t y = (int16_t)(x[i >> 1] >> 16 * (i & 1));
-        return (int16_t)(y ^ ((y >> 15) & 0x7FFF));
-    }
-    static __device__ int32_t highest(u32x4 x) {
-        const i16x2 y = __builtin_elementwise_max(__builtin_elementwise_max(orders(x[0]), orders(x[1])),
-                                                  __builtin_elementwise_max(orders(x[2]), orders(x[3])));
-        return max((int32_t)y[0], (int32_t)y[1]);
-    }
-    static __device__ float value(int32_t order) {
-        return __uint_as_float((uint32_t)(order ^ ((order >> 31) & 0x7FFF)) << 16);
-    }
+    static __device__ float load(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
 };
 
 // A sum of exponentials under their maximum.
@@ -92,11 +72,13 @@ __device__ inline Sum join(Sum a, Sum b) {
 }
 
 // Of all threads, in a fixed order.
+template <int kThreads>
 __device__ inline Sum join_block(Sum x) {
+    constexpr int kWaves = kThreads / kWave;
     __shared__ Sum waves[kWaves];
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) x = join(x, Sum{__shfl_xor(x.m, d), __shfl_xor(x.s, d)});
-    __syncthreads();
+    if (kWaves == 1) return x;
     if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = x;
     __syncthreads();
     x = waves[0];
@@ -107,10 +89,13 @@ __device__ inline Sum join_block(Sum x) {
 
 __device__ inline float log_of(Sum x) { return x.s == 0.f ? -INFINITY : x.m + logf(x.s); }
 
+template <int kThreads>
 __device__ inline int count_block(int mine) {
+    constexpr int kWaves = kThreads / kWave;
     __shared__ int waves[kWaves];
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) mine += __shfl_xor(mine, d);
+    if (kWaves == 1) return mine;
     __syncthreads();
     if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = mine;
     __syncthreads();
@@ -120,34 +105,60 @@ __device__ inline int count_block(int mine) {
     return all;
 }
 
-// A value that at least k of the threads' maxima reach and not many more do (where they are all different: k + k / 4 at
-// most), or `low` if no more than k reach that.  X: a signed integer, at most `high`; each wave looks at all of them.
-template <typename X>
-__device__ inline X near_kth(X mine, int k, X low, X high) {
-    using U = std::make_unsigned_t<X>;
-    __shared__ X all[kThreads];
-    all[threadIdx.x] = mine;
-    __syncthreads();
-    X x[kWaves];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) x[w] = all[w * kWave + threadIdx.x % kWave];
+// The k-th largest of the lanes' kPer values each, or a value under it that few more reach (kReach(k) at most where all are
+// different); `low` if no more reach that.  X: an unsigned integer.  The range is cut into four in each turn: three counts side by
+// side take hardly longer than one.
+constexpr int kReach(int k) { return k + k / 4; }
+
+template <int kPer, typename X>
+__device__ inline X near_kth_of(const X (&x)[kPer], int k, X low) {
     auto reach = [&](X y) {
         int n = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(x[w] >= y));
+        for (int w = 0; w < kPer; ++w) n += __popcll(__ballot(x[w] >= y));
         return n;
     };
-    if (reach(low) <= k) return low;
-    // reach(low) > k; what lies above `high` is reached by none
-    X above = high;
+    if (reach(low) <= kReach(k)) return low;
+    X above = ~(X)0;  // the k-th largest lies in low .. above
     while (low < above) {
-        const X mid = (X)((U)low + ((U)above - (U)low) / 2 + 1);  // (low < mid <= above but for above = low + 1: mid = above)
-        const int n = reach(mid);
-        if (n >= k) low = mid;
-        else above = mid - 1;
-        if (n >= k && n <= k + k / 4) break;
+        const X step = (above - low) / 4 + 1;
+        const X y1 = low + step, y2 = above - y1 >= step ? y1 + step : above, y3 = above - y2 >= step ? y2 + step : above;
+        const int n1 = reach(y1), n2 = reach(y2), n3 = reach(y3);
+        int n = INT_MAX;
+        if (n3 >= k) low = y3, n = n3;
+        else if (n2 >= k) low = y2, above = y3 - 1, n = n2;
+        else if (n1 >= k) low = y1, above = y2 - 1, n = n1;
+        else above = y1 - 1;
+        if (n <= kReach(k)) break;
     }
     return low;
+}
+
+// A value that at least k of all threads' reach, and few more: of 64 groups' maxima for a small k, or 256 (of logits in
+// any order, k of 4 k groups leave 1.15 k candidates).  The first wave finds it, since the others' instructions would only take
+// turns with its own, and those of the blocks beside.
+template <int kThreads, typename X>
+__device__ inline X near_kth(X mine, int k, X low) {
+    __shared__ X all[256], found;
+    const bool few = k <= 16;
+    const int lane = threadIdx.x, group = kThreads / (few ? 64 : 256);  // threads of a group
+#pragma unroll
+    for (int d = 1; d < kThreads / 64; d <<= 1)
+        if (d < group) mine = max(mine, __shfl_xor(mine, d));
+    if (threadIdx.x % group == 0) all[threadIdx.x / group] = mine;
+    __syncthreads();
+    if (threadIdx.x < kWave) {
+        if (few) {
+            const X x[1] = {all[lane]};
+            low = near_kth_of<1, X>(x, k, low);
+        } else {
+            const X x[4] = {all[lane], all[lane + 64], all[lane + 128], all[lane + 192]};
+            low = near_kth_of<4, X>(x, k, low);
+        }
+        if (lane == 0) found = low;
+    }
+    __syncthreads();
+    return found;
 }
 
 struct Top {
@@ -161,25 +172,70 @@ struct Top {
 
 __device__ inline void write(const Top &a, int64_t b, int i, uint64_t key, float lse) {
     a.tokens[b * a.k + i] = key ? (int32_t)(0xFFFFFFFFu - (uint32_t)key) : -1;
-    a.logprobs[b * a.k + i] = key ? logit_of(key) - lse : -INFINITY;
+    a.logprobs[b * a.k + i] = key ? logit_of((uint32_t)(key >> 32)) - lse : -INFINITY;
 }
 
-// The candidates' ranks; the first k of them go to their places.
-template <typename F>
+// The candidates' ranks, by counting those before each, `group` threads to a candidate; the first k of them go to their places.
+template <int kThreads, typename F>
 __device__ inline void rank(const uint64_t *found, int n, int k, F put) {
-    for (int i = threadIdx.x; i < n; i += kThreads) {
+    int group = 1;
+    while (group < kWave && 2 * group * n <= kThreads) group *= 2;
+    const int sub = threadIdx.x & (group - 1);
+    for (int i = threadIdx.x / group; i < n; i += kThreads / group) {
         const uint64_t mine = found[i];
         int before = 0;
-        for (int j = 0; j < n; ++j) before += found[j] > mine;
-        if (before < k) put(before, mine);
+#pragma unroll 4
+        for (int j = sub; j < n; j += group) before += found[j] > mine;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1)
+            if (d < group) before += __shfl_xor(before, d);
+        if (sub == 0 && before < k) put(before, mine);
     }
     for (int i = n + threadIdx.x; i < k; i += kThreads) put(i, 0);
 }
 
-template <typename T, int kVecs>
+// The candidates where there are too many, or a NaN: the order of the k-th key by halving, then how far in the tokens the keys
+// of that order go.  The logits are read again in each turn, so that nothing of this takes registers from the usual way.
+template <int kThreads, typename T>
+__device__ __attribute__((noinline)) int collect_exactly(const T *row, int64_t from, int64_t to, int k, uint64_t *found, int32_t *count) {
+    auto counted = [&](auto is) {
+        int mine = 0;
+        for (int64_t v = from + threadIdx.x; v < to; v += kThreads) mine += is(order_of(In<T>::load(row + v)), v);
+        return count_block<kThreads>(mine);
+    };
+    uint32_t low = kNone + 1, above = ~0u;
+    int n = counted([&](uint32_t o, int64_t) { return o >= low; });
+    if (n < k) above = low;  // all of them
+    while (low < above) {
+        const uint32_t mid = low + (above - low) / 2 + 1;
+        n = counted([&](uint32_t o, int64_t) { return o >= mid; });
+        if (n >= k) low = mid;
+        else above = mid - 1;
+        if (n == k) break;
+    }
+    n = counted([&](uint32_t o, int64_t) { return o > low; });
+    int64_t first = from, last = to;  // of the order `low` the tokens before `last`: k - n of them, or all
+    while (first < last) {
+        const int64_t mid = first + (last - first) / 2;
+        if (n + counted([&](uint32_t o, int64_t v) { return o == low && v < mid; }) >= k) last = mid;
+        else first = mid + 1;
+    }
+    last = min(last, to);
+    if (threadIdx.x == 0) *count = 0;
+    __syncthreads();
+    for (int64_t v = from + threadIdx.x; v < to; v += kThreads) {
+        const float x = In<T>::load(row + v);
+        const uint32_t o = order_of(x);
+        if (o > low || (o == low && v < last)) found[atomicAdd(count, 1)] = key_of(x, (uint32_t)v);
+    }
+    __syncthreads();
+    return *count;
+}
+
+template <typename T, int kVecs, int kThreads>
 __global__ void __launch_bounds__(kThreads) k_top(const T *__restrict__ logits, Top a) {
     using I = In<T>;
-    constexpr int N = I::n;
+    constexpr int N = I::n, kCandidates = 1024;
     __shared__ __align__(16) uint64_t found[kCandidates];
     __shared__ int32_t count;
     const int64_t b = blockIdx.x / (uint32_t)a.parts;
@@ -197,7 +253,12 @@ __global__ void __launch_bounds__(kThreads) k_top(const T *__restrict__ logits, 
         x[i] = j < vectors ? from[j] : u32x4{I::kMinusInf, I::kMinusInf, I::kMinusInf, I::kMinusInf};
     }
     if (threadIdx.x == 0) count = 0;
-    int32_t high[kVecs], most = INT_MIN;
+    // (no converted logits are kept from one pass over the registers to the next: they would take twice the room)
+    auto fresh = [&]() {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) asm volatile("" : "+v"(x[i]));
+    };
+    float high[kVecs], most = -INFINITY;  // (a NaN stays one)
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const int64_t e = (j0 + i * kThreads) * N - skip;
@@ -206,145 +267,140 @@ __global__ void __launch_bounds__(kThreads) k_top(const T *__restrict__ logits, 
             for (int c = 0; c < N; ++c)
                 if (e + c < 0 || e + c >= a.V) I::drop(x[i], c);
         }
-        high[i] = I::highest(x[i]);
-        most = max(most, high[i]);
+        high[i] = I::get(x[i], 0);
+#pragma unroll
+        for (int c = 1; c < N; ++c) high[i] = __builtin_elementwise_maximum(high[i], I::get(x[i], c));
+        most = __builtin_elementwise_maximum(most, high[i]);
     }
-    // (-inf: 0, so that nothing is taken from it; infinity: the largest number, and the sum is infinite)
-    const float m = I::value(most), under = m == -INFINITY ? 0.f : fminf(m, 3.4028234663852886e38f);
-    Sum sum{m, 0.f};
+    // sum exp(x - m) = exp2(mc - m c) sum exp2(x c - mc), c = log2(e), mc = m c rounded: one instruction per exponent, and
+    // it is rounded once.  A maximum of 2^126 or more, whose m c may have no fp32: what is not the maximum adds
+    // nothing, so any c will do that tells the two apart.  -inf: 0, so that nothing is taken from it.
+    fresh();
+    Sum sum{most, 0.f};
+    const float m = most == -INFINITY ? 0.f : fminf(most, 3.4028234663852886e38f);
+    const float c2 = fabsf(m) < 8.5e37f ? kLog2e : 8.6736174e-19f;
+    const float mc = m * c2;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i)
+    for (int i = 0; i < kVecs; ++i) {
+        if (!__any(!(high[i] == -INFINITY))) continue;  // nothing in the wave's vectors
 #pragma unroll
-        for (int c = 0; c < N; ++c) sum.s += __builtin_amdgcn_exp2f((__uint_as_float(I::bits(x[i], c)) - under) * kLog2e);
-    const bool odd = sum.s != sum.s;
-    if (odd) sum.m = -INFINITY;
-    sum = join_block(sum);
-    if (sum.s != sum.s) {  // a NaN, which may have a sign: above all
+        for (int c = 0; c < N; ++c) sum.s += __builtin_amdgcn_exp2f(__builtin_fmaf(I::get(x[i], c), c2, -mc));
+    }
+    sum.s *= __builtin_amdgcn_exp2f(__builtin_fmaf(-m, c2, mc));
+    if (sum.s != sum.s) sum.m = -INFINITY;
+    sum = join_block<kThreads>(sum);
+    int n = INT_MAX;
+    fresh();
+    if (sum.s == sum.s) {
+        const float low = logit_of(near_kth<kThreads, uint32_t>(order_of(most), a.k, kNone + 1));
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
+            if (high[i] >= low) {
 #pragma unroll
-            for (int c = 0; c < N; ++c) {
-                const uint32_t y = I::bits(x[i], c);
-                if ((y & 0x7FFFFFFFu) > 0x7F800000u) {
-                    if constexpr (N == 4) x[i][c] = 0x7FFFFFFFu;
-                    else x[i][c >> 1] |= 0x7FFFu << 16 * (c & 1), x[i][c >> 1] &= ~(0x8000u << 16 * (c & 1));
+                for (int c = 0; c < N; ++c) {
+                    const float y = I::get(x[i], c);
+                    if (y >= low) {
+                        const int at = atomicAdd(&count, 1);
+                        if (at < kCandidates) found[at] = key_of(y, (uint32_t)((j0 + i * kThreads) * N - skip + c));
+                    }
                 }
             }
-            high[i] = I::highest(x[i]);
-            most = max(most, high[i]);
         }
-    }
-    int32_t low = near_kth<int32_t>(most, a.k, I::kLowest, I::kAbove);
-    if (low == 0) low = -1;  // -0 is as high as 0
-    auto key = [&](int i, int c) { return key_of(I::bits(x[i], c), (uint32_t)((j0 + i * kThreads) * N - skip + c)); };
-    auto collect = [&](auto is) {
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            if (high[i] < low) continue;
-#pragma unroll
-            for (int c = 0; c < N; ++c) {
-                if (!is(i, c)) continue;
-                const int at = atomicAdd(&count, 1);
-                if (at < kCandidates) found[at] = key(i, c);
-            }
-        }
-    };
-    collect([&](int i, int c) { return I::order(x[i], c) >= low; });
-    __syncthreads();
-    int n = count;
-    if (n > kCandidates) {  // the k-th key itself
-        uint64_t floor = 1, above = ~0ull;
-        while (floor < above) {
-            const uint64_t mid = floor + (above - floor) / 2 + 1;
-            int mine = 0;
-#pragma unroll
-            for (int i = 0; i < kVecs; ++i)
-#pragma unroll
-                for (int c = 0; c < N; ++c) mine += I::order(x[i], c) >= low && key(i, c) >= mid;
-            const int all = count_block(mine);
-            if (all >= a.k) floor = mid;
-            else above = mid - 1;
-            if (all == a.k) break;
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) count = 0;
-        __syncthreads();
-        collect([&](int i, int c) { return I::order(x[i], c) >= low && key(i, c) >= floor; });
         __syncthreads();
         n = count;
+        __syncthreads();
+    }
+    if (n > kCandidates) {
+        const int64_t begin = (int64_t)part * kThreads * kVecs * N - skip, end = begin + kThreads * kVecs * N;
+        n = collect_exactly<kThreads, T>(row, max(begin, (int64_t)0), min(end, a.V), a.k, found, &count);
     }
     if (a.parts == 1) {
         const float lse = log_of(sum);
-        rank(found, n, a.k, [&](int i, uint64_t y) { write(a, b, i, y, lse); });
+        rank<kThreads>(found, n, a.k, [&](int i, uint64_t y) { write(a, b, i, y, lse); });
         if (a.lse && threadIdx.x == 0) a.lse[b] = lse;
     } else {
         const int64_t at = b * a.parts + part;
-        rank(found, n, a.k, [&](int i, uint64_t y) { a.keys[at * a.k + i] = y; });
+        rank<kThreads>(found, n, a.k, [&](int i, uint64_t y) { a.keys[at * a.k + i] = y; });
         if (threadIdx.x == 0) a.sums[at] = sum;
     }
 }
 
 // A thread's keys: of up to 8,192, which the entry point's limits on V and k and split_of keep to.  The keys are all different, so
-// that no more than 80 threads' are candidates.
-constexpr int kJoinKeys = 16;
-static_assert(kCandidates >= (TAM_MAX_TOP + TAM_MAX_TOP / 4) * kJoinKeys, "room for the join's candidates");
+// that no more than kReach(k) groups' of near_kth are candidates.
+constexpr int kJoin = 512, kJoinKeys = 16, kFewKeys = 128, kJoinCandidates = kReach(TAM_MAX_TOP) * kJoinKeys * (kJoin / 256);
+static_assert(kJoinCandidates >= kReach(16) * kJoinKeys * (kJoin / 64) && kJoinCandidates >= kFewKeys, "room for the candidates");
 
-__global__ void __launch_bounds__(kThreads) k_top_join(Top a) {
-    __shared__ __align__(16) uint64_t found[kCandidates];
+__global__ void __launch_bounds__(kJoin) k_top_join(Top a) {
+    __shared__ __align__(16) uint64_t found[kJoinCandidates];
     __shared__ int32_t count;
     const int64_t b = blockIdx.x;
-    const int n = a.parts * a.k;
+    int n = a.parts * a.k;
     const uint64_t *const keys = a.keys + b * n;
-    uint64_t x[kJoinKeys], most = 0;
-#pragma unroll
-    for (int i = 0; i < kJoinKeys; ++i) {
-        const int j = threadIdx.x + i * kThreads;
-        x[i] = j < n ? keys[j] : 0;
-        most = max(most, x[i]);
-    }
     if (threadIdx.x == 0) count = 0;
     Sum sum{-INFINITY, 0.f};
     if ((int)threadIdx.x < a.parts) sum = a.sums[b * a.parts + threadIdx.x];
-    sum = join_block(sum);
-    // (keys with their upper bit turned are signed integers in the same order)
-    constexpr uint64_t kTop = 1ull << 63;
-    const uint64_t low = (uint64_t)near_kth<int64_t>((int64_t)(most ^ kTop), a.k, (int64_t)(1 ^ kTop), INT64_MAX) ^ kTop;
+    if (n <= kFewKeys) {  // few enough to rank them all
+        const uint64_t x = (int)threadIdx.x < n ? keys[threadIdx.x] : 0;
+        sum = join_block<kJoin>(sum);
+        if (x) found[atomicAdd(&count, 1)] = x;
+        __syncthreads();
+        n = count;
+    } else {
+        uint64_t x[kJoinKeys], most = 0;
 #pragma unroll
-    for (int i = 0; i < kJoinKeys; ++i) {
-        if (x[i] < low) continue;
-        found[atomicAdd(&count, 1)] = x[i];
+        for (int i = 0; i < kJoinKeys; ++i) {
+            // the parts' best ones first, so that they lie in groups of their own
+            const int j = threadIdx.x + i * kJoin, place = j / a.parts;
+            x[i] = j < n ? keys[(j - place * a.parts) * a.k + place] : 0;
+            most = max(most, x[i]);
+        }
+        sum = join_block<kJoin>(sum);
+        const uint64_t low = near_kth<kJoin, uint64_t>(most, a.k, 1);
+#pragma unroll
+        for (int i = 0; i < kJoinKeys; ++i)
+            if (x[i] >= low) found[atomicAdd(&count, 1)] = x[i];
+        __syncthreads();
+        n = count;
     }
-    __syncthreads();
     const float lse = log_of(sum);
-    rank(found, count, a.k, [&](int i, uint64_t y) { write(a, b, i, y, lse); });
+    rank<kJoin>(found, n, a.k, [&](int i, uint64_t y) { write(a, b, i, y, lse); });
     if (a.lse && threadIdx.x == 0) a.lse[b] = lse;
 }
 
 struct Split {
-    int vecs, parts;
+    int vecs, threads, parts;
 };
 
+// Blocks of 256 threads, since smaller ones leave k_top_join more and larger ones wait for one another (us per call of 256 bf16
+// rows over V = 262,144, k_top and k_top_join, 64 threads: 32.3 and 7.4, 128: 30.1 and 4.7, 256: 29.6 and 4.1, 512: 35.7 and
+// 4.8, 1,024: 66 and 5), with as many vectors each as leave the chip 2,048 blocks; more threads only where a row would have more
+// parts than k_top_join holds.  Short rows, no more than there are CUs, take a block each, which leaves the second launch out (us
+// per call of 1, 64, 256 and 512 fp32 rows over V = 32,000, 4 of each: 8.1, 9.1, 11.9 and 22.9, in parts 8.1, 10.2, 15.2 and 21.5, and
+// 3 less on the host; 64 of each: 10.2, 11.5, 13.9 and 26.7, in parts 14.9, 17.3, 24.1 and 31.9; bf16 rows over V = 128,256, 24 of each,
+// 8 and 256: 16 and 21.3, in parts 14.4 and 29).
 template <typename T>
 Split split_of(int64_t B, int64_t V) {
     const int64_t vectors = (V + 2 * In<T>::n - 2) / In<T>::n;
-    Split s{1, 1};
-    for (;; s.vecs *= 2) {
-        s.parts = (int)((vectors + kThreads * s.vecs - 1) / (kThreads * s.vecs));
-        if (s.vecs == 16 || (B * s.parts <= 1024 && s.parts <= 128)) return s;
-    }
+    Split s{4, 256, 1};
+    auto parts = [&] { return (int)((vectors + s.threads * s.vecs - 1) / (s.threads * s.vecs)); };
+    while (s.vecs < 16 && (B * parts() > 2048 || parts() > 128)) s.vecs *= 2;
+    if (parts() > 128) s.threads = 512;
+    if (B <= 256 && vectors <= (B < 128 ? 8192 : 16384)) s.vecs = vectors <= 4096 ? 4 : vectors <= 8192 ? 8 : 16, s.threads = 1024;
+    s.parts = parts();
+    return s;
 }
 
 template <typename T>
 hipError_t launch(const void *logits, int64_t B, Top a, const Split &sp, hipStream_t s) {
-    void (*kernel)(const T *, Top) = sp.vecs == 1   ? k_top<T, 1>
-                                     : sp.vecs == 2 ? k_top<T, 2>
-                                     : sp.vecs == 4 ? k_top<T, 4>
-                                     : sp.vecs == 8 ? k_top<T, 8>
-                                                    : k_top<T, 16>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(B * sp.parts)), dim3(kThreads), 0, s, static_cast<const T *>(logits), a);
+    void (*kernel)(const T *, Top) = sp.threads == 512    ? k_top<T, 16, 512>
+                                     : sp.threads == 1024 ? (sp.vecs == 4 ? k_top<T, 4, 1024> : sp.vecs == 8 ? k_top<T, 8, 1024> : k_top<T, 16, 1024>)
+                                     : sp.vecs == 4      ? k_top<T, 4, 256>
+                                     : sp.vecs == 8      ? k_top<T, 8, 256>
+                                                       : k_top<T, 16, 256>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(B * sp.parts)), dim3((unsigned)sp.threads), 0, s, static_cast<const T *>(logits), a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || sp.parts == 1) return e;
-    hipLaunchKernelGGL(k_top_join, dim3((unsigned)B), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(k_top_join, dim3((unsigned)B), dim3(kJoin), 0, s, a);
     return hipGetLastError();
 }
 
