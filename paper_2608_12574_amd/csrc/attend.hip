@@ -998,11 +998,13 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
             uint64_t at1 = place_of(k0 + kWideKeys, id1);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) k_in[i] = load(kh, at0, i);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) v_in[i] = load(vh, at0, i);
             __syncthreads();  // the last tile is done with the buffers
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) store_k(0, i);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) k_in[i] = load(kh, at1, i), v_in[i] = load(vh, at0, i);
+            for (int i = 0; i < kLoads; ++i) k_in[i] = load(kh, at1, i);
             // the half unit before the first has weights of zero and a V of zeros
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
@@ -1132,17 +1134,29 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
         if (a.lse && lane == 0) a.lse[token * a.heads + head] = l == 0.f ? -INFINITY : mx * a.scale + logf(l);
     };
     if (!many) {
+        const int pieces = t.more + 2;  // five at most, asked for together
         for (int row = row0 + g; row < row1; row += kGroups) {
-            float mx = -INFINITY;
-            for (int64_t i = cut - 1; i <= last; ++i) mx = fmaxf(mx, ml[(slot_of(i) * kRows + row) * 2]);
+            f32x4 part_sum[5];
+            float mi[5], li[5], mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 5; ++i) {
+                mi[i] = -INFINITY;
+                if (i >= pieces) continue;
+                const int64_t at = slot_of(cut - 1 + i) * kRows + row;
+                mi[i] = ml[at * 2];
+                li[i] = ml[at * 2 + 1];
+                part_sum[i] = *reinterpret_cast<const f32x4 *>(a.sums + at * DP + 4 * lane);
+            }
+#pragma unroll
+            for (int i = 0; i < 5; ++i) mx = fmaxf(mx, mi[i]);
             f32x4 sum{0, 0, 0, 0};
             float l = 0.f;
-            for (int64_t i = cut - 1; i <= last; ++i) {
-                const int64_t at = slot_of(i) * kRows + row;
-                const float mi = ml[at * 2];
-                const float keep = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi - mx) * c);
-                sum += *reinterpret_cast<const f32x4 *>(a.sums + at * DP + 4 * lane) * keep;
-                l += ml[at * 2 + 1] * keep;
+#pragma unroll
+            for (int i = 0; i < 5; ++i) {
+                if (i >= pieces) break;
+                const float keep = mi[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi[i] - mx) * c);
+                sum += part_sum[i] * keep;
+                l += li[i] * keep;
             }
             write(row, sum, l, mx);
         }
