@@ -53,7 +53,7 @@ struct Attend {
     int64_t page_stride, head_stride, token_stride, q_token, q_head, out_token, out_head;
     const int32_t *table, *length, *offsets, *slot_ids;
     int64_t table_stride, slots, max_pages, rows, tokens;
-    int32_t pages, shift, heads, kv_heads, dim;
+    int32_t pages, shift, heads, kv_heads, per_kv, dim;  // per_kv: query heads to a K/V head
     float scale;
     // the cut: tiles of `tq` tokens by `group` heads, `parts` of them per K/V head
     int32_t tq, group, parts, blocks;
@@ -76,6 +76,14 @@ struct alignas(16) Cut {
 __device__ inline int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ inline int64_t uniform(int64_t x) {
     return (int64_t)(uint32_t)uniform((int32_t)x) | (int64_t)uniform((int32_t)(x >> 32)) << 32;
+}
+
+// x, of which the compiler knows nothing from here on: what is computed from it is computed where it is used. Else all that
+// does not change from tile to tile is computed before the first one, and waits in registers that have no room for it (a microsecond
+// and 60 spilled values, where a block has a single tile).
+__device__ inline int32_t here(int32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
 }
 
 // ------------------------------------------------------------------ the cut ---
@@ -140,13 +148,13 @@ struct Place {
 
 // Where piece number `share` (this block's) begins, and the keys of a piece.  All threads of
 // the block call it; row < 0 past the line's end.
-template <bool kSeen>
+template <bool kSeen, int kBlock = kThreads>
 __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
-    __shared__ int64_t sums[kThreads / kWave];
+    __shared__ int64_t sums[kBlock / kWave];
     __shared__ int64_t found[2];
     __shared__ Row found_row;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t per = (a.rows + kThreads - 1) / kThreads, lo = threadIdx.x * per, hi = min(lo + per, a.rows);
+    const int64_t per = (a.rows + kBlock - 1) / kBlock, lo = threadIdx.x * per, hi = min(lo + per, a.rows);
     const int64_t heads = (int64_t)a.kv_heads * a.parts;
     int64_t mine = 0;
     Row r{};
@@ -166,7 +174,7 @@ __device__ inline Place find(const Attend &a, int64_t share, int64_t *piece) {
     Place p;
     p.total = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / kWave; ++w) {
+    for (int w = 0; w < kBlock / kWave; ++w) {
         if (w < wave) upto += sums[w];
         p.total += sums[w];
     }
@@ -221,7 +229,7 @@ __device__ inline Tile tile_at(const Attend &a, const Row &r, int64_t rest) {
     t.tile = lo;
     t.first = lo * a.tq;
     t.n = min(a.tq, r.n - t.first);
-    t.heads = min(a.group, a.heads / a.kv_heads - t.part * a.group);
+    t.heads = min(a.group, a.per_kv - t.part * a.group);
     t.rest = rest - keys_before<kSeen>(a, r, lo);
     t.keys = r.n <= a.tq ? u : (int64_t)max(r.base, 0) + (kSeen ? r.n : t.first + t.n) + a.extra;
     return t;
@@ -250,7 +258,7 @@ __device__ inline void note(const Attend &a, int64_t block, const Row &r, const 
     const uint32_t keys = (uint32_t)min(piece, (int64_t)INT32_MAX), rest = (uint32_t)(t.keys - t.rest - 1);
     const int32_t behind = (int32_t)(t.rest - a.extra - kKeys);
     a.cuts[block] = Cut{behind >= 0, behind >= 0 ? (int32_t)((uint32_t)behind / keys) : 0, (int32_t)(rest / keys),
-                        r.first + t.first, t.n, t.head * (a.heads / a.kv_heads) + t.part * a.group, t.heads};
+                        r.first + t.first, t.n, t.head * a.per_kv + t.part * a.group, t.heads};
 }
 
 // ------------------------------------------------------------------ products ---
@@ -430,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
         const bool is = tok < t.n;
         const int32_t seen = !is ? 0 : kSeen ? all : max(0, min(r.base + t.first + tok + 1, all));  // keys that the query sees
         const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
-                              (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
+                              (int64_t)(t.head * a.per_kv + t.part * a.group + h) * a.q_head;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const int d = 32 * s + 8 * grp;
@@ -630,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
             if (whole) {
                 const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
                 const int64_t token = r.first + t.first + out_tok;
-                const int64_t head = t.head * (a.heads / a.kv_heads) + t.part * a.group + out_h;
+                const int64_t head = t.head * a.per_kv + t.part * a.group + out_h;
                 uint16_t *dst = a.out + token * a.out_token + head * a.out_head + d0;
                 if (d0 < a.dim) {
                     uint32_t y[kCols / 2];
@@ -676,9 +684,9 @@ constexpr int kWideKeys = 64;
 
 // What is not finite in V of the keys from .. to - 1, added to the sums or outputs that this lane has written (lanes and rows as
 // below).  Apart from these, and from the thread's number on, so that it takes none of their registers.
-template <int DP, int kBlocks, bool kHalf, bool kSeen>
+template <int DP, int kWaves, int kBlocks, bool kHalf, bool kSeen>
 __device__ inline void add_values(const Attend &a, const Row &r, const Tile &t, int32_t from, int32_t to, bool whole, int64_t at) {
-    constexpr int kWaveRows = 32 * kBlocks, kRows = 4 * kWaveRows;
+    constexpr int kWaveRows = 32 * kBlocks, kRows = kWaves * kWaveRows;
     int32_t thread = threadIdx.x;
     asm volatile("" : "+v"(thread));
     const int32_t *const pages = a.table + r.slot * a.table_stride;
@@ -686,7 +694,7 @@ __device__ inline void add_values(const Attend &a, const Row &r, const Tile &t, 
     for (int b = 0; b < kBlocks; ++b) {
         const int row = thread / kWave * kWaveRows + 32 * b + thread % 32, tok = row / t.heads, h = row - tok * t.heads;
         if (tok >= t.n) return;
-        const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
+        const int64_t token = r.first + t.first + tok, head = t.head * a.per_kv + t.part * a.group + h;
         uint16_t *const out = a.out + token * a.out_token + head * a.out_head;
         float *const sum = a.sums + (at * kRows + row) * DP;
         const int32_t end = kSeen ? to : min(to, r.base + t.first + tok + 1);
@@ -706,9 +714,9 @@ __device__ inline void add_values(const Attend &a, const Row &r, const Tile &t, 
     }
 }
 
-template <int DP, int kBlocks, bool kHalf, bool kRuns, bool kSeen>
-__global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_attend_wide(Attend a) {
-    constexpr int kWaveRows = 32 * kBlocks, kRows = 4 * kWaveRows;
+template <int DP, int kWaves, int kBlocks, bool kHalf, bool kRuns, bool kSeen>
+__global__ void __launch_bounds__(kWave * kWaves, kWaves == 4 && kBlocks == 1 && DP == 64 ? 2 : 1) k_attend_wide(Attend a) {
+    constexpr int kThreads = kWave * kWaves, kWaveRows = 32 * kBlocks, kRows = kWaves * kWaveRows;
     constexpr int kPieces = DP / 8;            // 16-byte pieces of a key
     constexpr int kSteps = DP / 16;            // products over 16 dimensions
     constexpr int kCols = DP / 32;             // blocks of 32 output dimensions
@@ -726,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
     int32_t number = 0;
     if (threadIdx.x == 0) odd = 0;
     int64_t piece;
-    Place p = find<kSeen>(a, block, &piece);
+    Place p = find<kSeen, kThreads>(a, block, &piece);
     if (p.row < 0) {
         if (threadIdx.x == 0) a.cuts[block].is = 0;
         return;
@@ -770,6 +778,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         ++number;
         u32x4 q[kBlocks][kSteps];
         int32_t seen[kBlocks];
+        const int half_q = here(half);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
             const int row = kWaveRows * wave + 32 * b + col, tok = row / t.heads, h = row - tok * t.heads;
@@ -777,10 +786,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
             // (kSeen: the token)
             seen[b] = kSeen ? (is ? r.first + t.first + tok : -1) : is ? max(0, min(r.base + t.first + tok + 1, all)) : 0;
             const uint16_t *src = a.q + (int64_t)(r.first + t.first + tok) * a.q_token +
-                                  (int64_t)(t.head * (a.heads / a.kv_heads) + t.part * a.group + h) * a.q_head;
+                                  (int64_t)(t.head * a.per_kv + t.part * a.group + h) * a.q_head;
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
-                const int d = 16 * s + 8 * half;
+                const int d = 16 * s + 8 * half_q;
                 q[b][s] = is && d < a.dim ? *reinterpret_cast<const u32x4 *>(src + d) : u32x4{0, 0, 0, 0};
             }
         }
@@ -1029,6 +1038,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                 clean(k, id0);
                 stage(sa, pb, k_half(x, 1), sb, v_half(x ^ 1, 1), pa, [&](int f) {
                     const int i = f / 4;
+                    if (i >= kLoads) return;
                     if (f % 4 == 0) {
                         store_k(x ^ 1, i);
                         k_in[i] = load(kh, at2, i);
@@ -1054,6 +1064,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         // o[b][d][i] is dimension 32 d + 8 (i / 4) + 4 half + i % 4 of query `col`
         const bool whole = share.to - share.from == share.all;
         const int64_t at = 2 * block + (share.from == 0);
+        const int half_o = here(half);
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
             const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[b]), __float_as_uint(l[b]), false, false);
@@ -1062,19 +1073,19 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
             if (tok >= t.n) continue;
             if (whole) {
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                const int64_t token = r.first + t.first + tok, head = t.head * (a.heads / a.kv_heads) + t.part * a.group + h;
+                const int64_t token = r.first + t.first + tok, head = t.head * a.per_kv + t.part * a.group + h;
                 uint16_t *dst = a.out + token * a.out_token + head * a.out_head;
 #pragma unroll
                 for (int d = 0; d < kCols; ++d)
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
-                        const int dim = 32 * d + 2 * i + 4 * half;
+                        const int dim = 32 * d + 2 * i + 4 * half_o;
                         if (dim < a.dim)
                             *reinterpret_cast<u32x2 *>(dst + dim) =
                                 u32x2{pack<kHalf>(o[b][d][i] * inv, o[b][d][i + 1] * inv),
                                       pack<kHalf>(o[b][d][i + 2] * inv, o[b][d][i + 3] * inv)};
                     }
-                if (a.lse && half == 0)
+                if (a.lse && half_o == 0)
                     a.lse[token * a.heads + head] = sum == 0.f ? -INFINITY : m[b] * a.scale + logf(sum);
             } else {
                 float *dst = a.sums + (at * kRows + row) * DP;
@@ -1082,9 +1093,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
                 for (int d = 0; d < kCols; ++d)
 #pragma unroll
                     for (int i = 0; i < 16; i += 4)
-                        *reinterpret_cast<f32x4 *>(dst + 32 * d + 2 * i + 4 * half) =
+                        *reinterpret_cast<f32x4 *>(dst + 32 * d + 2 * i + 4 * half_o) =
                             f32x4{o[b][d][i], o[b][d][i + 1], o[b][d][i + 2], o[b][d][i + 3]};
-                if (half == 0) {
+                if (half_o == 0) {
                     float *ml = a.sums + 2 * (int64_t)a.blocks * kRows * DP + (at * kRows + row) * 2;
                     ml[0] = m[b];
                     ml[1] = sum;
@@ -1093,7 +1104,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
         }
         // (`odd` was written before the last barrier, and the next tile writes it after one)
         if (__builtin_expect(k1 > shared_keys && shared_keys < most && odd == number, 0))
-            add_values<DP, kBlocks, kHalf, kSeen>(a, r, t, max(k0, shared_keys), min(k1, most), whole, at);
+            add_values<DP, kWaves, kBlocks, kHalf, kSeen>(a, r, t, max(k0, shared_keys), min(k1, most), whole, at);
     }
 }
 
@@ -1106,8 +1117,11 @@ __global__ void __launch_bounds__(kThreads, kBlocks == 1 && DP == 64 ? 2 : 1) k_
 // it, else the partial sums' bytes.
 // us per call: 3.9 for one row of 700 tokens, 7.7 for 4 tiles in 512 pieces (12 with the first
 // cut's blocks alone), 15.5 for 255 cuts of 256 rows of 128 (70 MB).
-template <int DP, int kRows, bool kHalf>
+// kSeen: rows of up to 16 pieces take a group each in tiles of 256 too, as their blocks would take several in turn (14.7 -> 10.7
+// us for four trees over 60,000 tokens).
+template <int DP, int kRows, bool kHalf, bool kSeen>
 __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
+    constexpr int kMost = kSeen && kRows == 256 ? 16 : 5;  // pieces of a row that a group takes alone
     constexpr int kLanes = DP / 4, kGroups = kThreads / kLanes;
     __shared__ float part[kGroups][DP];
     __shared__ float part_l[kGroups];
@@ -1133,30 +1147,38 @@ __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
                 u32x2{pack<kHalf>(x[0] * inv, x[1] * inv), pack<kHalf>(x[2] * inv, x[3] * inv)};
         if (a.lse && lane == 0) a.lse[token * a.heads + head] = l == 0.f ? -INFINITY : mx * a.scale + logf(l);
     };
-    if (!many) {
-        const int pieces = t.more + 2;  // five at most, asked for together
+    const int pieces = t.back + t.more + 2;
+    if (!many || (kMost > 5 && pieces <= kMost && row1 - row0 > 1)) {  // a group to a row; five pieces are asked for together
         for (int row = row0 + g; row < row1; row += kGroups) {
-            f32x4 part_sum[5];
-            float mi[5], li[5], mx = -INFINITY;
+            f32x4 x[5], sum{0, 0, 0, 0};
+            float mi[5], li[5], mx = -INFINITY, l = 0.f;
+            auto fetch = [&](int p0) {
 #pragma unroll
-            for (int i = 0; i < 5; ++i) {
-                mi[i] = -INFINITY;
-                if (i >= pieces) continue;
-                const int64_t at = slot_of(cut - 1 + i) * kRows + row;
-                mi[i] = ml[at * 2];
-                li[i] = ml[at * 2 + 1];
-                part_sum[i] = *reinterpret_cast<const f32x4 *>(a.sums + at * DP + 4 * lane);
-            }
+                for (int i = 0; i < 5; ++i) {
+                    mi[i] = -INFINITY;
+                    if (p0 + i >= pieces) continue;
+                    const int64_t at = slot_of(cut - 1 + p0 + i) * kRows + row;
+                    mi[i] = ml[at * 2];
+                    li[i] = ml[at * 2 + 1];
+                    x[i] = *reinterpret_cast<const f32x4 *>(a.sums + at * DP + 4 * lane);
+                }
+            };
+            fetch(0);
+#pragma unroll
+            for (int i = 5; i < kMost; ++i)
+                if (i < pieces) mx = fmaxf(mx, ml[(slot_of(cut - 1 + i) * kRows + row) * 2]);
 #pragma unroll
             for (int i = 0; i < 5; ++i) mx = fmaxf(mx, mi[i]);
-            f32x4 sum{0, 0, 0, 0};
-            float l = 0.f;
+            for (int p = 0;;) {
 #pragma unroll
-            for (int i = 0; i < 5; ++i) {
-                if (i >= pieces) break;
-                const float keep = mi[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi[i] - mx) * c);
-                sum += part_sum[i] * keep;
-                l += li[i] * keep;
+                for (int i = 0; i < 5; ++i) {
+                    if (p + i >= pieces) break;
+                    const float keep = mi[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mi[i] - mx) * c);
+                    sum += x[i] * keep;
+                    l += li[i] * keep;
+                }
+                if (kMost == 5 || (p += 5) >= pieces) break;
+                fetch(p);
             }
             write(row, sum, l, mx);
         }
@@ -1214,11 +1236,11 @@ Shape shape_of(const tam_chunk &c, int64_t heads) {
 
 int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
 
-template <int DP, int kRows, bool kHalf>
+template <int DP, int kRows, bool kHalf, bool kSeen>
 hipError_t launch_join(const Attend &a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_join<DP, kRows, kHalf>), dim3((unsigned)a.blocks - 1, kRows == 16 ? 4 : 16), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_join<DP, kRows, kHalf, kSeen>), dim3((unsigned)a.blocks - 1, kRows == 16 ? 4 : 16), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
@@ -1227,25 +1249,25 @@ bool runs(const Attend &a) {
     return a.shift >= 4 && a.page_stride <= INT32_MAX && a.token_stride <= (INT32_MAX / 2) >> a.shift;
 }
 
-template <int DP, int kBlocks, bool kHalf, bool kSeen>
+template <int DP, int kWaves, int kBlocks, bool kHalf, bool kSeen>
 hipError_t launch_wide(const Attend &a, hipStream_t s) {
     constexpr size_t kLds = 2 * kWideKeys * (DP + 8 + DP + 16) * sizeof(uint16_t);
     if (runs(a))
-        hipLaunchKernelGGL((k_attend_wide<DP, kBlocks, kHalf, true, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
+        hipLaunchKernelGGL((k_attend_wide<DP, kWaves, kBlocks, kHalf, true, kSeen>), dim3((unsigned)a.blocks), dim3(kWave * kWaves), kLds, s, a);
     else
-        hipLaunchKernelGGL((k_attend_wide<DP, kBlocks, kHalf, false, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), kLds, s, a);
-    return launch_join<DP, 128 * kBlocks, kHalf>(a, s);
+        hipLaunchKernelGGL((k_attend_wide<DP, kWaves, kBlocks, kHalf, false, kSeen>), dim3((unsigned)a.blocks), dim3(kWave * kWaves), kLds, s, a);
+    return launch_join<DP, 32 * kWaves * kBlocks, kHalf, kSeen>(a, s);
 }
 
 template <int DP, bool kHalf, bool kSeen>
 hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
-    if (sh.rows == 256) return launch_wide<DP, 2, kHalf, kSeen>(a, s);
-    if (sh.rows == 128) return launch_wide<DP, 1, kHalf, kSeen>(a, s);
+    if (sh.rows == 256) return DP == 64 && kSeen ? launch_wide<64, 8, 1, kHalf, kSeen>(a, s) : launch_wide<DP, 4, 2, kHalf, kSeen>(a, s);
+    if (sh.rows == 128) return launch_wide<DP, 4, 1, kHalf, kSeen>(a, s);
     if (runs(a))
         hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, true, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
     else
         hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, false, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);
-    return launch_join<DP, 16, kHalf>(a, s);
+    return launch_join<DP, 16, kHalf, kSeen>(a, s);
 }
 
 template <int DP, bool kHalf>
@@ -1268,7 +1290,7 @@ hipError_t launch_attend(const tam_chunk &c, const Queries &q, const Seen &seen,
              c.head_stride, c.token_stride, q.q_token, q.q_head, q.out_token, q.out_head, c.table, c.length,
              c.offsets, c.slot_ids, c.table_stride, c.slots, c.max_pages, c.rows, c.tokens, (int32_t)c.num_pages,
              __builtin_ctzll((unsigned long long)c.page_tokens), (int32_t)q.heads, (int32_t)c.kv_heads,
-             (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, 0, nullptr, nullptr, seen.bits, seen.stride, seen.words};
+             (int32_t)group, (int32_t)c.head_dim, q.scale, 0, 0, 0, 0, 0, 0, nullptr, nullptr, seen.bits, seen.stride, seen.words};
     a.group = (int32_t)std::min<int64_t>(group, sh.rows);
     a.parts = (int32_t)((group + a.group - 1) / a.group);
     a.tq = sh.rows / a.group;
