@@ -55,7 +55,8 @@ __global__ void __launch_bounds__(kTreeThreads) k_tree(const int32_t *__restrict
         const int32_t p = in_lds ? held[j] : up[j];
         return p < j ? p : -1;
     };
-    for (int32_t j = threadIdx.x; j < s.n; j += kTreeThreads) {
+    for (int64_t i = threadIdx.x; i < s.n; i += kTreeThreads) {
+        const int32_t j = (int32_t)i;
         uint64_t *row = seen + (s.lo + j) * words;
         int64_t w = words;  // the words from here on are written
         uint64_t bits = 0;
@@ -90,16 +91,15 @@ struct Walk {
 };
 
 // A wave takes a row.  The children of a token come after it, so that a step looks at the tokens from there on, 64 at a time.
-__global__ void __launch_bounds__(kWave) k_walk(Walk a) {
-    const int lane = threadIdx.x;
-    const int64_t i = blockIdx.x;
-    Span s = span_of(a.offsets, i, a.total);
+// (With the lists in registers a call takes as long.)
+__device__ inline void walk(const Walk &a, int64_t i, int lane) {
+    const Span s = span_of(a.offsets, i, a.total);
     const int64_t slot = a.slot_ids ? a.slot_ids[i] : i;
     const bool is = slot >= 0 && slot < a.slots;
     const int32_t most = (int32_t)(a.max_pages << a.shift);
     const int32_t len = is ? min(max(a.length[slot], 0), most) : 0;
     if (!is || s.n == 0) {  // nothing stays, nothing changes
-        for (int32_t d = lane; d < s.n; d += kWave) a.path[s.lo + d] = -1;
+        for (int64_t d = lane; d < s.n; d += kWave) a.path[s.lo + d] = -1;
         if (lane == 0) {
             a.count[i] = a.first[i] = 0;
             a.last[i] = -1;
@@ -129,12 +129,11 @@ __global__ void __launch_bounds__(kWave) k_walk(Walk a) {
         if (d % kWave == kWave - 1) write(d - (kWave - 1), kWave);
         ++d;
         int32_t then = -1;
-        for (int32_t j0 = here + 1; j0 < s.n; j0 += kWave) {
-            const int32_t j = j0 + lane;
-            const bool fits = j < s.n && a.parents[s.lo + j] == here && a.tokens[s.lo + j] == want;
-            const uint64_t some = __ballot(fits);
+        for (int64_t j0 = here + 1; j0 < s.n; j0 += kWave) {
+            const int64_t j = j0 + lane;
+            const uint64_t some = __ballot(j < s.n && a.parents[s.lo + j] == here && a.tokens[s.lo + j] == want);
             if (some) {
-                then = j0 + __builtin_ctzll(some);
+                then = (int32_t)j0 + __builtin_ctzll(some);
                 break;
             }
         }
@@ -143,7 +142,7 @@ __global__ void __launch_bounds__(kWave) k_walk(Walk a) {
         want = a.picks[s.lo + here];
     }
     if (d % kWave) write(d / kWave * kWave, d % kWave);
-    for (int32_t j = d + lane; j < s.n; j += kWave) a.path[s.lo + j] = -1;
+    for (int64_t j = (int64_t)d + lane; j < s.n; j += kWave) a.path[s.lo + j] = -1;
     const int32_t now = max(base + d, 0);
     if (lane == 0) {
         a.count[i] = d;
@@ -160,6 +159,8 @@ __global__ void __launch_bounds__(kWave) k_walk(Walk a) {
     }
 }
 
+__global__ void __launch_bounds__(kWave) k_walk(Walk a) { walk(a, blockIdx.x, threadIdx.x); }
+
 struct Shift {
     uint8_t *data;
     int64_t plane_stride, head_stride;  // bytes
@@ -172,13 +173,12 @@ struct Shift {
 
 constexpr int kShiftThreads = 256, kTogether = 4;
 
-// A thread takes 16 bytes of a plane and head, of all the row's tokens that move.
-__global__ void __launch_bounds__(kShiftThreads) k_shift(Shift a) {
-    const int64_t i = blockIdx.x;
+// A thread takes 16 bytes of a plane and head (items x, x + step, ...), of all the tokens of row i that move.
+__device__ inline void shift(const Shift &a, int64_t i, int64_t x, int64_t step) {
     const int32_t from = a.first[i], to = a.count[i];
     if (from >= to) return;
     const int64_t lo = span_of(a.offsets, i, a.total).lo;
-    for (int64_t x = blockIdx.y * (int64_t)kShiftThreads + threadIdx.x; x < a.items; x += (int64_t)gridDim.y * kShiftThreads) {
+    for (; x < a.items; x += step) {
         const int64_t vector = x / a.pieces, plane = vector / a.heads;
         uint8_t *const at = a.data + plane * a.plane_stride + (vector - plane * a.heads) * a.head_stride + (x - vector * a.pieces) * 16;
         for (int32_t d = from; d < to; d += kTogether) {
@@ -197,6 +197,19 @@ __global__ void __launch_bounds__(kShiftThreads) k_shift(Shift a) {
     }
 }
 
+__global__ void __launch_bounds__(kShiftThreads) k_shift(Shift a) {
+    shift(a, blockIdx.x, blockIdx.y * (int64_t)kShiftThreads + threadIdx.x, (int64_t)gridDim.y * kShiftThreads);
+}
+
+// Both for a row in one block.
+constexpr int kBothThreads = 1024;
+
+__global__ void __launch_bounds__(kBothThreads) k_walk_shift(Walk w, Shift a) {
+    if (threadIdx.x < kWave) walk(w, blockIdx.x, threadIdx.x);
+    __syncthreads();
+    shift(a, blockIdx.x, threadIdx.x, kBothThreads);
+}
+
 }  // namespace
 
 hipError_t launch_tree_masks(const int32_t *parents, const int32_t *offsets, int64_t rows, int64_t tokens, uint64_t *seen,
@@ -204,6 +217,11 @@ hipError_t launch_tree_masks(const int32_t *parents, const int32_t *offsets, int
     hipLaunchKernelGGL(k_tree, dim3((unsigned)rows), dim3(kTreeThreads), 0, s, parents, offsets, tokens, seen, words, depth);
     return hipGetLastError();
 }
+
+// Up to this many pieces of 16 bytes to a token (8 layers of 8 heads of 128) one launch does both, which costs the host 2.5 us
+// less.  us on the device per call of 1 and 128 trees of 32 tokens, 4 layers: 2.6 and 7.0, in two launches 3.9 and 7.4; 8 layers:
+// 5.3 and 10.4, 5.5 and 9.4; 16 layers: 7.3 and 13.5, 5.8 and 11.5.
+constexpr int64_t kBothItems = 2048;
 
 // places from and to of each token, and each row's first move
 int64_t accept_work_bytes(const tam_chunk &n) { return 16 * n.tokens + 4 * n.rows; }
@@ -215,12 +233,16 @@ hipError_t launch_pages_accept(const tam_pages &c, const tam_chunk &n, const int
     const Walk a{tokens, picks, parents, n.offsets, n.slot_ids, n.rows, n.tokens, c.table, c.length, c.refs, c.slots, c.max_pages,
                  c.table_stride, (int32_t)c.num_pages, __builtin_ctzll((unsigned long long)c.page_tokens), c.page_stride,
                  2 * n.token_stride, path, count, last, src, dst, first};
-    hipLaunchKernelGGL(k_walk, dim3((unsigned)n.rows), dim3(kWave), 0, s, a);
-    const hipError_t e = hipGetLastError();
     const int64_t pieces = n.head_dim / 8, items = c.planes * n.kv_heads * pieces;
-    if (e != hipSuccess || items == 0) return e;
     const Shift m{static_cast<uint8_t *>(c.data), c.plane_stride, 2 * n.head_stride, n.offsets, count, first, src, dst, n.tokens,
                   (int32_t)n.kv_heads, (int32_t)pieces, items};
+    if (items <= kBothItems) {
+        hipLaunchKernelGGL(k_walk_shift, dim3((unsigned)n.rows), dim3(kBothThreads), 0, s, a, m);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL(k_walk, dim3((unsigned)n.rows), dim3(kWave), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     const int64_t blocks = std::min<int64_t>((items + kShiftThreads - 1) / kShiftThreads, 1024);
     hipLaunchKernelGGL(k_shift, dim3((unsigned)n.rows, (unsigned)blocks), dim3(kShiftThreads), 0, s, m);
     return hipGetLastError();
