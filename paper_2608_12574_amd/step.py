@@ -34,15 +34,15 @@ def _rows_of(where, name, t, B, dtype, gpu):
     return t.data_ptr(), stride if rows > 1 else n, n
 
 
-_int = _float = _long = None  # torch's types, once torch is there
+_int = _float = _long = _byte = None  # torch's types, once torch is there
 
 
 def _ready():
-    global _int, _float, _long
+    global _int, _float, _long, _byte
     import torch
     c = _calls()
     c.adjust = _tam.lib().tam_adjust_logits
-    _int, _float, _long = torch.int32, torch.float32, torch.int64
+    _int, _float, _long, _byte = torch.int32, torch.float32, torch.int64, torch.uint8
     return c
 
 
@@ -131,14 +131,14 @@ def adjust_logits(logits, tokens=None, length=None, prompt=None, repetition=None
                    repetition=repetition, frequency=frequency, presence=presence, bias_ids=bias_ids, bias=bias)
 
 
-def _scratch(shape, dtype, device, stream):
+def _scratch(dtype, device, stream, *shape):
     """Memory for a call on ``stream``: from that stream's share of torch's allocator, so that
     nothing still running on another stream holds it."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
 
 
 def top_tokens(logits, k, return_lse=False, stream=None):
@@ -146,7 +146,6 @@ def top_tokens(logits, k, return_lse=False, stream=None):
     leave them: (int32 [B, k] tokens, fp32 [B, k] log probabilities) in descending order, of equal logits the lowest token
     first, and with ``return_lse`` the fp32 [B] logarithms of the sums.  Where fewer than ``k`` logits are left (-inf is
     none), the rest is token -1 at -inf.  A NaN is larger than every number, and its row's log probabilities are NaN."""
-    import torch
     where = "tam_top_tokens"
     c = _tam._calls_made if _int is not None else _ready()
     dtype = c.dtypes.get(logits.dtype)
@@ -164,9 +163,9 @@ def top_tokens(logits, k, return_lse=False, stream=None):
     if size < 0:
         _check(-1, where)
     device = logits.device
-    tokens, logprobs = _scratch((B, k), _int, device, stream), _scratch((B, k), _float, device, stream)
-    lse = _scratch(B, _float, device, stream) if return_lse else None
-    work = _scratch(size, torch.uint8, device, stream) if size else None
+    tokens, logprobs = _scratch(_int, device, stream, B, k), _scratch(_float, device, stream, B, k)
+    lse = _scratch(_float, device, stream, B) if return_lse else None
+    work = _scratch(_byte, device, stream, size) if size else None
     rc = lib.tam_top_tokens(logits.data_ptr(), dtype, B, V, row_stride, k, tokens.data_ptr(), logprobs.data_ptr(),
                             lse.data_ptr() if return_lse else None, work.data_ptr() if size else None, on)
     if rc != TAM_OK:
@@ -198,7 +197,8 @@ def tree_masks(parents, offsets=None, longest=None, stream=None):
     if longest is None:
         longest = T if offsets is not None else 1
     words = max(1, (longest + 63) // 64)
-    seen, depth = _scratch((T, words), _long, parents.device, stream), _scratch(T, _int, parents.device, stream)
+    device = parents.device
+    seen, depth = _scratch(_long, device, stream, T, words), _scratch(_int, device, stream, T)
     rc = _tam.lib().tam_tree_masks(up, off, rows, T, seen.data_ptr(), words, depth.data_ptr(), on)
     if rc != TAM_OK:
         _check(rc, where)
@@ -236,7 +236,7 @@ class PageCache:
         refs_p = _int32(where, "refs", refs, pages, gpu)
         self.data, self.table, self.length, self.refs = data, table, length, refs
         self.layers, self.kv_heads, self.page_tokens, self.head_dim = planes // 2, kv, page, dim
-        self._torch, self._device = torch, data.device
+        self._torch, self._device, self._dtype = torch, data.device, data.dtype
         size = data.element_size()
         self._pages = Pages(data.data_ptr(), planes, data.stride(0) * size, data.stride(1) * size, kv * page * dim * size,
                             pages, page, table.data_ptr(), slots, width, stride, length_p, refs_p)
@@ -261,7 +261,7 @@ class PageCache:
 
     # -- pages -----------------------------------------------------------------
     def _empty(self, shape, dtype, stream):
-        return _scratch(shape, dtype, self._device, stream)
+        return _scratch(dtype, self._device, stream, shape)
 
     def _work(self, stream):
         return self._empty(self._work_bytes, self._torch.uint8, stream)
@@ -342,12 +342,13 @@ class PageCache:
 
     def _vectors(self, where, name, t, heads=None):
         """(pointer, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
-        if (t.dim() != 3 or t.get_device() != self._gpu or t.dtype is not self.data.dtype or t.shape[2] != self.head_dim
-                or t.stride(2) != 1 or (heads is not None and t.shape[1] != heads)):
+        shape, strides = t.shape, t.stride()
+        if (len(shape) != 3 or t.get_device() != self._gpu or t.dtype is not self._dtype or shape[2] != self.head_dim
+                or strides[2] != 1 or (heads is not None and shape[1] != heads)):
             raise _bad(where, f"{name} must be a [tokens, {heads or 'heads'}, {self.head_dim}] {self.data.dtype} tensor "
                               f"on cuda:{self._gpu} with contiguous vectors")
         # of a single token or head any stride will do
-        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+        return t.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1] if shape[1] > 1 else 0
 
     def store(self, layer, k, v, offsets=None, slots=None, longest=None, stream=None):
         """K and V [tokens, kv_heads, head_dim] of the new tokens into their pages.  Row i's tokens are
@@ -375,17 +376,19 @@ class PageCache:
         T = k.shape[0]
         qp = op = (None, 0, 0)
         heads = 0
+        if v.shape[0] != T or (q is not None and q.shape[0] != T):
+            raise _bad(where, "q, k and v have different numbers of tokens")
         if q is not None:
             qp, heads = self._vectors(where, "q", q), q.shape[1]
             if out is None:
-                out = self._empty((T, heads, self.head_dim), q.dtype, stream)
+                out = _scratch(self._dtype, self._device, stream, T, heads, self.head_dim)
+                op = out.data_ptr(), heads * self.head_dim, self.head_dim
             elif out.shape != q.shape:
                 raise _bad(where, "out must have q's shape")
-            op = self._vectors(where, "out", out)
+            else:
+                op = self._vectors(where, "out", out)
         elif out is not None:
             raise _bad(where, "out without q")
-        if v.shape[0] != T or (q is not None and q.shape[0] != T):
-            raise _bad(where, "q, k and v have different numbers of tokens")
         if frequencies.dtype is not _float or frequencies.get_device() != self._gpu or frequencies.dim() != 1 or (
                 not frequencies.is_contiguous()):
             raise _bad(where, f"frequencies must be a contiguous [pairs] fp32 tensor on cuda:{self._gpu}")
@@ -412,17 +415,19 @@ class PageCache:
         qp = self._vectors(where, "q", q)
         T, heads = q.shape[0], q.shape[1]
         if out is None:
-            out = self._empty((T, heads, self.head_dim), q.dtype, stream)
+            out = _scratch(self._dtype, self._device, stream, T, heads, self.head_dim)
+            op = out.data_ptr(), heads * self.head_dim, self.head_dim
         elif out.shape != q.shape:
             raise _bad(where, "out must have q's shape")
-        op = self._vectors(where, "out", out)
-        lse = self._empty((T, heads), self._torch.float32, stream) if return_lse else None
+        else:
+            op = self._vectors(where, "out", out)
+        lse = _scratch(_float, self._device, stream, T, heads) if return_lse else None
         chunk = self._new(where, layer, T, offsets, slots, longest)
         lib = self._lib
         size = lib.tam_attend_work(chunk, heads)
         if size < 0:
             _check(-1, where)
-        work = self._empty(size, self._torch.uint8, stream) if size else None
+        work = _scratch(_byte, self._device, stream, size) if size else None
         scale = self.head_dim ** -0.5 if scale is None else scale
         rest = *op, lse.data_ptr() if return_lse else None, work.data_ptr() if size else None, on
         if seen is None:
@@ -451,11 +456,12 @@ class PageCache:
         size = self._lib.tam_pages_accept_work(chunk)
         if size < 0:
             _check(-1, where)
-        int32 = self._torch.int32
-        path, count, last = self._empty(T, int32, stream), self._empty(rows, int32, stream), self._empty(rows, int32, stream)
-        work = self._empty(size, self._torch.uint8, stream)
-        rc = self._lib.tam_pages_accept(self._pages_ref, chunk, *lists, path.data_ptr(), count.data_ptr(), last.data_ptr(),
-                                        work.data_ptr(), on)
+        # one piece of memory, which costs the host less than four: the scratch, the path, the two lists
+        words = (size + 15) // 16 * 4
+        both = _scratch(_int, self._device, stream, words + T + 2 * rows)
+        at = both.data_ptr()
+        rc = self._lib.tam_pages_accept(self._pages_ref, chunk, *lists, at + 4 * words, at + 4 * (words + T),
+                                        at + 4 * (words + T + rows), at, on)
         if rc != TAM_OK:
             _check(rc, where)
-        return path, count, last
+        return both.split((words, T, rows, rows))[1:]

@@ -127,7 +127,7 @@ def fake(P, two_gpus, monkeypatch):
     real = P.tam.lib
     monkeypatch.setattr(P.tam, "lib", lambda: lib)
     from paper_2608_12574_amd import step
-    monkeypatch.setattr(step, "_scratch", lambda shape, dtype, device, stream: On(torch.empty(shape, dtype=dtype), 0))
+    monkeypatch.setattr(step, "_scratch", lambda dtype, device, stream, *shape: On(torch.empty(*shape, dtype=dtype), 0))
 
     def cache(gpu):
         monkeypatch.setattr(P.tam, "lib", real)  # the size of the pages' scratch
