@@ -53,7 +53,7 @@ class Decoder:
 def search(model, handle, ends, prompts, width=4, most=32, presence=0.3, page_tokens=16):
     """The finished beams of each prompt, best first: [(score, tokens after the prompt)].  ``ends`` [V]: whether a
     token closes its string."""
-    groups, V = len(prompts), len(ends)
+    groups = len(prompts)
     B = groups * width
     int32 = dict(dtype=torch.int32, device="cuda")
     longest = max(len(p) for p in prompts)
@@ -81,11 +81,11 @@ def search(model, handle, ends, prompts, width=4, most=32, presence=0.3, page_to
     for step in range(most):
         at = begin + step
         handle.adjust_logits(nodes, logits, tokens=text, length=at, prompt=begin, presence=penalty)
-        total = (F.log_softmax(logits.float(), 1) + score.view(B, 1)).view(groups, width * V)
-        total = torch.where(total.isnan(), -torch.inf, total)  # a dead beam: nothing is valid
-        score, pick = total.topk(width, 1)
-        parents = (pick // V + torch.arange(0, B, width, device="cuda")[:, None]).view(B).to(torch.int32)
-        token = (pick % V).view(B).to(torch.int32)
+        # a group's best continuations are among each beam's (of a dead beam: token -1 at -inf)
+        best, total = tam.top_tokens(logits, width)
+        score, pick = (total + score.view(B, 1)).view(groups, width * width).topk(width, 1)
+        parents = (pick // width + torch.arange(0, B, width, device="cuda")[:, None]).view(B).to(torch.int32)
+        token = best.view(groups, width * width).gather(1, pick).view(B)
         text = text[parents.long()]
         text[slots.long(), at.long()] = token
         nodes = handle.advance(nodes[parents.long()], token)

@@ -4,7 +4,7 @@
 // before the row.  Parents come before their children, so every walk up or down ends.
 //
 // k_tree: seen(j) = {j} + seen(p), depth(j) = depth(p) + 1.
-// k_walk: from token 0 on to the first child that the choice made after a token names; a token that stays at depth d moves to
+// k_walk: from token 0 on to the first child that the choice made after a token names (below 0: none); a token that stays at depth d moves to
 // place d of the row, the row's other tokens are cut off, and pages past the new length are given back.
 // k_shift: the moves themselves, in every plane.  path[d] >= d grows with d, so a place moved to is never one that
 // a later token is still to be moved from, and a thread may move its piece of the tokens in their order.
@@ -129,7 +129,7 @@ __device__ inline void walk(const Walk &a, int64_t i, int lane) {
         if (d % kWave == kWave - 1) write(d - (kWave - 1), kWave);
         ++d;
         int32_t then = -1;
-        for (int64_t j0 = here + 1; j0 < s.n; j0 += kWave) {
+        for (int64_t j0 = here + 1; want >= 0 && j0 < s.n; j0 += kWave) {
             const int64_t j = j0 + lane;
             const uint64_t some = __ballot(j < s.n && a.parents[s.lo + j] == here && a.tokens[s.lo + j] == want);
             if (some) {

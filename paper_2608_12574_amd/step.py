@@ -444,7 +444,7 @@ class PageCache:
         """Of the new tokens' trees the path that the model's choices follow stays in the cache, in every layer.  Rows as for
         ``store``; ``tokens``, ``picks`` and ``parents`` int32 [tokens]: the drafted tokens, the choice after each, and their
         parents (as for ``tree_masks``).  A row's token 0 stays; after a token that stays, the first one that follows it and
-        is its choice.  They move to the places behind the text before the row, the slot ends there, and pages past its
+        is its choice (below 0, as ``top_tokens`` gives where nothing is valid: none).  They move to the places behind the text before the row, the slot ends there, and pages past its
         end are given back.  Returns, on the GPU, int32 [tokens]: the numbers in the row of its tokens that stay, then -1;
         int32 [rows]: how many; int32 [rows]: the choice after the last one (-1 for an empty row)."""
         where = "tam_pages_accept"

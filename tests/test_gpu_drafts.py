@@ -451,7 +451,7 @@ def accepted(parents, tokens, picks):
     path = [0] if parents else []
     while path:
         here = path[-1]
-        then = [j for j in range(here + 1, len(parents)) if parents[j] == here and tokens[j] == picks[here]]
+        then = [j for j in range(here + 1, len(parents)) if parents[j] == here and tokens[j] == picks[here] >= 0]
         if not then:
             break
         path.append(then[0])
@@ -484,8 +484,8 @@ def check_accept(P, rng, chunks, befores, page, kv=2, dim=16, layers=2, slots=No
     trees, tokens, picks = [], [], []
     for n in chunks:
         p = forest(rng, n, bushy, odd)
-        t = rng.integers(0, 6, n).tolist()
-        pick = rng.integers(0, 6, n).tolist()
+        t = rng.integers(-1, 6, n).tolist()
+        pick = rng.integers(-1, 6, n).tolist()
         for j in range(1, n):
             if 0 <= p[j] < j and rng.random() < likely:
                 pick[p[j]] = t[j]
@@ -672,3 +672,122 @@ def test_top_of_a_view_and_empty(P):
     check_top(P, y, 3)
     h.close()
     assert torch.equal(w[0], P.top_tokens(x, 9)[0])
+
+
+# --------------------------------------------------------------- together -------
+
+def test_tree_step_in_a_graph(P):
+    """A whole step over drafted trees captured, and replayed with eager work between the replays."""
+    rng = np.random.default_rng(3)
+    chunks, lens = [9, 20, 0, 33], [300, 90, 12, 33]
+    s = Trees(P, lens, chunks, 8, 2, 64, 16, torch.bfloat16, seed=14, garbage=0.5)
+    c = s.cache
+    T = sum(chunks)
+    trees = [forest(rng, n) for n in chunks]
+    up = ints(sum(trees, []))
+    tokens = ints([t for n in chunks for t in rng.integers(0, 4, n)])
+    k, v = (torch.randn((T, 2, 64), generator=gen(i), device="cuda").to(torch.bfloat16) for i in (1, 2))
+    logits = torch.randn((T, 5003), generator=gen(3), device="cuda").to(torch.bfloat16)
+    logits[:, 4:] -= 8  # mostly one of the first four tokens
+    f = torch.rand(32, generator=gen(4), device="cuda")
+    kept = [x.clone() for x in (c.data, c.table, c.length, c.refs)]
+
+    def step():
+        for x, y in zip((c.data, c.table, c.length, c.refs), kept):
+            x.copy_(y)
+        seen, depth = P.tree_masks(up, s.offsets, longest=40)
+        q = c.append(1, s.q, k, v, f, depth=depth, offsets=s.offsets, longest=40)
+        out, lse = c.attend(1, q, offsets=s.offsets, longest=40, seen=seen, return_lse=True)
+        best, logprobs, sums = P.top_tokens(logits, 5, return_lse=True)
+        path, count, last = c.accept(tokens, best[:, 0].contiguous(), up, offsets=s.offsets)
+        return seen, depth, q, out, lse, best, logprobs, sums, path, count, last
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in step()]
+    state = [x.clone() for x in (c.data, c.table, c.length, c.refs)]
+    assert int(want[9].max()) > 1 and not torch.equal(state[2], kept[2])
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    got = []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            got.append(step())
+    for i in range(6):
+        for x in got[i % 2]:
+            x.zero_()
+        c.data.zero_()
+        c.length.zero_()
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        for x, y in zip((*got[i % 2], c.data, c.table, c.length, c.refs), (*want, *state)):
+            assert torch.equal(x, y)
+        torch.randn(1000, device="cuda").sum().item()
+        P.top_tokens(logits, 3)
+
+
+def test_calls_on_two_streams_at_once(P):
+    logits = [torch.randn((40, 70001), generator=gen(i), device="cuda") for i in (1, 2)]
+    s = [Trees(P, [4000, 900], [40, 25], 8, 2, 128, 16, torch.bfloat16, seed=i) for i in (1, 2)]
+    want = [(*P.top_tokens(x, 9), *y.cache.attend(1, y.q, offsets=y.offsets, seen=y.seen, return_lse=True)) for x, y in zip(logits, s)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, on in enumerate(streams):
+            got[i].append((*P.top_tokens(logits[i], 9, stream=on),
+                           *s[i].cache.attend(1, s[i].q, offsets=s[i].offsets, seen=s[i].seen, return_lse=True, stream=on)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for calls in got[i]:
+            for x, y in zip(calls, want[i]):
+                assert torch.equal(x, y)
+
+
+def plain_decoder(model, tokens):
+    """The example's decoder over one text, in 64 bits: [tokens, vocab] logits."""
+    x = model.embed[torch.tensor(tokens, device="cuda")].double()
+    norm = lambda x: x * torch.rsqrt((x * x).mean(-1, keepdim=True) + torch.finfo(torch.bfloat16).eps)
+    T, heads, kv, dim = len(tokens), model.heads, model.kv_heads, model.head_dim
+    position = torch.arange(T, device="cuda")
+    hidden = position[None, :] > position[:, None]
+    for qkv, out, up, down in model.layers:
+        y = norm(x) @ qkv.double().T
+        q, k, v = y[:, :heads * dim].view(T, heads, dim), y[:, heads * dim:(heads + kv) * dim].view(T, kv, dim), y[:, (heads + kv) * dim:].view(T, kv, dim)
+        q, k = (turned(z, position, model.frequencies, False)[0] for z in (q, k))
+        a = torch.empty((T, heads, dim), dtype=torch.float64, device="cuda")
+        for h in range(heads):
+            score = (q[:, h] @ k[:, h // (heads // kv)].T.contiguous() * dim ** -0.5).masked_fill(hidden, -math.inf)
+            a[:, h] = torch.softmax(score, 1) @ v[:, h // (heads // kv)]
+        x = x + a.flatten(1) @ out.double().T
+        gate, y = (norm(x) @ up.double().T).chunk(2, 1)
+        x = x + (torch.nn.functional.silu(gate) * y) @ down.double().T
+    return norm(x) @ model.head.double().T
+
+
+@pytest.mark.parametrize("levels", [(), (4, 2, 1), (2, 1, 1, 1, 1), (16, 2)])
+def test_drafts_example(P, levels):
+    """What the example finds with drafts is the greedy continuation: at each token the model's best one, up to the rounding of
+    its logits.  Those are of size 1; bf16 activations of two layers take about 16 roundings of 2^-9 (a half step is at most
+    2^-8 of a value, 2^-9 on average) times the layers' gains of about 2: 16^0.5 2^-9 2 = 0.016, 4 times that for the worst
+    of thousands."""
+    import examples.drafts as E
+    vocab = E.beams.vocabulary()
+    h = P.compile(E.beams.STRINGS, vocab, device="cuda:0")
+    prior = torch.tensor([float(len(t)) for t in vocab], device="cuda")
+    prompts = [list(b"a prompt"), list(b"and one that is longer than a page of the cache"), list(b"x")]
+    model = E.Decoder(len(vocab))
+    found, steps, cache = E.generate(model, h, prior, prompts, levels)
+    assert not cache.refs.any() and not cache.length.any()
+    assert steps == max(len(t) for t in found) if not levels else steps < max(len(t) for t in found)
+    for prompt, tokens in zip(prompts, found):
+        assert b"".join(vocab[t] for t in tokens)[:-1] in E.beams.STRINGS
+        logits = plain_decoder(model, prompt + tokens)
+        node = ints([0])
+        for i, t in enumerate(tokens):
+            row = logits[len(prompt) - 1 + i:len(prompt) + i].float()
+            h.apply_mask(node, row)
+            assert row[0, t] >= row.max() - 2 * 0.064
+            node = h.advance(node, ints([t]))
+    h.close()
