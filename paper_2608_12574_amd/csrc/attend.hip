@@ -1224,10 +1224,16 @@ struct Shape {
     int grid, extra;  // blocks of the launch; keys that stand for a tile's own cost
 };
 
-Shape shape_of(const tam_chunk &c, int64_t heads) {
+// `seen`: with a mask among the new tokens.
+Shape shape_of(const tam_chunk &c, int64_t heads, bool seen) {
     const int64_t longest = c.longest ? std::min(c.longest, c.tokens) : c.tokens;
     const int64_t rows = longest * (heads / c.kv_heads);
     if (rows <= 16) return Shape{16, kNarrowKeys, 512, kNarrowKeys};
+    // One request's small tree over a short text: tiles of 16 rows begin sooner, and K and V read up to four times come from the caches
+    // (us per call in a graph, 16 tokens of 32 and 8 heads of 128 over 300, 700, 1,500, 3,000 and 12,000: 13.3, 14.8, 18.7, 21.0 and
+    // 34.0; in a tile of 128 rows 16.2, 17.5, 19.8, 22.0 and 29.5; four requests, 700 and 3,000: 22.0 and 41.6; 22.8 and 29.0).
+    const int64_t bytes = 4 * c.max_pages * c.page_tokens * c.kv_heads * c.head_dim;
+    if (seen && c.rows == 1 && rows <= 64 && bytes <= 16 << 20) return Shape{16, kNarrowKeys, 512, kNarrowKeys};
     // a batch of mostly short rows fills tiles of 128 rows better (us per call with 128 and 256: 40 chunks of up to
     // 200 tokens, 74 rows on average, 50 and 63; 24 of 265 rows on average, heads of 64, 46 and 41)
     if (rows <= 128 || c.tokens * (heads / c.kv_heads) <= 128 * c.rows) return Shape{128, kWideKeys, 512, 2 * kWideKeys};
@@ -1278,12 +1284,14 @@ hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
 }  // namespace
 
 int64_t attend_work_bytes(const tam_chunk &c, int64_t heads) {
-    const Shape sh = shape_of(c, heads);
-    return 2 * (int64_t)sh.grid * sh.rows * (padded(c.head_dim) + 2) * 4 + sh.grid * (int64_t)sizeof(Cut);
+    auto bytes = [&](const Shape &sh) {
+        return 2 * (int64_t)sh.grid * sh.rows * (padded(c.head_dim) + 2) * 4 + sh.grid * (int64_t)sizeof(Cut);
+    };
+    return std::max(bytes(shape_of(c, heads, false)), bytes(shape_of(c, heads, true)));
 }
 
 hipError_t launch_attend(const tam_chunk &c, const Queries &q, const Seen &seen, void *work, hipStream_t s) {
-    const Shape sh = shape_of(c, q.heads);
+    const Shape sh = shape_of(c, q.heads, seen.bits != nullptr);
     const int64_t group = q.heads / c.kv_heads;
     Attend a{static_cast<const uint16_t *>(c.k), static_cast<const uint16_t *>(c.v),
              static_cast<const uint16_t *>(q.q), static_cast<uint16_t *>(q.out), q.lse, c.page_stride,
