@@ -272,21 +272,17 @@ __global__ void __launch_bounds__(kThreads) k_top(const T *__restrict__ logits, 
         for (int c = 1; c < N; ++c) high[i] = __builtin_elementwise_maximum(high[i], I::get(x[i], c));
         most = __builtin_elementwise_maximum(most, high[i]);
     }
-    // sum exp(x - m) = exp2(mc - m c) sum exp2(x c - mc), c = log2(e), mc = m c rounded: one instruction per exponent, and
-    // it is rounded once.  A maximum of 2^126 or more, whose m c may have no fp32: what is not the maximum adds
-    // nothing, so any c will do that tells the two apart.  -inf: 0, so that nothing is taken from it.
-    fresh();
+    // (x - m is exact where it counts, however large both are.  -inf: 0, so that nothing is taken from it; infinity: the
+    // largest number, and the sum is infinite.)
     Sum sum{most, 0.f};
     const float m = most == -INFINITY ? 0.f : fminf(most, 3.4028234663852886e38f);
-    const float c2 = fabsf(m) < 8.5e37f ? kLog2e : 8.6736174e-19f;
-    const float mc = m * c2;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         if (!__any(!(high[i] == -INFINITY))) continue;  // nothing in the wave's vectors
+        asm volatile("" : "+v"(x[i]));
 #pragma unroll
-        for (int c = 0; c < N; ++c) sum.s += __builtin_amdgcn_exp2f(__builtin_fmaf(I::get(x[i], c), c2, -mc));
+        for (int c = 0; c < N; ++c) sum.s += __builtin_amdgcn_exp2f((I::get(x[i], c) - m) * kLog2e);
     }
-    sum.s *= __builtin_amdgcn_exp2f(__builtin_fmaf(-m, c2, mc));
     if (sum.s != sum.s) sum.m = -INFINITY;
     sum = join_block<kThreads>(sum);
     int n = INT_MAX;

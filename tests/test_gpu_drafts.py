@@ -635,6 +635,18 @@ def test_top_ties_and_masks(P, dtype, V):
         check_top(P, x[3:5], k)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("at", [1e4, -1e4, 1e6, 1e9, -1e9, 1e12, 1e20, -1e20, 1e30, 8e37, 3e38, -3e38])
+def test_top_far_from_zero(P, dtype, at):
+    """Logits around a large number, a few steps of its type apart."""
+    step = abs(at) * torch.finfo(dtype).eps
+    for V in (700, 40001):
+        n = torch.randint(0, 7, (3, V), generator=gen(V), device="cuda").double()
+        x = (at + n * step).to(dtype)
+        assert torch.isfinite(x).all() and x.unique().numel() > 1
+        check_top(P, x, 5)
+
+
 def test_top_infinities_and_nan(P):
     for dtype in (torch.float32, torch.bfloat16):
         for V in (70, 5000, 70000):
