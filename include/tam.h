@@ -689,8 +689,8 @@ typedef struct {
 
 /*
  * tam_pages_append -- tam_pages_store of the new tokens with K turned by their positions, and their queries turned alike:
- * out[t][h] of q[t][h].  Angles are exact to fp32 at any position; elements are turned in fp32 and rounded once.  The
- * tokens' places do not depend on `depth`.
+ * out[t][h] of q[t][h].  Angles of up to 10^8 radians are taken modulo whole turns to fp32's last place; elements are
+ * turned in fp32 and rounded once.  The tokens' places do not depend on `depth`.
  *   k_new, v_new   as for tam_pages_store; the tokens that are left out there are here too.
  *   q, heads, out  as for tam_attend (any number of heads); heads == 0: no queries.  Every token of a row is written; `out` may be
  *                  `q` itself, with its strides.
@@ -718,7 +718,8 @@ tam_status tam_attend_seen(const tam_chunk *c, const void *q, int64_t q_token, i
  *   c, n     the cache, and the new tokens of the call: n names c's tables, and its strides, kv_heads, head_dim and dtype
  *            say where a vector lies in a page; k and v are not read.
  *   tokens, picks, parents  device int32[n->tokens]: the drafted tokens, the model's choice after each, their parents.
- *   path     device int32[n->tokens]: the numbers, in the row, of its tokens that stay, then -1.
+ *   path     device int32[n->tokens]: the numbers, in the row, of its tokens that stay, then -1 (tokens of no row are
+ *            not written).
  *   count    device int32[n->rows]: how many stay (0 for a row without tokens or outside the slots, which changes nothing).
  *   last     device int32[n->rows]: the choice after the last of them (-1 if none): the next token of the text.
  *   work     tam_pages_accept_work(n) bytes.

@@ -447,8 +447,9 @@ class PageCache:
         ``store``; ``tokens``, ``picks`` and ``parents`` int32 [tokens]: the drafted tokens, the choice after each, and their
         parents (as for ``tree_masks``).  A row's token 0 stays; after a token that stays, the first one that follows it and
         is its choice (below 0, as ``top_tokens`` gives where nothing is valid: none).  They move to the places behind the text before the row, the slot ends there, and pages past its
-        end are given back.  Returns, on the GPU, int32 [tokens]: the numbers in the row of its tokens that stay, then -1;
-        int32 [rows]: how many; int32 [rows]: the choice after the last one (-1 for an empty row)."""
+        end are given back.  Returns, on the GPU, int32 [tokens]: the numbers in the row of its tokens that stay, then -1
+        (tokens of no row are not written); int32 [rows]: how many; int32 [rows]: the choice after the last one (-1 for an
+        empty row)."""
         where = "tam_pages_accept"
         on = self._on(where, stream)
         T, gpu = tokens.numel(), self._gpu

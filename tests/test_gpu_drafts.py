@@ -579,6 +579,50 @@ def test_accept_places_that_are_not_there(P):
     assert c.length.tolist() == [2, 11, 11] and c.table.tolist() == [[0, 1, 2], [3, 99, 4], [5, 6, 7]]
 
 
+def test_append_and_accept_past_32_bits(P):
+    """Pages past 2^31 elements of a plane, and a move from one to another."""
+    c = P.PageCache.empty(1, 8, 128, 70000, 2, 4, page_tokens=64)
+    c.table.copy_(ints([[69999, 3, 69000, -1], [2, 69998, -1, -1]]))
+    c.length.copy_(ints([130, 70]))
+    c.refs[[69999, 3, 69000, 2, 69998]] = 1
+    k, v = (torch.randn((70, 8, 128), generator=gen(i), device="cuda").to(torch.bfloat16) for i in (1, 2))
+    off = ints([0, 67, 70])
+    c.append(0, None, k, v, torch.zeros(64, device="cuda"), offsets=off)
+    # row 0's tokens lie at 63 .. 129: the first in page 69999, the last two in page 69000; row 1's at 67 .. 69, in page 69998
+    for t, page, place in ((0, 69999, 63), (1, 3, 0), (64, 3, 63), (65, 69000, 0), (66, 69000, 1), (67, 69998, 3), (69, 69998, 5)):
+        assert torch.equal(c.data[0, page, :, place], k[t]) and torch.equal(c.data[1, page, :, place], v[t])
+    up = ints([-1] + [0] * 65 + [65] + [-1, 0, 0])
+    token = ints([0] + [1] * 64 + [2, 3] + [0, 1, 2])
+    pick = ints([2] + [9] * 64 + [3, 7] + [2, 9, 5])
+    path, count, last = c.accept(token, pick, up, offsets=off)
+    assert count.tolist() == [3, 2] and last.tolist() == [7, 5] and c.length.tolist() == [66, 69]
+    for t, page, place in ((0, 69999, 63), (65, 3, 0), (66, 3, 1), (67, 69998, 3), (69, 69998, 4)):
+        assert torch.equal(c.data[0, page, :, place], k[t]) and torch.equal(c.data[1, page, :, place], v[t])
+    assert c.table.tolist() == [[69999, 3, -1, -1], [2, 69998, -1, -1]] and int(c.refs[69000]) == 0
+
+
+def test_append_and_accept_off_the_current_stream(P):
+    rng = np.random.default_rng(5)
+    s = Sequences(P, [300, 40], [20, 9], 8, 2, 64, 16, torch.bfloat16, seed=13, garbage=0.25)
+    k, v = (torch.randn((29, 2, 64), generator=gen(i), device="cuda").to(torch.bfloat16) for i in (1, 2))
+    f = torch.rand(32, generator=gen(3), device="cuda")
+    up, token, pick = (ints(x) for x in (forest(rng, 20) + forest(rng, 9), rng.integers(0, 3, 29), rng.integers(0, 3, 29)))
+    c = s.cache
+    kept = [x.clone() for x in (c.data, c.table, c.length)]
+
+    def step(**kw):
+        return [c.append(0, s.q, k, v, f, offsets=s.offsets, **kw), *c.accept(token, pick, up, offsets=s.offsets, **kw)]
+    want = step() + [x.clone() for x in (c.data, c.table, c.length)]
+    for x, y in zip((c.data, c.table, c.length), kept):
+        x.copy_(y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(stream=side) + [c.data, c.table, c.length]
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
 # ------------------------------------------------------------------- top -------
 
 def check_top(P, x, k):
