@@ -682,10 +682,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 // beside this half's exponentials.  4,096 tokens over 16,384 keys, 32 heads of 128: 905 to 980 us
 // by the card, not traced, 16 of k_join among them, 0.98 to 1.06 PFLOP/s (a bf16 product of 8,192^3 by the library: 1.23), the matrix units
 // busy in 47 cycles of 100 at the 2.1 GHz that the power leaves.  Where K and V's bytes bound it a unit takes 2.1
-// us, 4 TB/s (32 trees of up to 32 tokens over 158,700, kSeen: 658 MB in 139 to 147 us, 4.5 to 4.7 TB/s).
+// us, 4 TB/s (32 trees of up to 32 tokens over 158,700, kSeen: 658 MB in 135 to 147 us, 4.5 to 4.9 TB/s, with one block to a CU; two to four
+// units of each on their way in registers: 138 to 144).
 // In heads of up to 64 the exponentials and sums, not the products, keep the issue busy (53 cycles of 100, the matrix units 30), and a
 // second wave beside the first fills its gaps: 256 rows in eight waves of 32 (kSeen; four trees of up to 250 tokens over 116,700, 56
-// GFLOP: 94 us, in four waves of 64 108, in two blocks of 128 rows 100, whose join takes 5 more).
+// GFLOP: 92 us, in four waves of 64 108, in two blocks of 128 rows 100, whose join takes 5 more).
 constexpr int kWideKeys = 64;
 
 // What is not finite in V of the keys from .. to - 1, added to the sums or outputs that this lane has written (lanes and rows as
@@ -1235,15 +1236,15 @@ Shape shape_of(const tam_chunk &c, int64_t heads, bool seen) {
     const int64_t longest = c.longest ? std::min(c.longest, c.tokens) : c.tokens;
     const int64_t rows = longest * (heads / c.kv_heads);
     if (rows <= 16) return Shape{16, kNarrowKeys, 512, kNarrowKeys};
-    // One request's small tree over a short text: tiles of 16 rows begin sooner, and K and V read up to four times come from the caches
-    // (us per call in a graph, 16 tokens of 32 and 8 heads of 128 over 300, 700, 1,500, 3,000 and 12,000: 13.3, 14.8, 18.7, 21.0 and
-    // 34.0; in a tile of 128 rows 16.2, 17.5, 19.8, 22.0 and 29.5; four requests, 700 and 3,000: 22.0 and 41.6; 22.8 and 29.0).
-    const int64_t bytes = 4 * c.max_pages * c.page_tokens * c.kv_heads * c.head_dim;
-    if (seen && c.rows == 1 && rows <= 64 && bytes <= 16 << 20) return Shape{16, kNarrowKeys, 512, kNarrowKeys};
     // a batch of mostly short rows fills tiles of 128 rows better (us per call with 128 and 256: 40 chunks of up to
     // 200 tokens, 74 rows on average, 50 and 63; 24 of 265 rows on average, heads of 64, 46 and 41)
-    if (rows <= 128 || c.tokens * (heads / c.kv_heads) <= 128 * c.rows) return Shape{128, kWideKeys, 512, 2 * kWideKeys};
-    return Shape{256, kWideKeys, 256, 5 * kWideKeys};
+    // With a mask one block to a CU: half the cuts, whose sums cost more than a second block's loads bring (us per call in a graph
+    // with 256 blocks and 512, 16 tokens of 32 and 8 heads of 128 over 700, 3,000 and 12,000, one request: 15.2, 17.7 and 23.2; 17.5, 20.4
+    // and 29.5; four: 18.8, 24.4 and 45.4; 22.8, 29.6 and 52.9; 16: 24.1, 46.5 and 175; 26.4, 51.2 and 181); and a tile's own cost is
+    // higher.  (In tiles of 16 rows, which read K and V four times, one request takes 14.7, 20.7 and 34.)
+    const bool small = rows <= 128 || c.tokens * (heads / c.kv_heads) <= 128 * c.rows;
+    if (seen) return small ? Shape{128, kWideKeys, 256, 4 * kWideKeys} : Shape{256, kWideKeys, 256, 8 * kWideKeys};
+    return small ? Shape{128, kWideKeys, 512, 2 * kWideKeys} : Shape{256, kWideKeys, 256, 5 * kWideKeys};
 }
 
 int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
