@@ -6,7 +6,8 @@
 //
 // k_top: a block holds a span of a row in registers, read once.  Each thread finds its maximum and its sum; the k-th largest of
 // the maxima of 64 or 256 groups of threads (found by one wave, which cuts the range of values) leaves few more than k
-// candidates, which go to LDS and are ranked by counting.  Where equal logits leave too many, the k-th key itself is found.
+// candidates, which go to LDS and are ranked by counting.  Where thousands equal the bound, the first tokens of them are counted
+// off (rows of zeros: 92 us for 33); where thousands are above it, the k-th key itself is found, in a turn through the span per bit.
 // k_top_join: the spans' best, in the same way, and the sum of the sums.
 // The bytes bound a large call, with the exponentials (a quarter of the rate) close behind: 256 bf16 rows over V = 262,144, 8 of
 // each, 134 MB in 29 to 30.5 us (4.4 to 4.6 TB/s), 24 without looking for the best; the join 4 to 5.  A row of 32,000 is a chain of barriers in
@@ -108,6 +109,30 @@ __device__ inline int count_block(int mine) {
     return all;
 }
 
+// Sum over the threads before this one, and over all of them.
+template <int kThreads>
+__device__ inline int before_block(int mine, int *total) {
+    constexpr int kWaves = kThreads / kWave;
+    __shared__ int waves[kWaves];
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int up = __shfl_up(upto, d);
+        if ((int)threadIdx.x % kWave >= d) upto += up;
+    }
+    __syncthreads();
+    if (threadIdx.x % kWave == kWave - 1) waves[threadIdx.x / kWave] = upto;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < (int)threadIdx.x / kWave) upto += waves[w];
+        all += waves[w];
+    }
+    *total = all;
+    return upto - mine;
+}
+
 // The k-th largest of the lanes' kPer values each, or a value under it that few more reach (kReach(k) at most where all are
 // different); `low` if no more reach that.  X: an unsigned integer.  The range is cut into four in each turn: three counts side by
 // side take hardly longer than one.
@@ -197,8 +222,8 @@ __device__ inline void rank(const uint64_t *found, int n, int k, F put) {
     for (int i = n + threadIdx.x; i < k; i += kThreads) put(i, 0);
 }
 
-// The candidates where there are too many, or a NaN: the order of the k-th key by halving, then how far in the tokens the keys
-// of that order go.  The logits are read again in each turn, so that nothing of this takes registers from the usual way.
+// The candidates where there are too many and k or more of them above the bound: the order of the k-th key by halving, then how far in the tokens the keys of that order go.  The logits are read again in each turn, so that nothing of this
+// takes registers from the usual way.
 template <int kThreads, typename T>
 __device__ __attribute__((noinline)) int collect_exactly(const T *row, int64_t from, int64_t to, int k, uint64_t *found, int32_t *count) {
     auto counted = [&](auto is) {
@@ -288,26 +313,66 @@ __global__ void __launch_bounds__(kThreads) k_top(const T *__restrict__ logits, 
     }
     if (sum.s != sum.s) sum.m = -INFINITY;
     sum = join_block<kThreads>(sum);
-    int n = INT_MAX;
     fresh();
-    if (sum.s == sum.s) {
-        const float low = logit_of(near_kth<kThreads, uint32_t>(order_of(most), a.k, kNone + 1));
+    // (comparisons that a NaN passes, as it is above all)
+    const float low = logit_of(near_kth<kThreads, uint32_t>(order_of(most), a.k, kNone + 1));
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            if (high[i] >= low) {
+    for (int i = 0; i < kVecs; ++i) {
+        if (!(high[i] < low)) {
 #pragma unroll
-                for (int c = 0; c < N; ++c) {
-                    const float y = I::get(x[i], c);
-                    if (y >= low) {
-                        const int at = atomicAdd(&count, 1);
-                        if (at < kCandidates) found[at] = key_of(y, (uint32_t)((j0 + i * kThreads) * N - skip + c));
-                    }
+            for (int c = 0; c < N; ++c) {
+                const float y = I::get(x[i], c);
+                if (!(y < low)) {
+                    const int at = atomicAdd(&count, 1);
+                    if (at < kCandidates) found[at] = key_of(y, (uint32_t)((j0 + i * kThreads) * N - skip + c));
                 }
             }
         }
-        __syncthreads();
-        n = count;
-        __syncthreads();
+    }
+    __syncthreads();
+    int n = count;
+    __syncthreads();
+    if (n > kCandidates) {
+        // equal logits: with fewer than k above `low` that is the k-th, and of those that equal it the first tokens are taken, a
+        // vector of each thread after the other
+        fresh();
+        int above = 0;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+            if (!(high[i] <= low)) {
+#pragma unroll
+                for (int c = 0; c < N; ++c) above += !(I::get(x[i], c) <= low);
+            }
+        above = count_block<kThreads>(above);
+        if (above < a.k) {
+            if (threadIdx.x == 0) count = 0;
+            __syncthreads();
+            auto take = [&](int i, int c) { found[atomicAdd(&count, 1)] = key_of(I::get(x[i], c), (uint32_t)((j0 + i * kThreads) * N - skip + c)); };
+            int need = a.k - above;
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                asm volatile("" : "+v"(x[i]));
+                if (!(high[i] <= low)) {
+#pragma unroll
+                    for (int c = 0; c < N; ++c)
+                        if (!(I::get(x[i], c) <= low)) take(i, c);
+                }
+                if (need > 0) {
+                    int equal = 0, all;
+#pragma unroll
+                    for (int c = 0; c < N; ++c) equal += I::get(x[i], c) == low;
+                    int before = before_block<kThreads>(equal, &all);
+                    if (equal && before < need) {
+#pragma unroll
+                        for (int c = 0; c < N; ++c)
+                            if (I::get(x[i], c) == low && before++ < need) take(i, c);
+                    }
+                    need -= all;
+                }
+            }
+            __syncthreads();
+            n = count;
+        }
     }
     if (n > kCandidates) {
         const int64_t begin = (int64_t)part * kThreads * kVecs * N - skip, end = begin + kThreads * kVecs * N;

@@ -725,6 +725,24 @@ def test_top_of_wide_rows_and_many(P, dtype):
         P.top_tokens(torch.zeros((1, 2 ** 21 + 1), dtype=dtype, device="cuda"), 1)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [900, 32000, 262144])
+def test_top_many_nan(P, dtype, V):
+    """NaN of both signs, few and by the thousand: first, the lowest token first, and the numbers behind them."""
+    for share in (3 / V, 0.01, 1.0):
+        x = torch.randn((4, V), generator=gen(V), device="cuda").to(dtype)
+        at = torch.rand((4, V), generator=gen(V + 1), device="cuda") < share
+        at[:, 7] = True
+        x[at] = math.nan
+        bits = x.view(torch.int32 if dtype is torch.float32 else torch.int16)
+        bits[:, 1::2] = torch.where(at[:, 1::2], torch.full_like(bits[:, 1::2], -1), bits[:, 1::2])
+        for k in (1, 5, 64):
+            tokens, logprobs, lse = P.top_tokens(x, k, return_lse=True)
+            y = torch.where(at, math.inf, x.double())
+            want = torch.sort(y, dim=1, descending=True, stable=True).indices[:, :k]
+            assert torch.equal(tokens.long(), want) and lse.isnan().all() and logprobs.isnan().all()
+
+
 def test_top_of_a_view_and_empty(P):
     x = torch.randn((6, 5003), generator=gen(6), device="cuda")
     check_top(P, x[1:2, 3:], 7)
