@@ -440,8 +440,8 @@ struct Split {
 // 4.8, 1,024: 66 and 5), with as many vectors each as leave the chip 2,048 blocks; more threads only where a row would have more
 // parts than k_top_join holds.  Short rows, no more than there are CUs, take a block each, which leaves the second launch out (us
 // per call of 1, 64, 256 and 512 fp32 rows over V = 32,000, 4 of each: 8.1, 9.1, 11.9 and 22.9, in parts 8.1, 10.2, 15.2 and 21.5, and
-// 3 less on the host; 64 of each: 10.2, 11.5, 13.9 and 26.7, in parts 14.9, 17.3, 24.1 and 31.9; bf16 rows over V = 128,256, 24 of each,
-// 8 and 256: 16 and 21.3, in parts 14.4 and 29).
+// 3 less on the host; 64 of each: 10.2, 11.5, 13.9 and 26.7, in parts 14.9, 17.3, 24.1 and 31.9).  Twice as long ones do not
+// fit a block's registers: 256 bf16 rows over V = 128,256 27, in parts 22.
 template <typename T>
 Split split_of(int64_t B, int64_t V) {
     const int64_t vectors = (V + 2 * In<T>::n - 2) / In<T>::n;
@@ -449,7 +449,7 @@ Split split_of(int64_t B, int64_t V) {
     auto parts = [&] { return (int)((vectors + s.threads * s.vecs - 1) / (s.threads * s.vecs)); };
     while (s.vecs < 16 && (B * parts() > 2048 || parts() > 128)) s.vecs *= 2;
     if (parts() > 128) s.threads = 512;
-    if (B <= 256 && vectors <= (B < 128 ? 8192 : 16384)) s.vecs = vectors <= 4096 ? 4 : vectors <= 8192 ? 8 : 16, s.threads = 1024;
+    if (B <= 256 && vectors <= 8192) s.vecs = vectors <= 4096 ? 4 : 8, s.threads = 1024;
     s.parts = parts();
     return s;
 }
@@ -457,7 +457,7 @@ Split split_of(int64_t B, int64_t V) {
 template <typename T>
 hipError_t launch(const void *logits, int64_t B, Top a, const Split &sp, hipStream_t s) {
     void (*kernel)(const T *, Top) = sp.threads == 512    ? k_top<T, 16, 512>
-                                     : sp.threads == 1024 ? (sp.vecs == 4 ? k_top<T, 4, 1024> : sp.vecs == 8 ? k_top<T, 8, 1024> : k_top<T, 16, 1024>)
+                                     : sp.threads == 1024 ? (sp.vecs == 4 ? k_top<T, 4, 1024> : k_top<T, 8, 1024>)
                                      : sp.vecs == 4      ? k_top<T, 4, 256>
                                      : sp.vecs == 8      ? k_top<T, 8, 256>
                                                        : k_top<T, 16, 256>;
