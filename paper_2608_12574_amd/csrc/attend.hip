@@ -82,8 +82,8 @@ __device__ inline int64_t uniform(int64_t x) {
 }
 
 // x, of which the compiler knows nothing from here on: what is computed from it is computed where it is used. Else all that
-// does not change from tile to tile is computed before the first one, and waits in registers that have no room for it (a microsecond
-// and 60 spilled values, where a block has a single tile).
+// does not change from tile to tile is computed before the first one, and waits in registers (one request's 16 tokens over 700, 32/8
+// heads of 128: 10.1 us with it and 10.9 without, medians of eight; four of up to 250 over 116,700, 16/2 heads of 64: 91.5 and 91.0).
 __device__ inline int32_t here(int32_t x) {
     asm volatile("" : "+v"(x));
     return x;
