@@ -403,7 +403,7 @@ class PageCache:
         return out
 
     def attend(self, layer, q, offsets=None, slots=None, longest=None, scale=None, out=None, return_lse=False,
-               seen=None, stream=None):
+               stream=None, seen=None):
         """Attention of the new tokens' queries ``q`` [tokens, heads, head_dim] over their sequences, each over the
         tokens up to its own; ``heads`` is a multiple of ``kv_heads``.  Rows as for ``store``, whose tokens
         have been stored.  ``scale``: of the products (1 / sqrt(head_dim)).  ``longest``: the tokens of the longest

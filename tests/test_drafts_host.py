@@ -174,6 +174,15 @@ def test_arguments_of_the_cache(P, fake):
             call(fake(1))
 
 
+def test_attend_takes_its_stream_by_place(P, two_gpus):
+    """The mask came after the other arguments: calls that give them by place are what they were."""
+    c, on = two_gpus(0), []
+    c._lib.tam_attend = lambda *a: on.append(a[-1]) or 0
+    q = On(torch.zeros((3, 1, 8), dtype=torch.bfloat16), 0)
+    c.attend(0, q, None, None, None, None, On(torch.zeros((3, 1, 8), dtype=torch.bfloat16), 0), False, SimpleNamespace(cuda_stream=77, device_index=0))
+    assert on == [77]
+
+
 def test_arguments_of_the_functions(P, fake):
     ints = lambda n, gpu=0: On(torch.zeros(n, dtype=torch.int32), gpu)
     x = lambda *shape, gpu=0, dtype=torch.float32: On(torch.zeros(shape, dtype=dtype), gpu)
