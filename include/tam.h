@@ -716,7 +716,7 @@ tam_status tam_attend_seen(const tam_chunk *c, const void *q, int64_t q_token, i
  * token's.  K and V of those that stay move, in every plane, to the places after the text before the row in the order
  * of their depth; the slot ends behind them, and pages past its end are given back (their table entries become -1).
  *   c, n     the cache, and the new tokens of the call: n names c's tables, and its strides, kv_heads, head_dim and dtype
- *            say where a vector lies in a page; k and v are not read.
+ *            say where a vector lies in a page; k and v are not looked at.
  *   tokens, picks, parents  device int32[n->tokens]: the drafted tokens, the model's choice after each, their parents.
  *   path     device int32[n->tokens]: the numbers, in the row, of its tokens that stay, then -1 (tokens of no row are
  *            not written).

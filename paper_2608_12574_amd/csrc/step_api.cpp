@@ -76,7 +76,8 @@ const char *rows_wrong(const tam_pages *c, int64_t n) {
     return nullptr;
 }
 
-const char *chunk_wrong(const tam_chunk *c) {
+// `plane`: the call reads or writes k and v
+const char *chunk_wrong(const tam_chunk *c, bool plane = true) {
     if (!c) return "null chunk";
     if (const char *w = tables_wrong(c->table, c->length, c->slots, c->max_pages, c->table_stride, c->num_pages,
                                      c->page_tokens))
@@ -88,8 +89,8 @@ const char *chunk_wrong(const tam_chunk *c) {
         return "rows and tokens must be in 0 .. 2^31 - 2";
     if (!c->slot_ids && c->rows > c->slots) return "rows must be <= slots without slot_ids";
     if (c->longest < 0) return "longest must be >= 0";
-    if (!c->k || !c->v) return "null k or v";
-    if (!aligned(c->k, 16) || !aligned(c->v, 16) || c->page_stride % 8 || c->head_stride % 8 || c->token_stride % 8)
+    if (plane && (!c->k || !c->v)) return "null k or v";
+    if ((plane && (!aligned(c->k, 16) || !aligned(c->v, 16))) || c->page_stride % 8 || c->head_stride % 8 || c->token_stride % 8)
         return "k and v must be 16-byte aligned and their strides multiples of 8";
     if (c->page_stride < 0 || c->head_stride < 0 || c->token_stride < 0) return "strides must be >= 0";
     if (!aligned(c->offsets, 4) || !aligned(c->slot_ids, 4)) return "offsets and slot_ids must be 4-byte aligned";
@@ -261,7 +262,7 @@ tam_status tam_pages_append(const tam_chunk *c, const tam_rotation *r, const voi
 
 int64_t tam_pages_accept_work(const tam_chunk *n) {
     tam::api_begin();
-    if (const char *w = chunk_wrong(n)) return api_fail(TAM_E_INVAL, w), -1;
+    if (const char *w = chunk_wrong(n, false)) return api_fail(TAM_E_INVAL, w), -1;
     return tam::accept_work_bytes(*n);
 }
 
@@ -269,7 +270,7 @@ tam_status tam_pages_accept(const tam_pages *c, const tam_chunk *n, const int32_
                             const int32_t *parents, int32_t *path, int32_t *count, int32_t *last, void *work, void *stream) {
     tam::api_begin();
     const char *w = pages_wrong(c);
-    if (!w) w = chunk_wrong(n);
+    if (!w) w = chunk_wrong(n, false);
     if (!w && (n->table != c->table || n->length != c->length || n->slots != c->slots || n->max_pages != c->max_pages ||
                n->table_stride != c->table_stride || n->num_pages != c->num_pages || n->page_tokens != c->page_tokens))
         w = "the chunk's tables are not the cache's";

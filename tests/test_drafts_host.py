@@ -96,6 +96,20 @@ def test_accept_refusals(P):
     refused(L, L.tam_pages_accept_work(ctypes.byref(chunk(P, tokens=-1))), "tokens")
 
 
+def test_accept_does_not_look_at_k_and_v(P):
+    """The vectors lie in the cache's planes: the chunk's own k and v may be anything."""
+    L = P.lib()
+    page = 4 * 16 * 64 * 2
+    pages = P.tam.Pages(AT, 4, 10 * page, page, page, 10, 16, AT, 3, 5, 5, AT, AT)
+    for at in (None, AT + 2):
+        c = chunk(P)
+        c.k = c.v = at
+        assert L.tam_pages_accept_work(ctypes.byref(c)) >= 7 * 16 + 3 * 4
+        c.rows = 0
+        assert L.tam_pages_accept(ctypes.byref(pages), ctypes.byref(c), AT, AT, AT, AT, AT, AT, AT, None) == 0
+        refused(L, L.tam_attend_work(ctypes.byref(c), 8), "k")
+
+
 def test_top_tokens_refusals(P):
     L = P.lib()
     good = dict(logits=AT, dtype=P.DTYPE_BF16, B=4, V=100000, stride=100000, k=8, tokens=AT, logprobs=AT, lse=AT, work=AT)
