@@ -691,6 +691,7 @@ typedef struct {
  * tam_pages_append -- tam_pages_store of the new tokens with K turned by their positions, and their queries turned alike:
  * out[t][h] of q[t][h].  Angles of up to 10^8 radians are taken modulo whole turns to fp32's last place; elements are
  * turned in fp32 and rounded once.  The tokens' places do not depend on `depth`.
+ *   c              fewer than 2^24 tokens.
  *   k_new, v_new   as for tam_pages_store; the tokens that are left out there are here too.
  *   q, heads, out  as for tam_attend (any number of heads); heads == 0: no queries.  Every token of a row is written; `out` may be
  *                  `q` itself, with its strides.

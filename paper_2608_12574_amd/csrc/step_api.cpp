@@ -22,6 +22,9 @@ using tam::api_fail;
 bool power_of_two(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
 bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
+// A launch has fewer than 2^32 threads along an axis: blocks of 256.
+constexpr int64_t kMostBlocks = (1 << 24) - 1;
+
 struct Axis {
     int64_t count, stride;
 };
@@ -240,6 +243,7 @@ tam_status tam_pages_append(const tam_chunk *c, const tam_rotation *r, const voi
                             int64_t heads, void *out, int64_t out_token, int64_t out_head, void *stream) {
     tam::api_begin();
     const char *w = store_wrong(c, k_new, k_token, k_head, v_new, v_token, v_head);
+    if (!w && c->tokens > kMostBlocks) w = "tokens must be below 2^24";
     if (!w && !r) w = "null rotation";
     if (!w && (r->pairs < 0 || r->pairs > c->head_dim / 2 || r->pairs % 4)) w = "pairs must be a multiple of 4, at most head_dim / 2";
     if (!w && r->adjacent != 0 && r->adjacent != 1) w = "adjacent must be 0 or 1";

@@ -54,6 +54,19 @@ def test_append_refusals(P):
     assert call(c=chunk(P, tokens=0)) == 0 and call(c=chunk(P, tokens=0), heads=0, q=None, out=None, out_token=0, frequencies=None, pairs=0) == 0
 
 
+def test_append_refuses_more_tokens_than_blocks(P):
+    L = P.lib()
+    turn = P.tam.Rotation(AT, 32, 0, None)
+
+    def call(tokens, heads, q):
+        c = chunk(P, tokens=tokens)
+        return L.tam_pages_append(ctypes.byref(c), ctypes.byref(turn), AT, 256, 64, AT, 256, 64, q, 512, 64, heads, q, 512, 64, None)
+    for tokens in (2 ** 24, 2 ** 24 + 7, 2 ** 31 - 2):
+        refused(L, call(tokens, 8, AT), "2^24")
+        refused(L, call(tokens, 0, None), "2^24")
+    refused(L, call(2 ** 24 - 1, 8, None), "null")  # as many are looked at further
+
+
 def test_attend_seen_refusals(P):
     L = P.lib()
     good = dict(q=AT, q_token=512, q_head=64, heads=8, scale=0.1, seen=AT, words=2, stride=2, out=AT, out_token=512, out_head=64, lse=None,
