@@ -724,7 +724,7 @@ tam_status tam_attend_seen(const tam_chunk *c, const void *q, int64_t q_token, i
  *   count    device int32[n->rows]: how many stay (0 for a row without tokens or outside the slots, which changes nothing).
  *   last     device int32[n->rows]: the choice after the last of them (-1 if none): the next token of the text.
  *   work     tam_pages_accept_work(n) bytes.
- * The slots of the rows are distinct, and the pages of the rows' tokens their own (as tam_pages_extend leaves them).
+ * n has fewer than 2^24 rows.  The slots of the rows are distinct, and the pages of the rows' tokens their own (as tam_pages_extend leaves them).
  * Tokens without a place (tam_pages_store) do not move.  Errors: TAM_E_INVAL, TAM_E_DEVICE.
  */
 tam_status tam_pages_accept(const tam_pages *c, const tam_chunk *n, const int32_t *tokens, const int32_t *picks,

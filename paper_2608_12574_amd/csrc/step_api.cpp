@@ -279,6 +279,7 @@ tam_status tam_pages_accept(const tam_pages *c, const tam_chunk *n, const int32_
                n->table_stride != c->table_stride || n->num_pages != c->num_pages || n->page_tokens != c->page_tokens))
         w = "the chunk's tables are not the cache's";
     if (!w && n->rows > c->slots) w = "rows must be <= slots";
+    if (!w && n->rows > kMostBlocks) w = "rows must be below 2^24";
     if (!w && !apart<2>(n->head_dim, {{{n->kv_heads, n->head_stride}, {n->page_tokens, n->token_stride}}})) w = "a page's vectors overlap";
     if (!w && c->planes > 0) {
         // (strides of 2^62 and more would wrap below; a page cannot be that large)

@@ -225,6 +225,7 @@ hipError_t launch_tree_masks(const int32_t *parents, const int32_t *offsets, int
 // less.  us on the device per call of 1 and 128 trees of 32 tokens, 4 layers: 2.6 and 7.0, in two launches 3.9 and 7.4; 8 layers:
 // 5.3 and 10.4, 5.5 and 9.4; 16 layers: 7.3 and 13.5, 5.8 and 11.5.
 constexpr int64_t kBothItems = 2048;
+constexpr int64_t kBothRows = ((1ll << 32) - 1) / kBothThreads;  // a launch has fewer than 2^32 threads
 
 // places from and to of each token, and each row's first move
 int64_t accept_work_bytes(const tam_chunk &n) { return 16 * n.tokens + 4 * n.rows; }
@@ -239,7 +240,7 @@ hipError_t launch_pages_accept(const tam_pages &c, const tam_chunk &n, const int
     const int64_t pieces = n.head_dim / 8, items = c.planes * n.kv_heads * pieces;
     const Shift m{static_cast<uint8_t *>(c.data), c.plane_stride, 2 * n.head_stride, n.offsets, count, first, src, dst, n.tokens,
                   (int32_t)n.kv_heads, (int32_t)pieces, items};
-    if (items <= kBothItems) {
+    if (items <= kBothItems && n.rows <= kBothRows) {
         hipLaunchKernelGGL(k_walk_shift, dim3((unsigned)n.rows), dim3(kBothThreads), 0, s, a, m);
         return hipGetLastError();
     }

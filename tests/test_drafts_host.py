@@ -123,6 +123,20 @@ def test_accept_does_not_look_at_k_and_v(P):
         refused(L, L.tam_attend_work(ctypes.byref(c), 8), "k")
 
 
+def test_accept_refuses_more_rows_than_blocks(P):
+    L = P.lib()
+    page = 4 * 16 * 64 * 2
+
+    def call(rows, path):
+        pages = P.tam.Pages(AT, 4, 10 * page, page, page, 10, 16, AT, 2 ** 30, 5, 5, AT, AT)
+        c = chunk(P)
+        c.slots, c.rows = 2 ** 30, rows
+        return L.tam_pages_accept(ctypes.byref(pages), ctypes.byref(c), AT, AT, AT, path, AT, AT, AT, None)
+    for rows in (2 ** 24, 2 ** 30):
+        refused(L, call(rows, AT), "2^24")
+    refused(L, call(2 ** 24 - 1, None), "null")  # as many are looked at further
+
+
 def test_top_tokens_refusals(P):
     L = P.lib()
     good = dict(logits=AT, dtype=P.DTYPE_BF16, B=4, V=100000, stride=100000, k=8, tokens=AT, logprobs=AT, lse=AT, work=AT)

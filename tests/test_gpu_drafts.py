@@ -579,6 +579,38 @@ def test_accept_places_that_are_not_there(P):
     assert c.length.tolist() == [2, 11, 11] and c.table.tolist() == [[0, 1, 2], [3, 99, 4], [5, 6, 7]]
 
 
+def test_accept_of_millions_of_rows(P):
+    """More rows than blocks of 1,024 threads in a launch, one token each and some in trees of three."""
+    rows = 2 ** 22 + 3
+    c = P.PageCache.empty(1, 1, 8, rows, rows, 1, page_tokens=4)
+    page = torch.randperm(rows, generator=gen(0), device="cuda")
+    c.data.copy_(torch.randn(c.data.shape, generator=gen(1), device="cuda"))
+    c.table[:, 0] = page
+    c.refs.fill_(1)
+    n = torch.ones(rows, dtype=torch.int64, device="cuda")
+    trees = torch.tensor([0, 1234567, rows - 1], device="cuda")
+    n[trees] = 3
+    c.length.copy_(n)
+    off = torch.zeros(rows + 1, dtype=torch.int64, device="cuda")
+    off[1:] = n.cumsum(0)
+    first = off[:-1]
+    tokens, picks, up = (torch.full((rows + 6,), x, dtype=torch.int32, device="cuda") for x in (5, 6, -1))
+    for j, (token, pick, parent) in enumerate(((5, 8, -1), (7, 1, 0), (8, 9, 0))):  # the root's choice is token 2
+        for x, y in zip((tokens, picks, up), (token, pick, parent)):
+            x[first[trees] + j] = y
+    want = c.data.clone()
+    want[:, page[trees], :, 1] = c.data[:, page[trees], :, 2]
+    path, count, last = c.accept(tokens, picks, up, offsets=off.int())
+    assert torch.equal(c.data, want)
+    in_tree = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    in_tree[trees] = True
+    assert torch.equal(count, torch.where(in_tree, 2, 1).int()) and torch.equal(last, torch.where(in_tree, 9, 6).int())
+    assert torch.equal(c.length, count) and torch.equal(c.table[:, 0].long(), page) and bool((c.refs == 1).all())
+    want = torch.zeros_like(path)
+    want[first[trees] + 1], want[first[trees] + 2] = 2, -1
+    assert torch.equal(path, want)
+
+
 def test_append_and_accept_past_32_bits(P):
     """Pages past 2^31 elements of a plane, and a move from one to another."""
     c = P.PageCache.empty(1, 8, 128, 70000, 2, 4, page_tokens=64)
