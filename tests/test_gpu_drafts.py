@@ -538,6 +538,53 @@ def test_accept_layouts_and_slots(P, kv, dim, layers):
     check_accept(P, rng, [12, 50], [20, 5], 16, kv=kv, dim=dim, layers=layers, slots=[-1, 0], bushy=0.1, likely=0.95)
 
 
+@pytest.mark.parametrize("kv,dim,layers", [(8, 128, 9), (7, 120, 15), (136, 128, 64)])
+def test_accept_of_many_layers(P, kv, dim, layers):
+    """Caches whose walk and moves are launches of their own, from 2,049 pieces of 16 bytes per token on: in whole blocks of 256,
+    with a last one that is not full, and more than 1,024 blocks, so that a thread takes several.  Of a row's tokens every
+    second one stays (0, 2, 4, ..., the others are leaves), or all of them."""
+    pieces = 2 * layers * kv * dim // 8
+    assert pieces in (9 * 256, 3150) or pieces > 1024 * 256
+    page = 8 if layers < 64 else 2
+    rows = [(150, 5, 2), (0, 7, 2), (9, 0, 1), (1, 3, 2), (33, 12, 2)] if layers < 64 else [(17, 3, 2), (2, 0, 2), (5, 1, 1)]
+    slots = [3, 0, 5, 1, 2] if layers < 64 else [2, 0, 1]
+    c = P.PageCache.empty(layers, kv, dim, sum(-(-(n + b) // page) for n, b, _ in rows) + 1, 6, 20, page_tokens=page)
+    for plane in c.data:
+        plane.copy_(torch.randn(plane.shape, generator=gen(0), device="cuda"))
+    ids = np.random.default_rng(layers).permutation(c.data.shape[1])
+    table, length, refs, at = np.full((6, 20), -1, np.int32), np.zeros(6, np.int32), np.zeros(len(ids), np.int32), 0
+    for s, (n, b, _) in zip(slots, rows):
+        length[s] = n + b
+        held = -(-(n + b) // page)
+        table[s, :held] = ids[at:at + held]
+        refs[ids[at:at + held]] = 1
+        at += held
+    c.table.copy_(ints(table))
+    c.length.copy_(ints(length))
+    c.refs.copy_(ints(refs))
+    want, tokens, picks, up, path, count, last = c.data.clone(), [], [], [], [], [], []
+    for s, (n, b, each) in zip(slots, rows):
+        stay = list(range(0, n, each))
+        up += [-1 if j == 0 else j - 1 - (j - 1) % each for j in range(n)]
+        tokens += list(range(n))
+        picks += [j + each if j % each == 0 else 3 for j in range(n)]
+        path += stay + [-1] * (n - len(stay))
+        count.append(len(stay))
+        last.append(stay[-1] + each if n else -1)
+        for d, j in enumerate(stay):
+            want[:, table[s, (b + d) // page], :, (b + d) % page] = c.data[:, table[s, (b + j) // page], :, (b + j) % page]
+        if n:
+            length[s] = b + len(stay)
+            for x in table[s, -(-length[s] // page):]:
+                refs[x] -= x >= 0
+            table[s, -(-length[s] // page):] = -1
+    off = ints(np.concatenate([[0], np.cumsum([n for n, _, _ in rows])]).astype(np.int32))
+    got = c.accept(ints(tokens), ints(picks), ints(up), offsets=off, slots=ints(slots))
+    assert got[0].tolist() == path and got[1].tolist() == count and got[2].tolist() == last
+    assert c.table.tolist() == table.tolist() and c.length.tolist() == length.tolist() and c.refs.tolist() == refs.tolist()
+    assert torch.equal(c.data.view(torch.int16), want.view(torch.int16))
+
+
 def test_accept_whole_chains_and_none(P):
     """A chain that stays whole moves nothing; a path longer than a wave; a root whose choice was not drafted."""
     c = P.PageCache.empty(1, 1, 8, 60, 3, 20, page_tokens=8)
