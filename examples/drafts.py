@@ -55,14 +55,14 @@ def shape(levels):
 
 
 def generate(model, handle, prior, prompts, levels=(4, 2, 1), most=32, page_tokens=16):
-    """The greedy continuation of each prompt, and the steps that it took: (tokens, steps).  ``prior`` [V]: what is drafted
-    first; no ``levels``: one token per step."""
+    """The greedy continuation of each prompt, the steps that it took and the cache: (tokens, steps, cache).  ``prior`` [V]: what is
+    drafted first; no ``levels``: one token per step; ``most``: steps at most, each of which adds up to len(levels) + 1 tokens."""
     B, V = len(prompts), len(prior)
     int32 = dict(dtype=torch.int32, device="cuda")
     begin = [len(p) for p in prompts]
     parents = shape(levels)
     n = len(parents)
-    held = -(-(max(begin) + most + n) // page_tokens)
+    held = -(-(max(begin) + most * (len(levels) + 1) + n) // page_tokens)  # what stays, and a tree behind it
     cache = tam.PageCache.empty(len(model.layers), model.kv_heads, model.head_dim, pages=B * held, slots=B, max_pages=held,
                                 page_tokens=page_tokens)
     slots = torch.arange(B, **int32)

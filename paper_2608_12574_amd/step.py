@@ -298,8 +298,8 @@ class PageCache:
     def extend(self, slots, counts, stream=None):
         """Room for ``counts[i]`` more tokens in slot ``slots[i]``, for all of them or for none;
         a shared, partly filled last page is copied first.  Returns int32 [4] on the GPU: 1 if done
-        (else 0, and nothing has changed), pages needed, pages that were free, slots that
-        ``max_pages`` is too small for."""
+        (else 0, and nothing has changed: ``store``, ``append``, ``attend`` and ``accept`` would take the sequences' last tokens
+        for the new ones), pages needed, pages that were free, slots that ``max_pages`` is too small for."""
         where = "tam_pages_extend"
         n, gpu, on = slots.numel(), self._gpu, self._on(where, stream)
         s, c = _int32(where, "slots", slots, n, gpu), _int32(where, "counts", counts, n, gpu)

@@ -955,3 +955,22 @@ def test_drafts_example(P, levels):
             assert row[0, t] >= row.max() - 2 * 0.064
             node = h.advance(node, ints([t]))
     h.close()
+
+
+@pytest.mark.parametrize("levels,most", [((4, 2, 1), 32), ((1, 1, 1, 1, 1), 20), ((), 110)])
+def test_drafts_example_of_long_strings(P, monkeypatch, levels, most):
+    """Strings as long as the steps allow: the cache has room for every tree, and the tokens of each."""
+    import examples.drafts as E
+    made = []
+    monkeypatch.setattr(P.PageCache, "extend", lambda c, *a, real=P.PageCache.extend, **kw: made.append(real(c, *a, **kw)) or made[-1])
+    vocab = E.beams.vocabulary()
+    strings = [bytes(65 + (i * i + k * (i > 90)) % 26 for i in range(107)) for k in (0, 1)]
+    h = P.compile(strings, vocab, device="cuda:0")
+    prior = torch.ones(len(vocab), device="cuda")
+    prompts = [list(b"short"), list(b"a prompt that is longer than a page")]
+    found, steps, cache = E.generate(E.Decoder(len(vocab)), h, prior, prompts, levels, most=most)
+    assert len(made) == steps + 1 and [x[0].item() for x in made] == [1] * len(made)
+    assert steps <= most and not cache.refs.any() and not cache.length.any()
+    for tokens in found:
+        assert b"".join(vocab[t] for t in tokens)[:-1] in strings
+    h.close()
