@@ -435,6 +435,8 @@ struct Split {
     int vecs, threads, parts;
 };
 
+constexpr int kParts = kJoin * kJoinKeys / TAM_MAX_TOP;  // of a row, whose best k_top_join holds
+
 // Blocks of 256 threads, since smaller ones leave k_top_join more and larger ones wait for one another (us per call of 256 bf16
 // rows over V = 262,144, k_top and k_top_join, 64 threads: 32.3 and 7.4, 128: 30.1 and 4.7, 256: 29.6 and 4.1, 512: 35.7 and
 // 4.8, 1,024: 66 and 5), with as many vectors each as leave the chip 2,048 blocks; more threads only where a row would have more
@@ -447,20 +449,27 @@ Split split_of(int64_t B, int64_t V) {
     const int64_t vectors = (V + 2 * In<T>::n - 2) / In<T>::n;
     Split s{4, 256, 1};
     auto parts = [&] { return (int)((vectors + s.threads * s.vecs - 1) / (s.threads * s.vecs)); };
-    while (s.vecs < 16 && (B * parts() > 2048 || parts() > 128)) s.vecs *= 2;
-    if (parts() > 128) s.threads = 512;
+    while (s.vecs < 16 && (B * parts() > 2048 || parts() > kParts)) s.vecs *= 2;
+    if (parts() > kParts) s.threads = 512;
     if (B <= 256 && vectors <= 8192) s.vecs = vectors <= 4096 ? 4 : 8, s.threads = 1024;
     s.parts = parts();
     return s;
 }
 
+// Whether some row has too many vectors for kParts parts of 256 threads: of fp32, whose widest rows (from TAM_MAX_TOP_COLUMNS - 2 on)
+// may lie over one vector more.  These take blocks of 512 threads (256 rows, 8 of each: 343 us, in the short rows' blocks of 1,024 568).
+template <typename T>
+constexpr bool kWide = (TAM_MAX_TOP_COLUMNS + 2 * In<T>::n - 2) / In<T>::n > kParts * 256 * 16;
+
 template <typename T>
 hipError_t launch(const void *logits, int64_t B, Top a, const Split &sp, hipStream_t s) {
-    void (*kernel)(const T *, Top) = sp.threads == 512    ? k_top<T, 16, 512>
-                                     : sp.threads == 1024 ? (sp.vecs == 4 ? k_top<T, 4, 1024> : k_top<T, 8, 1024>)
-                                     : sp.vecs == 4      ? k_top<T, 4, 256>
-                                     : sp.vecs == 8      ? k_top<T, 8, 256>
-                                                       : k_top<T, 16, 256>;
+    void (*kernel)(const T *, Top) = sp.threads == 1024 ? (sp.vecs == 4 ? k_top<T, 4, 1024> : k_top<T, 8, 1024>)
+                                     : sp.vecs == 4     ? k_top<T, 4, 256>
+                                     : sp.vecs == 8     ? k_top<T, 8, 256>
+                                                        : k_top<T, 16, 256>;
+    if constexpr (kWide<T>) {
+        if (sp.threads == 512) kernel = k_top<T, 16, 512>;
+    }
     hipLaunchKernelGGL(kernel, dim3((unsigned)(B * sp.parts)), dim3((unsigned)sp.threads), 0, s, static_cast<const T *>(logits), a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || sp.parts == 1) return e;
