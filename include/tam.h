@@ -570,7 +570,7 @@ int64_t tam_pages_work(const tam_pages *c, int64_t n);
  *                   [0, c->slots) is left out.
  *   lengths         device int32[n], or NULL for the parents' whole length.
  *   work            tam_pages_work(c, n) bytes.
- * No page is copied: a last page that stays shared is copied by tam_pages_extend.
+ * n is below 2^24.  No page is copied: a last page that stays shared is copied by tam_pages_extend.
  */
 tam_status tam_pages_fork(const tam_pages *c, const int32_t *slots, const int32_t *parents, const int32_t *lengths,
                           int64_t n, void *work, void *stream);
@@ -594,7 +594,7 @@ tam_status tam_pages_extend(const tam_pages *c, const int32_t *slots, const int3
  * tam_pages_compact -- the pages in use move to the numbers 0 .. used - 1: each
  * one numbered `used` or more, in ascending order, into the next free page
  * below, in every plane, with its count and the table entries of every slot.
- * Entries past a slot's pages become -1.
+ * Entries past a slot's pages become -1.  The cache has fewer than 2^24 - 4096 slots.
  *   info   device int32[2]: pages in use, pages moved.
  *   moved  device int32[num_pages]: the new number of each page, -1 of a free one.
  *   work   tam_pages_work(c, 0) bytes.
@@ -629,6 +629,7 @@ typedef struct {
  * head h, dimension d) of the new K is at k_new[t * k_token + h * k_head + d] (a
  * multiple of 8 each, 16-byte aligned), V alike.  Tokens whose position is
  * negative, past the slot's pages or in a page outside the pool are left out.
+ * c has fewer than 2^24 tokens.
  */
 tam_status tam_pages_store(const tam_chunk *c, const void *k_new, int64_t k_token, int64_t k_head, const void *v_new,
                            int64_t v_token, int64_t v_head, void *stream);
@@ -691,8 +692,7 @@ typedef struct {
  * tam_pages_append -- tam_pages_store of the new tokens with K turned by their positions, and their queries turned alike:
  * out[t][h] of q[t][h].  Angles of up to 10^8 radians are taken modulo whole turns to fp32's last place; elements are
  * turned in fp32 and rounded once.  The tokens' places do not depend on `depth`.
- *   c              fewer than 2^24 tokens.
- *   k_new, v_new   as for tam_pages_store; the tokens that are left out there are here too.
+ *   k_new, v_new   as for tam_pages_store; the tokens that are left out there are here too, and c's are as few.
  *   q, heads, out  as for tam_attend (any number of heads); heads == 0: no queries.  Every token of a row is written; `out` may be
  *                  `q` itself, with its strides.
  * Errors: TAM_E_INVAL, TAM_E_DEVICE.

@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kBlock) k_copy(Pool p, const int32_t *__restri
     copy_pages<V>(p, src, dst, n, nullptr, blockIdx.x, gridDim.x);
 }
 
-constexpr int64_t kCopyBlocks = 256 * 16;
+constexpr int64_t kCopyBlocks = 256 * 16;  // (at most, and with the slots of a cache that tam_pages_compact takes, below 2^24)
 
 Pool pool_of(const tam_pages &c) {
     return Pool{static_cast<uint8_t *>(c.data), c.planes, c.plane_stride, c.page_stride, c.page_bytes};

@@ -103,6 +103,7 @@ const char *chunk_wrong(const tam_chunk *c, bool plane = true) {
 const char *store_wrong(const tam_chunk *c, const void *k_new, int64_t k_token, int64_t k_head, const void *v_new,
                         int64_t v_token, int64_t v_head) {
     if (const char *w = chunk_wrong(c)) return w;
+    if (c->tokens > kMostBlocks) return "tokens must be below 2^24";
     if (c->tokens > 0 && (!k_new || !v_new)) return "null device pointer";
     if (!aligned(k_new, 16) || !aligned(v_new, 16) || k_token % 8 || k_head % 8 || v_token % 8 || v_head % 8)
         return "k_new and v_new must be 16-byte aligned and their strides multiples of 8";
@@ -153,6 +154,7 @@ tam_status tam_pages_fork(const tam_pages *c, const int32_t *slots, const int32_
     tam::api_begin();
     const char *w = pages_wrong(c);
     if (!w) w = rows_wrong(c, n);
+    if (!w && n > kMostBlocks) w = "n must be below 2^24";
     if (!w && n > 0 && (!slots || !parents || !work)) w = "null device pointer";
     if (!w && !aligned(work, 16)) w = "work must be 16-byte aligned";
     if (w) return api_fail(TAM_E_INVAL, w);
@@ -178,6 +180,7 @@ tam_status tam_pages_extend(const tam_pages *c, const int32_t *slots, const int3
 tam_status tam_pages_compact(const tam_pages *c, int32_t *info, int32_t *moved, void *work, void *stream) {
     tam::api_begin();
     const char *w = pages_wrong(c);
+    if (!w && c->slots > kMostBlocks - 4096) w = "slots must be below 2^24 - 4096";  // a block each, beside those that copy pages
     if (!w && (!info || !moved || !work)) w = "null device pointer";
     if (!w && !aligned(work, 16)) w = "work must be 16-byte aligned";
     if (w) return api_fail(TAM_E_INVAL, w);
@@ -243,7 +246,6 @@ tam_status tam_pages_append(const tam_chunk *c, const tam_rotation *r, const voi
                             int64_t heads, void *out, int64_t out_token, int64_t out_head, void *stream) {
     tam::api_begin();
     const char *w = store_wrong(c, k_new, k_token, k_head, v_new, v_token, v_head);
-    if (!w && c->tokens > kMostBlocks) w = "tokens must be below 2^24";
     if (!w && !r) w = "null rotation";
     if (!w && (r->pairs < 0 || r->pairs > c->head_dim / 2 || r->pairs % 4)) w = "pairs must be a multiple of 4, at most head_dim / 2";
     if (!w && r->adjacent != 0 && r->adjacent != 1) w = "adjacent must be 0 or 1";

@@ -61,6 +61,25 @@ def test_pages_refuse_pools_that_overlap(P):
         assert b"overlap" in L.tam_last_error()
 
 
+def test_more_blocks_than_a_launch_has_are_refused(P):
+    """A token, a row or a slot takes a block of 256 threads, of which a launch has fewer than 2^32."""
+    L = P.lib()
+
+    def pages(slots):
+        return ctypes.byref(P.tam.Pages(AT, 4, 10 * 1024, 1024, 1024, 10, 16, AT, slots, 5, 5, AT, AT))
+
+    def store(tokens, k):
+        c = chunk(P, tokens=tokens)
+        return L.tam_pages_store(ctypes.byref(c), k, 256, 64, AT, 256, 64, None)
+    for call in (lambda: store(2 ** 24, AT), lambda: L.tam_pages_fork(pages(2 ** 25), AT, AT, None, 2 ** 24, AT, None),
+                 lambda: L.tam_pages_compact(pages(2 ** 24 - 4096), AT, AT, AT, None)):
+        assert call() == INVAL and b"2^24" in L.tam_last_error()
+    # as many are looked at further
+    for call in (lambda: store(2 ** 24 - 1, None), lambda: L.tam_pages_fork(pages(2 ** 25), None, AT, None, 2 ** 24 - 1, AT, None),
+                 lambda: L.tam_pages_compact(pages(2 ** 24 - 4097), None, AT, AT, None)):
+        assert call() == INVAL and b"null" in L.tam_last_error()
+
+
 class On:
     """A tensor of the CPU that says it lies on a GPU."""
 
