@@ -52,7 +52,7 @@ class Decoder:
 
 def search(model, handle, ends, prompts, width=4, most=32, presence=0.3, page_tokens=16):
     """The finished beams of each prompt, best first: [(score, tokens after the prompt)].  ``ends`` [V]: whether a
-    token closes its string."""
+    token closes its string; ``width``: beams of each prompt, up to the 64 tokens that ``top_tokens`` gives."""
     groups = len(prompts)
     B = groups * width
     int32 = dict(dtype=torch.int32, device="cuda")

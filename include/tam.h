@@ -704,7 +704,8 @@ tam_status tam_pages_append(const tam_chunk *c, const tam_rotation *r, const voi
 /*
  * tam_attend_seen -- tam_attend with a mask among the row's new tokens: a token sees the keys of its slot before the row's
  * first token, and token j of the row if j < 64 * words and bit j % 64 of seen[t * seen_stride + j / 64] is set (its own and
- * later ones too).  Bits of tokens that the row does not have are not looked at.
+ * later ones too).  Bits of tokens that the row does not have are not looked at.  As there, the weights are rounded to `dtype`
+ * before they meet V, the sum of weights is not.
  *   seen  device uint64, 8-byte aligned; words >= 1; seen_stride >= words.
  */
 tam_status tam_attend_seen(const tam_chunk *c, const void *q, int64_t q_token, int64_t q_head, int64_t heads, float scale,

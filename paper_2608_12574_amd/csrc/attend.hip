@@ -682,11 +682,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_narrow(Attend a) {
 // beside this half's exponentials.  4,096 tokens over 16,384 keys, 32 heads of 128: 905 to 980 us
 // by the card, not traced, 16 of k_join among them, 0.98 to 1.06 PFLOP/s (a bf16 product of 8,192^3 by the library: 1.23), the matrix units
 // busy in 47 cycles of 100 at the 2.1 GHz that the power leaves.  Where K and V's bytes bound it a unit takes 2.1
-// us, 4 TB/s (32 trees of up to 32 tokens over 158,700, kSeen: 658 MB in 135 to 147 us, 4.5 to 4.9 TB/s, with one block to a CU; two to four
-// units of each on their way in registers: 138 to 144).
-// In heads of up to 64 the exponentials and sums, not the products, keep the issue busy (53 cycles of 100, the matrix units 30), and a
-// second wave beside the first fills its gaps: 256 rows in eight waves of 32 (kSeen; four trees of up to 250 tokens over 116,700, 56
-// GFLOP: 92 us, in four waves of 64 108, in two blocks of 128 rows 100, whose join takes 5 more).
+// us, 4 TB/s (32 trees of up to 32 tokens over 158,700, kSeen: 658 MB in 135 to 147 us, 4.5 to 4.9 TB/s, with one block to a CU, on some
+// cards 150 to 170; two to four units of each on their way in registers: 138 to 144).
+// kSeen in tiles of 256 rows, heads of 128: 16 trees of up to 64 over 74,600 tokens, 32 and 8 heads, 52 GFLOP and 316 MB in 103 to 120 us
+// (matrix units 33 cycles of 100, vector issue 31); four of up to 250 over 134,800, 345 GFLOP in 440 to 520 (44 and 40), 0.66 to 0.78 PFLOP/s.
+// In heads of up to 64 there are more exponentials and sums to a product, and a second wave beside the first fills its gaps: 256 rows
+// in eight waves of 32 (kSeen; four trees of up to 250 tokens over 116,700, 56 GFLOP: 92 us, in four waves of 64 108, in two blocks of 128
+// rows 100, whose join takes 5 more).  Neither unit is full (vector issue 55 cycles of 100, matrix units 31): a wave issues in 45 of its
+// cycles, waits in 32, for its turn in 23.
 constexpr int kWideKeys = 64;
 
 // What is not finite in V of the keys from .. to - 1, added to the sums or outputs that this lane has written (lanes and rows as
@@ -1015,7 +1018,7 @@ __global__ void __launch_bounds__(kWave * kWaves, kWaves == 4 && kBlocks == 1 &&
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) k_in[i] = load(kh, at0, i);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) v_in[i] = load(vh, at0, i);
+            for (int i = 0; i < kLoads; ++i) v_in[i] = load(vh, at0, i);  // (with K's, or behind it: takes as long)
             __syncthreads();  // the last tile is done with the buffers
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) store_k(0, i);

@@ -442,7 +442,9 @@ constexpr int kParts = kJoin * kJoinKeys / TAM_MAX_TOP;  // of a row, whose best
 // 4.8, 1,024: 66 and 5), with as many vectors each as leave the chip 2,048 blocks; more threads only where a row would have more
 // parts than k_top_join holds.  Short rows, no more than there are CUs, take a block each, which leaves the second launch out (us
 // per call of 1, 64, 256 and 512 fp32 rows over V = 32,000, 4 of each: 8.1, 9.1, 11.9 and 22.9, in parts 8.1, 10.2, 15.2 and 21.5, and
-// 3 less on the host; 64 of each: 10.2, 11.5, 13.9 and 26.7, in parts 14.9, 17.3, 24.1 and 31.9).  Twice as long ones do not
+// 3 less on the host; 64 of each: 10.2, 11.5, 13.9 and 26.7, in parts 14.9, 17.3, 24.1 and 31.9).  More short rows than CUs go in parts:
+// of the 512's 21.5 k_top takes 16.4, k_top_join 4.0 (64 of each: 23.2 and 9.1); k_top's waves wait in 46 cycles of 100, at the barriers and
+// for the loads, and for their turn to issue in 35.  Twice as long ones do not
 // fit a block's registers: 256 bf16 rows over V = 128,256 27, in parts 22.
 template <typename T>
 Split split_of(int64_t B, int64_t V) {

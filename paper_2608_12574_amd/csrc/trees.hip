@@ -4,13 +4,14 @@
 // before the row.  Parents come before their children, so every walk up or down ends.
 //
 // k_tree: seen(j) = {j} + seen(p), depth(j) = depth(p) + 1.  A chain of LDS reads per token: 1.9 us for one tree of 16, 4.4 for 256 of
-// up to 256 tokens (31,000, 1.2 MB), where a block waits for its largest depth in each of four turns.
+// up to 256 tokens (31,000, 1.2 MB), where a block takes as long as its deepest token's chain.
 // k_walk: from token 0 on to the first child that the choice made after a token names (below 0: none); a token that stays at depth d moves to
 // place d of the row, the row's other tokens are cut off, and pages past the new length are given back.
 // k_shift: the moves themselves, in every plane.  path[d] >= d grows with d, so a place moved to is never one that
 // a later token is still to be moved from, and a thread may move its piece of the tokens in their order.  The walk is a trip to
-// memory per step of the path, the moves are bound by their bytes where there are many: 128 trees of 64 tokens in 8 layers 11.6 to
-// 13.6 us (8 MB, in one launch), 128 of 32 tokens in 32 layers 15 (45 MB).
+// memory per step of the path, the moves are bound by their bytes where there are many: 128 trees of up to 64 tokens in 8 layers 11.6 to
+// 13.6 us (8 MB, in one launch, on half of the CUs; a wave waits in 89 cycles of 100), 128 of 32 tokens in 32 layers 16 to 18 (45 MB), of
+// which the walk takes 6 and the moves 10.5 to 12 (3.7 to 4.3 TB/s; waits in 73).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -39,8 +40,8 @@ __device__ inline Span span_of(const int32_t *offsets, int64_t i, int64_t tokens
 
 // ------------------------------------------------------------------- masks ---
 
-// A block takes a row, a thread a token: up the chain of parents, in LDS where the row fits, once per word of the mask (the
-// ancestors' numbers fall, so that a word's are a run of the chain).
+// A block takes a row, a thread a token: once up the chain of parents, in LDS where the row fits (the ancestors' numbers fall, so
+// that a word's are a run of the chain, and it is written where they end).
 constexpr int kTreeThreads = 256, kHeld = 4096;
 
 __global__ void __launch_bounds__(kTreeThreads) k_tree(const int32_t *__restrict__ parents, const int32_t *__restrict__ offsets,
@@ -223,7 +224,8 @@ hipError_t launch_tree_masks(const int32_t *parents, const int32_t *offsets, int
 
 // Up to this many pieces of 16 bytes to a token (8 layers of 8 heads of 128) one launch does both, which costs the host 2.5 us
 // less.  us on the device per call of 1 and 128 trees of 32 tokens, 4 layers: 2.6 and 7.0, in two launches 3.9 and 7.4; 8 layers:
-// 5.3 and 10.4, 5.5 and 9.4; 16 layers: 7.3 and 13.5, 5.8 and 11.5.
+// 5.3 and 10.4, 5.5 and 9.4; 16 layers: 7.3 and 13.5, 5.8 and 11.5.  (The rows are not asked: many of them in 5 to 8 layers lose up to
+// 1 us by it where a graph has spared the host its part.)
 constexpr int64_t kBothItems = 2048;
 constexpr int64_t kBothRows = ((1ll << 32) - 1) / kBothThreads;  // a launch has fewer than 2^32 threads
 

@@ -177,7 +177,7 @@ def tree_masks(parents, offsets=None, longest=None, stream=None):
     """Which tokens of its row each drafted token sees.  ``parents`` int32 [tokens]: the number, in its row, of the
     token that each one follows; -1 (or whatever is no earlier token of the row): the text before the row.  Row i is
     ``offsets[i]:offsets[i + 1]`` (one token per row without ``offsets``).  ``longest``: tokens of the longest row, or more, if the
-    host knows (else all of them): the width of the masks.  Returns (int64 [tokens, ceil(longest / 64)]: bit j % 64 of word
+    host knows (else all of them, and masks that grow with the square of the call's tokens): the width of the masks.  Returns (int64 [tokens, ceil(longest / 64)]: bit j % 64 of word
     j // 64 is set for the token itself and its ancestors, as ``PageCache.attend`` takes it; int32 [tokens]: how many ancestors,
     as ``PageCache.append`` takes it).  Tokens of no row are not written."""
     where = "tam_tree_masks"
@@ -410,6 +410,7 @@ class PageCache:
         row, or more, if the host knows (a hint that chooses the launch: give it with ``offsets`` where rows are short).
         ``seen`` int64 [tokens, words]: a token sees, of its row's tokens, those j whose bit j % 64 of word j // 64 is set
         (``tree_masks``; any will do), instead of those up to itself, and all that lies before the row's first one.
+        The softmax and its sums are fp32; its weights are rounded to the cache's type before they meet V.
         Returns ``out`` (like ``q``; tokens of no row and the memory between are not written) and with ``return_lse``
         the fp32 [tokens, heads] logarithms of the sums."""
         where = "tam_attend" if seen is None else "tam_attend_seen"
